@@ -4,4 +4,6 @@ from .binding import (  # noqa: F401
     lsr_head_backward_profiled, lsr_head_forward_static, lsr_copy_probe, lsr_gather_probe, LSR_STATIC_SCRATCH_BYTES,
     lsr_head_forward, lsr_head_forward_profiled, lsr_head_plan, lsr_head_plan_ex, lsr_head_dw_route, lsr_head_workspace_bytes, lsr_mfma_peak_probe,
     lsr_status_string,
+    LSR_I8, lsr_distill_backward, lsr_distill_forward, lsr_distill_workspace_bytes, lsr_int8_matmul, lsr_int8_matmul_workspace_bytes,
+    lsr_int8_row_bytes, lsr_quantize_rows, lsr_top_logits, lsr_top_logits_workspace_bytes,
 )

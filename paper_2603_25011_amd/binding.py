@@ -1,6 +1,6 @@
 """ctypes binding of liblsr_head.so: argument marshalling only.
 
-Every function here has the name and argument order of its C entry point (include/lsr_head.h) and
+Every function here has the name and argument order of its C entry point (include/lsr_head.h, include/lsr_distill.h) and
 does nothing but turn torch tensors into device pointers and pass the current HIP stream.  All of the
 head's arithmetic runs in the HIP kernels; there is no fallback: if the library has not been built
 or cannot be loaded, importing succeeds but every call raises.
@@ -13,6 +13,7 @@ from typing import Optional
 
 LSR_F32 = 0
 LSR_BF16 = 1
+LSR_I8 = 2                    # rows of 8-bit integers (include/lsr_distill.h)
 LSR_PROFILE_SLOTS = 8
 LSR_STATIC_SCRATCH_BYTES = 16 << 20
 LSR_DW_BEHIND_DH, LSR_DW_ON_AUX_STREAM, LSR_DW_IN_PLACEMENT_LAUNCH, LSR_DW_IN_DH_LAUNCH = range(4)
@@ -35,6 +36,11 @@ class _BackwardOpts(ctypes.Structure):
 class _Desc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int64), ("S", ctypes.c_int64), ("D", ctypes.c_int64), ("V", ctypes.c_int64),
                 ("hw_dtype", ctypes.c_int32)]
+
+
+class _DistillDesc(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("D", ctypes.c_int64), ("V", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("hw_dtype", ctypes.c_int32), ("temperature", ctypes.c_float)]
 
 
 def library_path() -> str:
@@ -80,6 +86,26 @@ def load_library():
     lib.lsr_gather_probe.argtypes = [vp, sz, ctypes.c_int, ctypes.c_int, vp, sz, ctypes.POINTER(ctypes.c_double), vp]
     lib.lsr_head_backward_profiled.restype = ctypes.c_int
     lib.lsr_head_backward_profiled.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, fp]
+    i64, i32 = ctypes.c_int64, ctypes.c_int32
+    lib.lsr_int8_row_bytes.restype = i64
+    lib.lsr_int8_row_bytes.argtypes = [i64]
+    lib.lsr_quantize_rows.restype = ctypes.c_int
+    lib.lsr_quantize_rows.argtypes = [i64, i64, i32, vp, i64, vp, i64, vp, vp]
+    lib.lsr_int8_matmul_workspace_bytes.restype = sz
+    lib.lsr_int8_matmul_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.lsr_int8_matmul.restype = ctypes.c_int
+    lib.lsr_int8_matmul.argtypes = [i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+    lib.lsr_top_logits_workspace_bytes.restype = sz
+    lib.lsr_top_logits_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.lsr_top_logits.restype = ctypes.c_int
+    lib.lsr_top_logits.argtypes = [i64, i64, i64, i32, ctypes.c_float, vp, i64, vp, vp, vp, vp, sz, vp]
+    ddp = ctypes.POINTER(_DistillDesc)
+    lib.lsr_distill_workspace_bytes.restype = sz
+    lib.lsr_distill_workspace_bytes.argtypes = [ddp, ctypes.c_int]
+    lib.lsr_distill_forward.restype = ctypes.c_int
+    lib.lsr_distill_forward.argtypes = [ddp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lsr_distill_backward.restype = ctypes.c_int
+    lib.lsr_distill_backward.argtypes = [ddp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lsr_status_string.restype = ctypes.c_char_p
     lib.lsr_status_string.argtypes = [ctypes.c_int]
     _lib = lib
@@ -235,3 +261,60 @@ def lsr_head_backward_profiled(B, S, D, V, hw_dtype, H, W, dY, Y, I, dH, dW, db,
     _check(load_library().lsr_head_backward_profiled(ctypes.byref(d), _ptr(H), _ptr(W), _ptr(dY), _ptr(Y), _ptr(I),
                                                      _ptr(dH), _ptr(dW), _ptr(db), wp, wb, _stream(stream), ms))
     return list(ms)
+
+
+# ---- the operators around the dense logits (include/lsr_distill.h) ----
+
+def lsr_int8_row_bytes(cols) -> int:
+    return int(load_library().lsr_int8_row_bytes(int(cols)))
+
+
+def lsr_quantize_rows(rows, cols, x_dtype, X, ldx, Q, ldq, scale, stream=None) -> None:
+    _check(load_library().lsr_quantize_rows(int(rows), int(cols), int(x_dtype), _ptr(X), int(ldx), _ptr(Q), int(ldq), _ptr(scale),
+                                            _stream(stream)))
+
+
+def lsr_int8_matmul_workspace_bytes(N, V, K, a_dtype) -> int:
+    return int(load_library().lsr_int8_matmul_workspace_bytes(int(N), int(V), int(K), int(a_dtype)))
+
+
+def lsr_int8_matmul(N, V, K, a_dtype, out_dtype, A, lda, a_scale, W, ldw, w_scale, bias, out, ldo, workspace, stream=None) -> None:
+    wp, wb = _ws(workspace)
+    _check(load_library().lsr_int8_matmul(int(N), int(V), int(K), int(a_dtype), int(out_dtype), _ptr(A), int(lda), _ptr(a_scale),
+                                          _ptr(W), int(ldw), _ptr(w_scale), _ptr(bias), _ptr(out), int(ldo), wp, wb, _stream(stream)))
+
+
+def lsr_top_logits_workspace_bytes(rows, V, K) -> int:
+    return int(load_library().lsr_top_logits_workspace_bytes(int(rows), int(V), int(K)))
+
+
+def lsr_top_logits(rows, V, K, x_dtype, temperature, X, ldx, values, ids, lse, workspace, stream=None) -> None:
+    wp, wb = _ws(workspace)
+    _check(load_library().lsr_top_logits(int(rows), int(V), int(K), int(x_dtype), float(temperature), _ptr(X), int(ldx), _ptr(values),
+                                         _ptr(ids), _ptr(lse), wp, wb, _stream(stream)))
+
+
+def _distill_desc(N, D, V, K, hw_dtype, temperature) -> _DistillDesc:
+    return _DistillDesc(int(N), int(D), int(V), int(K), int(hw_dtype), float(temperature))
+
+
+def lsr_distill_workspace_bytes(N, D, V, K, hw_dtype, temperature, for_backward: bool) -> int:
+    d = _distill_desc(N, D, V, K, hw_dtype, temperature)
+    return int(load_library().lsr_distill_workspace_bytes(ctypes.byref(d), 1 if for_backward else 0))
+
+
+def lsr_distill_forward(N, D, V, K, hw_dtype, temperature, H, W, bias, teacher_ids, teacher_logits, teacher_lse, mask, loss, lse, workspace,
+                        stream=None) -> None:
+    d = _distill_desc(N, D, V, K, hw_dtype, temperature)
+    wp, wb = _ws(workspace)
+    _check(load_library().lsr_distill_forward(ctypes.byref(d), _ptr(H), _ptr(W), _ptr(bias), _ptr(teacher_ids), _ptr(teacher_logits),
+                                              _ptr(teacher_lse), _ptr(mask), _ptr(loss), _ptr(lse), wp, wb, _stream(stream)))
+
+
+def lsr_distill_backward(N, D, V, K, hw_dtype, temperature, H, W, bias, teacher_ids, teacher_logits, teacher_lse, mask, lse, dloss, dH, dW, db,
+                         workspace, stream=None) -> None:
+    d = _distill_desc(N, D, V, K, hw_dtype, temperature)
+    wp, wb = _ws(workspace)
+    _check(load_library().lsr_distill_backward(ctypes.byref(d), _ptr(H), _ptr(W), _ptr(bias), _ptr(teacher_ids), _ptr(teacher_logits),
+                                               _ptr(teacher_lse), _ptr(mask), _ptr(lse), _ptr(dloss), _ptr(dH), _ptr(dW), _ptr(db), wp, wb,
+                                               _stream(stream)))

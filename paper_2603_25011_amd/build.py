@@ -9,6 +9,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "liblsr_head.so")
 SRC = os.path.join(PKG, "csrc", "lsr_head.hip")
+# the operators around the head's dense logits, in the same library
+DISTILL_SRC = os.path.join(PKG, "csrc", "lsr_distill.hip")
 # benchmark comparator (the reduce step of the paper's hybrid forward); not part of the product library
 ALG2_LIB = os.path.join(PKG, "libalg2_reduce.so")
 ALG2_SRC = os.path.join(PKG, "csrc", "alg2_reduce.hip")
@@ -21,10 +23,10 @@ HIPCC_FLAGS = [
 ]
 
 
-def _compile(src: str, lib: str, verbose: bool) -> None:
+def _compile(src: list, lib: str, verbose: bool) -> None:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     cmd = [hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "csrc"),
-           "-o", lib, src]
+           f"-parallel-jobs={len(src)}", "-o", lib, *src]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -36,8 +38,8 @@ def _compile(src: str, lib: str, verbose: bool) -> None:
 
 
 def build(verbose: bool = False) -> str:
-    _compile(SRC, LIB, verbose)
-    _compile(ALG2_SRC, ALG2_LIB, verbose)
+    _compile([SRC, DISTILL_SRC], LIB, verbose)
+    _compile([ALG2_SRC], ALG2_LIB, verbose)
     return LIB
 
 

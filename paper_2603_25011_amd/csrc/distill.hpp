@@ -1,0 +1,650 @@
+// Distillation from a teacher's top logits, fused with the head: the student's N x V logits exist only as accumulator tiles.
+//
+//   z = (H W^T + bias) / T,  lse_n = log sum_v exp z_nv,  p_nj = exp(t_nj / T - L_n),  mass_n = sum_j p_nj
+//   loss_n = sum_j p_nj (t_nj / T - L_n - z_n,id + lse_n)
+//   g_nv   = dloss_n / T (mass_n exp(z_nv - lse_n) - sum_{j: id = v} p_nj),   dH = g W,  dW = g^T H,  db_v = sum_n g_nv
+//
+// Passes.  Rows that the mask leaves out are dropped first (distill_compact_kernel), the others laid out densely with whole
+// slabs (distill_rows_kernel; three planes each for float32).  The teacher's entries are bucketed by logit tile (distill_hits_kernel),
+// so that the workgroup which holds a tile in registers also finds the entries that fall into it: the forward picks their logits
+// there, the backward subtracts their probabilities there, before anything is rounded.
+//   forward   distill_logits_kernel<false>: per tile and token one (maximum, sum of exp); distill_loss_kernel joins them
+//   backward  distill_logits_kernel<true>: logits again, g in bfloat16 in two layouts for a piece of the vocabulary at a time, db from
+//             the unrounded g; distill_grads_kernel: the two products of that piece in one launch
+// The vocabulary runs along the rows of a logit tile, tokens along the columns: a lane then holds 64 logits of each of two tokens,
+// and the softmax statistics are in-lane sums with one exchange at the end.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tile_product.hpp"
+#include "top_logits.hpp"
+
+namespace lsr {
+
+// p of one entry; every kernel forms it from the same operations
+__device__ __forceinline__ float teacher_p(float t, float inv_t, float L) { return __builtin_amdgcn_exp2f(fmaf(t, inv_t, -L) * LOG2E); }
+
+// ---- rows ----
+
+// rows[0 .. *count) = the rows whose mask byte is not 0, in order; place[r] = its place among them or -1.  loss and lse of the others
+// become 0.  One workgroup.
+constexpr int COMPACT_THREADS = 1024;
+__global__ __launch_bounds__(COMPACT_THREADS) void distill_compact_kernel(const uint8_t* __restrict__ mask, int N, int* __restrict__ rows,
+                                                                          int* __restrict__ count, int* __restrict__ place,
+                                                                          float* __restrict__ loss, float* __restrict__ lse) {
+    __shared__ int s_wave[COMPACT_THREADS / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int base = 0;
+    for (int r0 = 0; r0 < N; r0 += COMPACT_THREADS) {
+        const int r = r0 + tid;
+        const bool on = r < N && mask[r] != 0;
+        const unsigned long long b = __ballot(on);
+        if (lane == 0) s_wave[wave] = __popcll(b);
+        __syncthreads();
+        int at = base + __popcll(b & ((1ull << lane) - 1ull));
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < COMPACT_THREADS / 64; ++w) {
+            at += w < wave ? s_wave[w] : 0;
+            all += s_wave[w];
+        }
+        if (on) rows[at] = r;
+        if (place && r < N) place[r] = on ? at : -1;
+        if (loss && r < N && !on) { loss[r] = 0.f; lse[r] = 0.f; }
+        base += all;
+        __syncthreads();
+    }
+    if (tid == 0) *count = base;
+}
+
+// Number of valid rows, and the row at a place: identity without a mask.
+struct RowList {
+    const int* rows;
+    const int* count;
+    int N;
+    __device__ __forceinline__ int n() const { return count ? *count : N; }
+    __device__ __forceinline__ int row(int i) const { return rows ? rows[i] : i; }
+};
+
+struct Teacher {
+    const int* ids;          // [N, K]
+    const float* logits;     // [N, K]
+    const float* given_lse;  // [N] or null
+    float* L;                // [places]
+    float* mass;             // [places]
+    int K, V;
+    float inv_t;
+    __device__ __forceinline__ bool valid(int id, float t) const { return (unsigned)id < (unsigned)V && t != -INFINITY; }
+};
+
+// One wave per valid row: the row's hidden states into whole slabs (PLANES planes of `width` elements, zeros behind D; dst null:
+// they are used where they are), and the teacher's L and mass (ids null: a matrix without a teacher).
+template <typename T, int PLANES>
+__global__ __launch_bounds__(256) void distill_rows_kernel(const T* __restrict__ X, int D, RowList list, uint16_t* __restrict__ dst,
+                                                           int width, size_t plane, Teacher t) {
+    const int lane = threadIdx.x & 63;
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (i >= list.n()) return;
+    const int64_t r = list.row(i);
+    if (dst) {
+        for (int d = lane * 8; d < width; d += 512) {
+            uint16_t o[PLANES][8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) o[q][e] = 0;
+            if (d < D) {                         // (D is a multiple of 8)
+                if constexpr (PLANES == 1) {
+                    *reinterpret_cast<uint4*>(&o[0][0]) = *reinterpret_cast<const uint4*>(X + r * D + d);
+                } else {
+                    float f[8];
+                    *reinterpret_cast<float4*>(&f[0]) = *reinterpret_cast<const float4*>(X + r * D + d);
+                    *reinterpret_cast<float4*>(&f[4]) = *reinterpret_cast<const float4*>(X + r * D + d + 4);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        uint16_t p[3];
+                        split_bf16(f[e], p);
+#pragma unroll
+                        for (int q = 0; q < PLANES; ++q) o[q][e] = p[q];
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < PLANES; ++q)
+                *reinterpret_cast<uint4*>(dst + q * plane + (size_t)i * width + d) = *reinterpret_cast<const uint4*>(&o[q][0]);
+        }
+    }
+    if (t.ids) {
+        float x[TOP_MAX_K / 64];
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < TOP_MAX_K / 64; ++k) {
+            const int j = k * 64 + lane;
+            x[k] = -INFINITY;
+            if (j < t.K) {
+                const float tl = t.logits[r * t.K + j];
+                if (t.valid(t.ids[r * t.K + j], tl)) x[k] = tl;
+            }
+            m = fmaxf(m, x[k]);
+        }
+#pragma unroll
+        for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+        float L = 0.f;
+        if (t.given_lse) {
+            L = t.given_lse[r];
+        } else {
+            const float z = finite_or_zero(m);
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < TOP_MAX_K / 64; ++k) s += __builtin_amdgcn_exp2f((x[k] - z) * (t.inv_t * LOG2E));
+#pragma unroll
+            for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+            L = s == 0.f ? 0.f : fmaf(z, t.inv_t, logf(s));
+        }
+        float mass = 0.f;
+#pragma unroll
+        for (int k = 0; k < TOP_MAX_K / 64; ++k) mass += x[k] == -INFINITY ? 0.f : teacher_p(x[k], t.inv_t, L);
+#pragma unroll
+        for (int o = 32; o; o >>= 1) mass += __shfl_xor(mass, o);
+        if (lane == 0) { t.L[i] = L; t.mass[i] = mass; }
+    }
+}
+
+// dst[q][c][i] = src[q][i][c] for i < rows, 0 for rows <= i < rows_up (both in elements of bfloat16); 64 x 64 pieces.
+// rows comes from the list (hidden states) or is a constant (a piece of the matrix).
+__global__ __launch_bounds__(256) void distill_transpose_kernel(const uint16_t* __restrict__ src, int src_pitch, size_t src_plane, RowList list,
+                                                                int cols, uint16_t* __restrict__ dst, int dst_pitch, size_t dst_plane) {
+    __shared__ uint16_t s[64][66];
+    const int n = list.n();
+    const int i0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    if (i0 >= (n + 255) / 256 * 256) return;      // whole tiles: what lies behind n is zero
+    src += blockIdx.z * src_plane;
+    dst += blockIdx.z * dst_plane;
+    const int a = threadIdx.x & 31, b = threadIdx.x >> 5;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * 8 + b, c = c0 + 2 * a;
+        uint32_t w = 0;
+        if (i < n && c < cols) w = *reinterpret_cast<const uint32_t*>(src + (size_t)i * src_pitch + c);   // (cols is even)
+        s[k * 8 + b][2 * a] = (uint16_t)w;
+        s[k * 8 + b][2 * a + 1] = (uint16_t)(w >> 16);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int c = c0 + k * 8 + b;
+        if (c < cols)
+            *reinterpret_cast<uint32_t*>(dst + (size_t)c * dst_pitch + i0 + 2 * a) = s[2 * a][k * 8 + b] | (uint32_t)s[2 * a + 1][k * 8 + b] << 16;
+    }
+}
+
+// ---- the teacher's entries by logit tile ----
+
+// hits[tt 256 K + first[tt][vt] .. first[tt][vt + 1]) = the entries of token tile tt that fall into vocabulary tile vt: .x = place in the
+// token tile << 16 | place in the vocabulary tile << 8 | j, .y = p.  Entries with p = 0 are left out.  One workgroup per token tile: a count,
+// a prefix sum, a placement (the order within a bucket is free: every entry has its own result).
+constexpr int HITS_THREADS = 1024;
+__global__ __launch_bounds__(HITS_THREADS) void distill_hits_kernel(Teacher t, RowList list, int n_vt, int2* __restrict__ hits,
+                                                                    int* __restrict__ first) {
+    extern __shared__ int s_cnt[];               // [n_vt]
+    __shared__ int s_wave[HITS_THREADS / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = list.n();
+    const int i0 = blockIdx.x * TP_T;
+    if (i0 >= n) return;
+    const int live = min(TP_T, n - i0) * t.K;
+    for (int v = tid; v < n_vt; v += HITS_THREADS) s_cnt[v] = 0;
+    __syncthreads();
+    auto entry = [&](int e, int& id, int& tok, int& j) -> float {
+        tok = e / t.K;
+        j = e - tok * t.K;
+        const int64_t at = (int64_t)list.row(i0 + tok) * t.K + j;
+        id = t.ids[at];
+        const float tl = t.logits[at];
+        return t.valid(id, tl) ? teacher_p(tl, t.inv_t, t.L[i0 + tok]) : 0.f;
+    };
+    for (int e = tid; e < live; e += HITS_THREADS) {
+        int id, tok, j;
+        if (entry(e, id, tok, j) != 0.f) atomicAdd(&s_cnt[id >> 8], 1);
+    }
+    __syncthreads();
+    int base = 0;
+    int* const out = first + (size_t)blockIdx.x * (n_vt + 1);
+    for (int v0 = 0; v0 < n_vt; v0 += HITS_THREADS) {
+        const int v = v0 + tid;
+        const int c = v < n_vt ? s_cnt[v] : 0;
+        int x = c;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 63) s_wave[wave] = x;
+        __syncthreads();
+        int at = base + x - c, all = 0;
+#pragma unroll
+        for (int w = 0; w < HITS_THREADS / 64; ++w) {
+            at += w < wave ? s_wave[w] : 0;
+            all += s_wave[w];
+        }
+        if (v < n_vt) { s_cnt[v] = at; out[v] = at; }
+        base += all;
+        __syncthreads();
+    }
+    if (tid == 0) out[n_vt] = base;
+    int2* const list_out = hits + (size_t)i0 * t.K;
+    for (int e = tid; e < live; e += HITS_THREADS) {
+        int id, tok, j;
+        const float p = entry(e, id, tok, j);
+        if (p != 0.f) list_out[atomicAdd(&s_cnt[id >> 8], 1)] = make_int2(tok << 16 | (id & 255) << 8 | j, __float_as_int(p));
+    }
+}
+
+// ---- logits ----
+
+struct LogitsParams {
+    const void* W;             // bfloat16 planes, whole slabs
+    const void* Hc;            // valid rows, the same
+    size_t w_pitch, h_pitch;   // bytes of a row
+    SlabWalk walk;             // A = W
+    const float* bias;
+    RowList list;
+    const int2* hits;
+    const int* first;
+    int n_vt;                  // tiles of the whole vocabulary
+    int vt0, nvt;              // those of this launch
+    int V, K, ga;
+    float inv_t;
+    // forward
+    float2* part;              // [n_vt][places]: (maximum, sum of exp) of a tile's logits of a token
+    int places;                // pitch of part: N
+    float* picked;             // [N, K] logits at the teacher's ids (times temperature: as the product gives them)
+    // backward
+    const float* lse;          // [N]
+    const float* dloss;        // [N]
+    const float* mass;         // [places]
+    uint16_t* G;               // [planes][places up to 256][g_pitch]: g of this piece, vocabulary contiguous; null if not wanted
+    uint16_t* Gt;              // [planes][vocabulary of the piece][gt_pitch]: tokens contiguous; null if not wanted
+    int g_pitch, gt_pitch;
+    size_t g_plane, gt_plane;
+    float* db_part;            // [token tiles][V up to 256]; null if not wanted
+    int db_pitch;
+};
+
+// Sets element = f(element, owner, hit, p) for the hits of this wave: the entries of the tile's bucket that lie in its 128 x 64 part, one after
+// the other; `element` is the accumulator of the entry, in lane `owner`.  The bucket is read 64 entries at a time; the accumulator's
+// index is wave-uniform, so the choice is a jump, not a search.
+template <typename F>
+__device__ __forceinline__ void for_hits(const LogitsParams& p, int tt, int vt, const TileLane& t, floatx16 (&acc)[4][2], F&& f) {
+    const int* const first = p.first + (size_t)tt * (p.n_vt + 1) + vt;
+    const int lo = first[0], hi = first[1];
+    const int2* const hits = p.hits + (size_t)tt * TP_T * p.K;
+    for (int h0 = lo; h0 < hi; h0 += 64) {
+        int2 e = make_int2(0, 0);
+        const bool in = h0 + t.lane < hi;
+        if (in) e = hits[h0 + t.lane];
+        const int tok = e.x >> 16, v = e.x >> 8 & 255;
+        unsigned long long mine = __ballot(in && (tok >> 6) == t.wn && ((v >> 5) & 1) == t.wm);
+        while (mine) {
+            const int l = __builtin_ctzll(mine);
+            mine &= mine - 1;
+            const int hx = __builtin_amdgcn_readlane(e.x, l), hy = __builtin_amdgcn_readlane(e.y, l);
+            const int htok = hx >> 16, hv = hx >> 8 & 255;
+            const int owner = ((hv >> 2) & 1) * 32 + (htok & 31);
+            // accumulator (i, c, r): block hv / 64, column block (htok / 32) % 2, register 4 ((hv % 32) / 8) + hv % 4
+            const int at = (hv >> 6) * 32 + ((htok >> 5) & 1) * 16 + ((hv & 31) >> 3) * 4 + (hv & 3);
+#define LSR_HIT1(n) case n: acc[(n) >> 5][((n) >> 4) & 1][(n) & 15] = f(acc[(n) >> 5][((n) >> 4) & 1][(n) & 15], owner, hx, hy); break;
+#define LSR_HIT4(n) LSR_HIT1(n) LSR_HIT1(n + 1) LSR_HIT1(n + 2) LSR_HIT1(n + 3)
+#define LSR_HIT16(n) LSR_HIT4(n) LSR_HIT4(n + 4) LSR_HIT4(n + 8) LSR_HIT4(n + 12)
+            switch (at) {
+                LSR_HIT16(0) LSR_HIT16(16) LSR_HIT16(32) LSR_HIT16(48)
+                LSR_HIT16(64) LSR_HIT16(80) LSR_HIT16(96) LSR_HIT16(112)
+            }
+#undef LSR_HIT16
+#undef LSR_HIT4
+#undef LSR_HIT1
+        }
+    }
+}
+
+template <bool SPLIT, bool BWD>
+__global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsParams p) {
+    __shared__ __attribute__((aligned(1024))) uint8_t s_ring0[TP_STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_ring1[TP_STAGE];
+    __shared__ __attribute__((aligned(16))) float s_bias[TP_T];
+    __shared__ __attribute__((aligned(16))) float2 s_stat[2][TP_T];       // forward: per wave row; backward: db per wave column
+    const int n = p.list.n();
+    const int ntt = (n + TP_T - 1) / TP_T;
+    int u, vt, tt;
+    if (!xcd_unit(p.nvt * ntt, u)) return;
+    tile_of_unit(u, p.nvt, ntt, p.ga, vt, tt);
+    vt += p.vt0;
+    const TileLane t;
+    const int v0 = vt * TP_T, i0 = tt * TP_T;
+    // entries behind the vocabulary: logits of -inf
+    if (t.tid < TP_T) s_bias[t.tid] = v0 + t.tid < p.V ? p.bias[v0 + t.tid] : -INFINITY;
+
+    floatx16 acc[4][2];
+    tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, p.W, p.w_pitch, v0, p.V, p.Hc, p.h_pitch, i0, n, p.walk, acc);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(&s_bias[t.row(i, r)]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                acc[i][c][r] += b.x; acc[i][c][r + 1] += b.y; acc[i][c][r + 2] += b.z; acc[i][c][r + 3] += b.w;
+            }
+        }
+
+    if constexpr (!BWD) {
+        for_hits(p, tt, vt, t, acc, [&](float z, int owner, int hx, int) -> float {
+            if (t.lane == owner) p.picked[(size_t)(i0 + (hx >> 16)) * p.K + (hx & 255)] = z;
+            return z;
+        });
+        const float cc = p.inv_t * LOG2E;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) m = fmaxf(m, acc[i][c][r]);
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float z = finite_or_zero(m);
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][c][r] - z) * cc);
+            s += __shfl_xor(s, 32);
+            if (t.half == 0) s_stat[t.wm][t.col(c)] = make_float2(m, s);
+        }
+        __syncthreads();
+        if (t.tid < TP_T && i0 + t.tid < n) {
+            const float2 a = s_stat[0][t.tid], b = s_stat[1][t.tid];
+            const ExpSum e = join(ExpSum{a.x, a.y}, ExpSum{b.x, b.y}, cc);
+            p.part[(size_t)vt * p.places + i0 + t.tid] = make_float2(e.m, e.s);
+        }
+    } else {
+        // g: dloss / T (mass exp(z - lse) - p), the subtraction before any rounding
+        float gs[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int i = i0 + t.col(c);
+            float ga = 0.f, lse = 0.f;
+            gs[c] = 0.f;
+            if (i < n) {
+                const int r = p.list.row(i);
+                gs[c] = p.dloss[r] * p.inv_t;
+                ga = gs[c] * p.mass[i];
+                lse = p.lse[r];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    acc[k][c][r] = i < n ? ga * __builtin_amdgcn_exp2f(fmaf(acc[k][c][r], p.inv_t, -lse) * LOG2E) : 0.f;
+        }
+        for_hits(p, tt, vt, t, acc, [&](float g, int owner, int hx, int hy) -> float {
+            const float s = (hx >> 16) & 32 ? gs[1] : gs[0];
+            return t.lane == owner ? g - s * __int_as_float(hy) : g;
+        });
+
+        if (p.db_part) {
+            // sums over the wave's 64 tokens: 64 row sums, folded over the 32 lanes of a half-wave so that lane l ends with those of
+            // rows 2 l and 2 l + 1 of its half's 64
+            float x[64];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[i * 16 + r] = acc[i][0][r] + acc[i][1][r];
+#pragma unroll
+            for (int k = 0; k < 5; ++k) {
+                const int o = 16 >> k, len = 32 >> k;
+                const bool up = t.lane & o;
+#pragma unroll
+                for (int q = 0; q < len; ++q) {
+                    const float keep = up ? x[q + len] : x[q], send = up ? x[q] : x[q + len];
+                    x[q] = keep + __shfl_xor(send, o);
+                }
+            }
+            float* const s_db = reinterpret_cast<float*>(&s_stat[0][0]);      // [4][TP_T]
+            static_assert(sizeof(s_stat) >= 4 * TP_T * sizeof(float), "db of four wave columns");
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int e = t.l32 * 2 + q;                                  // element 16 i + r
+                s_db[t.wn * TP_T + acc_row(2 * (e >> 4) + t.wm, e & 15, t.half)] = x[q];
+            }
+            __syncthreads();
+            if (t.tid < TP_T)
+                p.db_part[(size_t)tt * p.db_pitch + v0 + t.tid] = (s_db[t.tid] + s_db[TP_T + t.tid]) + (s_db[2 * TP_T + t.tid] + s_db[3 * TP_T + t.tid]);
+        }
+
+        // the tile through LDS (the ring is free), in whole 512-byte rows of either layout
+        auto half_tile = [&](int row) -> uint8_t* { return row < TP_T / 2 ? s_ring0 + row * 512 : s_ring1 + (row - TP_T / 2) * 512; };
+        const int vp = (vt - p.vt0) * TP_T;
+        constexpr int PLANES = SPLIT ? 3 : 1;
+#pragma unroll
+        for (int q = 0; q < PLANES; ++q) {
+            auto plane_bits = [&](float g) -> uint16_t {
+                if constexpr (!SPLIT) return bf16_bits(g);
+                else {
+                    uint16_t b[3];
+                    split_bf16(g, b);
+                    return b[q];
+                }
+            };
+            if (p.G) {
+                __syncthreads();
+                // token rows; 16-byte chunks (8 entries) XORed with the token, so that the 32 tokens of a store lie on different banks
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int r = 0; r < 16; r += 4) {
+                            const int v = t.row(i, r), tok = t.col(c);
+                            const uint32_t lo = plane_bits(acc[i][c][r]) | (uint32_t)plane_bits(acc[i][c][r + 1]) << 16;
+                            const uint32_t hi = plane_bits(acc[i][c][r + 2]) | (uint32_t)plane_bits(acc[i][c][r + 3]) << 16;
+                            *reinterpret_cast<uint2*>(half_tile(tok) + (((v >> 3) ^ (tok & 31)) << 4) + (v & 4) * 2) = make_uint2(lo, hi);
+                        }
+                __syncthreads();
+#pragma unroll 4
+                for (int k = 0; k < 16; ++k) {
+                    const int tok = k * 16 + t.wave * 2 + t.half;
+                    const uint4 w = *reinterpret_cast<const uint4*>(half_tile(tok) + ((t.l32 ^ (tok & 31)) << 4));
+                    *reinterpret_cast<uint4*>(p.G + q * p.g_plane + (size_t)(i0 + tok) * p.g_pitch + vp + t.l32 * 8) = w;
+                }
+            }
+            if (p.Gt) {
+                __syncthreads();
+                // vocabulary rows; the half-waves, four rows apart, XORed onto different banks
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int v = t.row(i, r), tok = t.col(c);
+                            *reinterpret_cast<uint16_t*>(half_tile(v) + (((tok >> 3) ^ (v & 4)) << 4) + (tok & 7) * 2) = plane_bits(acc[i][c][r]);
+                        }
+                __syncthreads();
+#pragma unroll 4
+                for (int k = 0; k < 16; ++k) {
+                    const int v = k * 16 + t.wave * 2 + t.half;
+                    const uint4 w = *reinterpret_cast<const uint4*>(half_tile(v) + ((t.l32 ^ (v & 4)) << 4));
+                    *reinterpret_cast<uint4*>(p.Gt + q * p.gt_plane + (size_t)(vp + v) * p.gt_pitch + i0 + t.l32 * 8) = w;
+                }
+            }
+        }
+    }
+}
+
+// ---- loss ----
+
+// One group of 16 threads per token: the tiles' statistics joined, then the teacher's entries.
+constexpr int LOSS_THREADS = 1024;
+constexpr int LOSS_TOKENS = 64;
+constexpr int LOSS_GROUPS = LOSS_THREADS / LOSS_TOKENS;
+__global__ __launch_bounds__(LOSS_THREADS) void distill_loss_kernel(Teacher t, RowList list, const float2* __restrict__ part, int n_vt, int places,
+                                                                    const float* __restrict__ picked, float* __restrict__ loss,
+                                                                    float* __restrict__ lse_out) {
+    __shared__ float2 s_part[LOSS_GROUPS][LOSS_TOKENS];
+    __shared__ float s_sum[LOSS_GROUPS][LOSS_TOKENS];
+    const int n = list.n();
+    const int tok = threadIdx.x % LOSS_TOKENS, grp = threadIdx.x / LOSS_TOKENS;
+    const int i = blockIdx.x * LOSS_TOKENS + tok;
+    if (blockIdx.x * LOSS_TOKENS >= n) return;
+    const float cc = t.inv_t * LOG2E;
+    ExpSum e = {-INFINITY, 0.f};
+    if (i < n)
+        for (int v = grp; v < n_vt; v += LOSS_GROUPS) {
+            const float2 x = part[(size_t)v * places + i];
+            e = join(e, ExpSum{x.x, x.y}, cc);
+        }
+    s_part[grp][tok] = make_float2(e.m, e.s);
+    __syncthreads();
+    e = {-INFINITY, 0.f};
+#pragma unroll
+    for (int g = 0; g < LOSS_GROUPS; ++g) e = join(e, ExpSum{s_part[g][tok].x, s_part[g][tok].y}, cc);
+    const float lse = e.m == -INFINITY ? e.m : fmaf(e.m, t.inv_t, logf(e.s));
+    float sum = 0.f;
+    if (i < n) {
+        const int64_t r = list.row(i);
+        const float L = t.L[i];
+        for (int j = grp; j < t.K; j += LOSS_GROUPS) {
+            const float tl = t.logits[r * t.K + j];
+            if (!t.valid(t.ids[r * t.K + j], tl)) continue;
+            const float p = teacher_p(tl, t.inv_t, L);
+            if (p != 0.f) sum += p * (fmaf(tl, t.inv_t, -L) - fmaf(picked[(size_t)i * t.K + j], t.inv_t, -lse));
+        }
+    }
+    s_sum[grp][tok] = sum;
+    __syncthreads();
+    if (grp == 0 && i < n) {
+        float all = 0.f;
+#pragma unroll
+        for (int g = 0; g < LOSS_GROUPS; ++g) all += s_sum[g][tok];
+        const int64_t r = list.row(i);
+        loss[r] = all;
+        lse_out[r] = lse;
+    }
+}
+
+// ---- gradients ----
+
+struct GradsParams {
+    RowList list;
+    // dW [piece, D] = Gt Ht^T over the tokens
+    const void* Gt; const void* Ht; size_t gt_pitch, ht_pitch, gt_plane, ht_plane;     // bytes
+    void* dW;                  // of the piece; null if not wanted
+    int nv;                    // vocabulary entries of the piece
+    // dH_part[split] [places, D] (+)= G Wt^T over the piece
+    const void* G; const void* Wt; size_t g_pitch, wt_pitch, g_plane, wt_plane;        // bytes
+    float* dh_part;            // null if not wanted
+    size_t dh_plane;           // elements
+    int splits, accumulate;
+    int D, nd;                 // hidden size, tiles of it
+    int ga;
+};
+
+template <typename OT>
+__device__ __forceinline__ void store_tile(const TileLane& t, const floatx16 (&acc)[4][2], OT* out, size_t pitch, int rows, int cols, bool add) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = t.row(i, r);
+            if (row < rows) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int col = t.col(c);
+                    if (col < cols) {
+                        OT* const o = out + (size_t)row * pitch + col;
+                        if constexpr (sizeof(OT) == 4) *o = add ? *o + acc[i][c][r] : acc[i][c][r];
+                        else *o = bf16_bits(acc[i][c][r]);
+                    }
+                }
+            }
+        }
+}
+
+// Both products of a piece of the vocabulary: units of dW first, then those of dH, whose contracted axis (the piece) is cut into
+// `splits`, each with a plane of partial sums of its own.
+template <bool SPLIT, typename OT>
+__global__ __launch_bounds__(TP_THREADS, 2) void distill_grads_kernel(GradsParams p) {
+    __shared__ __attribute__((aligned(1024))) uint8_t s_ring0[TP_STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_ring1[TP_STAGE];
+    const int n = p.list.n();
+    const int ntt = (n + TP_T - 1) / TP_T;
+    const int nvt = (p.nv + TP_T - 1) / TP_T;
+    const int w_units = p.dW ? nvt * p.nd : 0;
+    const int h_units = p.dh_part ? ntt * p.nd : 0;
+    int u;
+    if (!xcd_unit(w_units + h_units * p.splits, u)) return;
+    const TileLane t;
+    floatx16 acc[4][2];
+    int at, bt;
+    SlabWalk walk;
+    if (u < w_units) {
+        tile_of_unit(u, nvt, p.nd, p.ga, at, bt);
+        walk.nkp = (n + 63) / 64;
+        walk.nk = SPLIT ? walk.nkp * TP_PAIRS : walk.nkp;
+        walk.a_plane = p.gt_plane;
+        walk.b_plane = p.ht_plane;
+        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, p.Gt, p.gt_pitch, at * TP_T, p.nv, p.Ht, p.ht_pitch, bt * TP_T, p.D, walk, acc);
+        store_tile(t, acc, reinterpret_cast<OT*>(p.dW) + (size_t)at * TP_T * p.D + bt * TP_T, p.D, p.nv - at * TP_T, p.D - bt * TP_T, false);
+    } else {
+        u -= w_units;
+        const int s = u / h_units;
+        tile_of_unit(u - s * h_units, ntt, p.nd, p.ga, at, bt);
+        const int slabs = (p.nv + 63) / 64;
+        const int k0 = (int)((long long)slabs * s / p.splits);
+        walk.nkp = (int)((long long)slabs * (s + 1) / p.splits) - k0;
+        walk.nk = SPLIT ? walk.nkp * TP_PAIRS : walk.nkp;
+        walk.a_plane = p.g_plane;
+        walk.b_plane = p.wt_plane;
+        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, reinterpret_cast<const char*>(p.G) + (size_t)k0 * TP_RB, p.g_pitch, at * TP_T, n,
+                                    reinterpret_cast<const char*>(p.Wt) + (size_t)k0 * TP_RB, p.wt_pitch, bt * TP_T, p.D, walk, acc);
+        store_tile(t, acc, p.dh_part + s * p.dh_plane + (size_t)at * TP_T * p.D + bt * TP_T, p.D, n - at * TP_T, p.D - bt * TP_T, p.accumulate != 0);
+    }
+}
+
+// dH from its partial sums (rows left out: 0), four elements per thread.
+template <typename OT>
+__global__ __launch_bounds__(256) void distill_dh_kernel(const float* __restrict__ part, size_t plane, int splits, const int* __restrict__ place, int N,
+                                                         int D, OT* __restrict__ dH) {
+    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int per = D / 4;
+    if (q >= (int64_t)N * per) return;
+    const int r = (int)(q / per), d = (int)(q - (int64_t)r * per) * 4;
+    const int i = place ? place[r] : r;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i >= 0) {
+        for (int k = 0; k < splits; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(part + k * plane + (size_t)i * D + d);
+            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        }
+    }
+    OT* const o = dH + (size_t)r * D + d;
+    if constexpr (sizeof(OT) == 4) {
+        *reinterpret_cast<float4*>(o) = s;
+    } else {
+        *reinterpret_cast<uint2*>(o) = make_uint2(bf16_bits(s.x) | (uint32_t)bf16_bits(s.y) << 16, bf16_bits(s.z) | (uint32_t)bf16_bits(s.w) << 16);
+    }
+}
+
+// db from the token tiles' sums.
+__global__ __launch_bounds__(256) void distill_db_kernel(const float* __restrict__ part, int pitch, RowList list, int V, float* __restrict__ db) {
+    const int v = blockIdx.x * 256 + threadIdx.x;
+    if (v >= V) return;
+    const int ntt = (list.n() + TP_T - 1) / TP_T;
+    float s = 0.f;
+    for (int k = 0; k < ntt; ++k) s += part[(size_t)k * pitch + v];
+    db[v] = s;
+}
+
+}  // namespace lsr

@@ -69,6 +69,8 @@ namespace lsr {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef int intx16 __attribute__((ext_vector_type(16)));
 
 constexpr int FWD_TM = 256;        // tile rows (tokens)
 // A workgroup has 2 x NWN waves: two wave rows (wm) that split the tile's row blocks, NWN wave
@@ -167,6 +169,10 @@ __device__ __forceinline__ floatx16 mma_chunk(floatx4 a, floatx4 b, floatx16 c) 
     for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
     return c;
 }
+// (8-bit integers: 32 elements of K per k-step, one MFMA; sums are exact, so their order is free)
+__device__ __forceinline__ intx16 mma_chunk(intx4 a, intx4 b, intx16 c) {
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
+}
 __device__ __forceinline__ bf16x8 in_k_order(bf16x8 f) { return f; }
 __device__ __forceinline__ floatx4 in_k_order(floatx4 f) {
     // lower half-wave: elements 0..3 of the k-step, upper: 4..7.  A swap exchanges the upper half of its first
@@ -208,10 +214,10 @@ __device__ __forceinline__ void mma_slab(const uint8_t* sa, int a_stride, const 
 //           k-steps 0 .. KS-2 (reading 1 .. KS-1)
 //   MODE 2  after the last slab of the tile: its k-step KS-1
 // The order of the MFMAs on every accumulator is the same as without the rotation.
-template <int NA, int KS, int MODE, int NDMA, int SPREAD, typename Frag, typename DmaFn>
+template <int NA, int KS, int MODE, int NDMA, int SPREAD, typename Frag, typename Acc, typename DmaFn>
 __device__ __forceinline__ void mma_rot(const uint8_t* sa, int a_stride, const uint8_t* sb, int b_stride,
                                         const int (&fsw)[KS], Frag (&fa)[2][4], Frag (&fb)[2][2],
-                                        floatx16 (&acc)[4][2], DmaFn&& dma) {
+                                        Acc (&acc)[4][2], DmaFn&& dma) {
     static_assert(KS % 2 == 0 && KS >= 2, "buffer parity must not depend on the slab");
     constexpr int M = NA * 2;
     constexpr int Q = SPREAD > 0 ? NDMA / SPREAD : 0;

@@ -1,0 +1,476 @@
+// C ABI of the operators around the head's dense logits: host-side validation, workspace layout and kernel launches.
+// See include/lsr_distill.h for the contract of every entry point.
+#include "lsr_distill.h"
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "distill.hpp"
+#include "host_checks.hpp"
+#include "int8_product.hpp"
+#include "quantize.hpp"
+#include "top_logits.hpp"
+
+namespace {
+
+using namespace lsr;
+
+constexpr int64_t INT8_MAX_K = 65536;
+constexpr int64_t MAX_INDEX = (int64_t(1) << 31) - 4096;
+
+inline bool float_type(int32_t t) { return t == LSR_F32 || t == LSR_BF16; }
+inline size_t type_bytes(int32_t t) { return t == LSR_F32 ? 4 : t == LSR_BF16 ? 2 : 1; }
+inline bool off_type(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+// rows of values begin on 16-byte boundaries
+inline bool rows_on_16(const void* p, int64_t ld, size_t esize) { return !misaligned(p) && (ld * (int64_t)esize) % 16 == 0; }
+
+template <typename T>
+void launch_quantize(const void* X, int64_t ldx, int64_t rows, int cols, int8_t* Q, int64_t ldq, float* scale, hipStream_t st) {
+    const unsigned grid = (unsigned)((rows + QUANT_THREADS / 64 - 1) / (QUANT_THREADS / 64));
+    if (rows_on_16(X, ldx, sizeof(T)))
+        quantize_kernel<T, true><<<grid, QUANT_THREADS, 0, st>>>(static_cast<const T*>(X), ldx, rows, cols, Q, ldq, scale);
+    else
+        quantize_kernel<T, false><<<grid, QUANT_THREADS, 0, st>>>(static_cast<const T*>(X), ldx, rows, cols, Q, ldq, scale);
+}
+void quantize(int32_t type, const void* X, int64_t ldx, int64_t rows, int cols, int8_t* Q, int64_t ldq, float* scale, hipStream_t st) {
+    if (type == LSR_F32) launch_quantize<float>(X, ldx, rows, cols, Q, ldq, scale, st);
+    else launch_quantize<uint16_t>(X, ldx, rows, cols, Q, ldq, scale, st);
+}
+
+// Few rows: their quantised form fits the LDS of the kernel that reads W straight into registers.
+bool int8_few(int64_t N, int64_t K) {
+    return N <= FEW8_ROWS && N * few8_stride((int)up(K, 128)) <= FEW8_LDS;
+}
+
+struct Int8Ws { size_t q, scale, total; };
+Int8Ws int8_ws(int64_t N, int64_t K) {
+    Int8Ws w;
+    w.q = 0;
+    w.scale = align_up((size_t)N * up(K, 128));
+    w.total = w.scale + (size_t)N * 4;
+    return w;
+}
+
+template <typename OT>
+void launch_int8_few(const Int8Params& p, int32_t a_type, int n_cus, hipStream_t st) {
+    const int stride = few8_stride(p.row_bytes);
+    const int n_tiles = (p.V + FEW8_COLS - 1) / FEW8_COLS;
+    const unsigned grid = (unsigned)(n_tiles < 2 * n_cus ? n_tiles : 2 * n_cus);
+    const size_t lds = (size_t)p.N * stride;
+    if (a_type == LSR_I8) int8_few_kernel<int8_t, OT, true><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
+    else if (a_type == LSR_F32) {
+        if (rows_on_16(p.A, p.lda, 4)) int8_few_kernel<float, OT, true><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
+        else int8_few_kernel<float, OT, false><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
+    } else {
+        if (rows_on_16(p.A, p.lda, 2)) int8_few_kernel<uint16_t, OT, true><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
+        else int8_few_kernel<uint16_t, OT, false><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
+    }
+}
+
+// ---- top logits ----
+
+// Segments per row: enough workgroups to fill the chip where there are few rows, no segment shorter than TOP_MIN_SEG, no
+// more keys in all than the joining launch holds.
+constexpr int64_t TOP_WANTED = 2048;
+constexpr int64_t TOP_MIN_SEG = 4096;
+struct TopPlan { int splits, seg; };
+TopPlan top_plan(int64_t rows, int64_t V, int64_t K) {
+    int64_t s = (TOP_WANTED + rows - 1) / rows;
+    const int64_t by_len = V / TOP_MIN_SEG, by_keys = TOP_MERGE_KEYS / K;
+    s = s < by_len ? s : by_len;
+    s = s < by_keys ? s : by_keys;
+    s = s < 64 ? s : 64;
+    s = s < 1 ? 1 : s;
+    TopPlan p;
+    p.seg = (int)up((V + s - 1) / s, 16);
+    p.splits = (int)((V + p.seg - 1) / p.seg);
+    return p;
+}
+struct TopWs { size_t keys, sums, total; };
+TopWs top_ws(int64_t rows, const TopPlan& p, int64_t K) {
+    TopWs w = {0, 0, 0};
+    if (p.splits > 1) {
+        w.sums = align_up((size_t)rows * p.splits * K * 8);
+        w.total = w.sums + (size_t)rows * p.splits * sizeof(ExpSum);
+    }
+    return w;
+}
+bool top_shape(int64_t rows, int64_t V, int64_t K) {
+    return rows >= 1 && rows < (int64_t(1) << 31) && V >= 1 && V < MAX_INDEX && K >= 1 && K <= V && K <= TOP_MAX_K &&
+           rows * top_plan(rows, V, K).splits < (int64_t(1) << 31);
+}
+
+// ---- distillation ----
+
+struct DShape {
+    int N, D, V, K, dtype;
+    int planes;         // bfloat16 planes of an operand
+    int width;          // elements of a laid-out row: whole slabs
+    int n_up;           // N up to whole tiles
+    int n_vt, n_tt;
+    float inv_t;
+};
+int check_distill(const lsr_distill_desc* d, DShape* s) {
+    if (!d) return LSR_ERR_NULL;
+    if (!float_type(d->hw_dtype)) return LSR_ERR_DTYPE;
+    if (d->N < 1 || d->N > (int64_t(1) << 22) || d->D < 8 || d->D > 8192 || d->D % 8 != 0) return LSR_ERR_SHAPE;
+    if (d->V < 1 || d->V > (int64_t(1) << 21) || d->K < 1 || d->K > TOP_MAX_K) return LSR_ERR_SHAPE;
+    if (!(d->temperature > 0.f) || !isfinite(d->temperature) || !isfinite(1.f / d->temperature)) return LSR_ERR_SHAPE;
+    s->N = (int)d->N; s->D = (int)d->D; s->V = (int)d->V; s->K = (int)d->K; s->dtype = d->hw_dtype;
+    s->planes = s->dtype == LSR_F32 ? 3 : 1;
+    s->width = (int)up(d->D, 64);
+    s->n_up = (int)up(d->N, TP_T);
+    s->n_vt = (s->V + TP_T - 1) / TP_T;
+    s->n_tt = s->n_up / TP_T;
+    s->inv_t = 1.f / d->temperature;
+    return LSR_OK;
+}
+// Rows of H or W that are multiplied where they lie: bfloat16, whole slabs.
+bool in_place(const DShape& s) { return s.dtype == LSR_BF16 && s.D == s.width; }
+
+// The backward walks the vocabulary in pieces of whole tiles: g of a piece has at most 2^28 elements (or one tile's).
+struct Pieces { int tiles, n; };
+Pieces pieces(const DShape& s) {
+    int64_t most = (int64_t(1) << 28) / s.n_up / TP_T;
+    most = most < 1 ? 1 : most;
+    Pieces p;
+    p.n = (int)((s.n_vt + most - 1) / most);
+    p.tiles = (s.n_vt + p.n - 1) / p.n;
+    p.n = (s.n_vt + p.tiles - 1) / p.tiles;
+    return p;
+}
+// Cuts of the piece as the contracted axis of dH: units of about an eighth of a CU's share of the piece's slabs, so that the last round of
+// workgroups is short; no unit below 16 slabs.
+int dh_splits(const DShape& s, const Pieces& p, int n_cus) {
+    const int64_t nd = (s.D + TP_T - 1) / TP_T;
+    const int64_t slabs = (int64_t)p.tiles * TP_T / 64;
+    const int64_t share = ((int64_t)p.tiles * nd * (s.n_up / 64) + (int64_t)s.n_tt * nd * slabs) / n_cus;
+    int64_t want = share / 8;
+    want = want < 16 ? 16 : want;
+    int64_t k = (slabs + want - 1) / want;
+    k = k < 1 ? 1 : k;
+    return (int)(k > 8 ? 8 : k);
+}
+
+struct DWs {
+    size_t rows, count, place, L, mass, hits, first, Hc, Wc;      // both directions
+    size_t part, picked;                                          // forward
+    size_t Ht, Wt, G, Gt, db_part, dh_part;                       // backward
+    size_t total;
+    int splits;
+};
+constexpr int DH_CUS = 256;      // CUs that the number of partial sums is chosen for (a size that must not depend on the device)
+DWs distill_ws(const DShape& s, bool backward) {
+    DWs w = {};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes); return o; };
+    w.rows = take((size_t)s.N * 4);
+    w.count = take(4);
+    w.place = take((size_t)s.N * 4);
+    w.L = take((size_t)s.N * 4);
+    w.mass = take((size_t)s.N * 4);
+    w.hits = take((size_t)s.n_up * s.K * 8);
+    w.first = take((size_t)s.n_tt * (s.n_vt + 1) * 4);
+    w.Hc = take((size_t)s.planes * s.N * s.width * 2);
+    w.Wc = in_place(s) ? 0 : take((size_t)s.planes * s.V * s.width * 2);
+    if (!backward) {
+        w.part = take((size_t)s.n_vt * s.N * 8);
+        w.picked = take((size_t)s.N * s.K * 4);
+    } else {
+        const Pieces p = pieces(s);
+        const size_t pv = (size_t)p.tiles * TP_T;
+        w.splits = dh_splits(s, p, DH_CUS);
+        w.Ht = take((size_t)s.planes * s.D * s.n_up * 2);
+        w.Wt = take((size_t)s.planes * s.D * pv * 2);
+        w.G = take((size_t)s.planes * s.n_up * pv * 2);
+        w.Gt = take((size_t)s.planes * s.n_up * pv * 2);
+        w.db_part = take((size_t)s.n_tt * s.n_vt * TP_T * 4);
+        w.dh_part = take((size_t)w.splits * s.N * s.D * 4);
+    }
+    w.total = at;
+    return w;
+}
+
+// What both directions begin with: valid rows, their layout, the teacher's statistics and entries by tile.
+struct Begun {
+    RowList list;
+    Teacher teacher;
+    const void *Hc, *Wc;
+    size_t pitch, h_plane, w_plane;       // bytes
+    const int* place;
+};
+template <typename T, int PLANES>
+Begun begin(const DShape& s, const DWs& w, char* ws, const void* H, const void* W, const int32_t* ids, const float* logits, const float* given_lse,
+            const uint8_t* mask, float* loss, float* lse, hipStream_t st) {
+    Begun b;
+    int* const rows = reinterpret_cast<int*>(ws + w.rows);
+    int* const count = reinterpret_cast<int*>(ws + w.count);
+    int* const place = reinterpret_cast<int*>(ws + w.place);
+    b.list = RowList{mask ? rows : nullptr, mask ? count : nullptr, s.N};
+    b.place = mask ? place : nullptr;
+    b.teacher = Teacher{ids, logits, given_lse, reinterpret_cast<float*>(ws + w.L), reinterpret_cast<float*>(ws + w.mass), s.K, s.V, s.inv_t};
+    if (mask) distill_compact_kernel<<<1, COMPACT_THREADS, 0, st>>>(mask, s.N, rows, count, place, loss, lse);
+    const bool h_here = in_place(s) && !mask;
+    b.Hc = h_here ? H : ws + w.Hc;
+    b.Wc = in_place(s) ? W : ws + w.Wc;
+    b.pitch = (size_t)s.width * 2;
+    b.h_plane = (size_t)s.N * s.width * 2;
+    b.w_plane = (size_t)s.V * s.width * 2;
+    distill_rows_kernel<T, PLANES><<<(s.N + 3) / 4, 256, 0, st>>>(static_cast<const T*>(H), s.D, b.list,
+        h_here ? nullptr : reinterpret_cast<uint16_t*>(ws + w.Hc), s.width, b.h_plane / 2, b.teacher);
+    if (!in_place(s)) {
+        Teacher none = {};
+        distill_rows_kernel<T, PLANES><<<(s.V + 3) / 4, 256, 0, st>>>(static_cast<const T*>(W), s.D, RowList{nullptr, nullptr, s.V},
+            reinterpret_cast<uint16_t*>(ws + w.Wc), s.width, b.w_plane / 2, none);
+    }
+    distill_hits_kernel<<<s.n_tt, HITS_THREADS, (size_t)s.n_vt * 4, st>>>(b.teacher, b.list, s.n_vt, reinterpret_cast<int2*>(ws + w.hits),
+                                                                          reinterpret_cast<int*>(ws + w.first));
+    return b;
+}
+
+LogitsParams logits_params(const DShape& s, const DWs& w, char* ws, const Begun& b, const float* bias) {
+    LogitsParams p = {};
+    p.W = b.Wc; p.Hc = b.Hc;
+    p.w_pitch = p.h_pitch = b.pitch;
+    p.walk.nkp = s.width / 64;
+    p.walk.nk = p.walk.nkp * (s.planes == 3 ? TP_PAIRS : 1);
+    p.walk.a_plane = b.w_plane; p.walk.b_plane = b.h_plane;
+    p.bias = bias;
+    p.list = b.list;
+    p.hits = reinterpret_cast<const int2*>(ws + w.hits);
+    p.first = reinterpret_cast<const int*>(ws + w.first);
+    p.n_vt = s.n_vt; p.vt0 = 0; p.nvt = s.n_vt;
+    p.V = s.V; p.K = s.K; p.ga = 8; p.inv_t = s.inv_t;
+    return p;
+}
+
+template <typename T, int PLANES>
+int run_forward(const DShape& s, const void* H, const void* W, const float* bias, const int32_t* ids, const float* logits, const float* given_lse,
+                const uint8_t* mask, float* loss, float* lse, char* ws, hipStream_t st) {
+    const DWs w = distill_ws(s, false);
+    const Begun b = begin<T, PLANES>(s, w, ws, H, W, ids, logits, given_lse, mask, loss, lse, st);
+    LogitsParams p = logits_params(s, w, ws, b, bias);
+    p.part = reinterpret_cast<float2*>(ws + w.part);
+    p.places = s.N;
+    p.picked = reinterpret_cast<float*>(ws + w.picked);
+    distill_logits_kernel<PLANES == 3, false><<<xcd_grid((long long)s.n_vt * s.n_tt), TP_THREADS, 0, st>>>(p);
+    distill_loss_kernel<<<(s.N + LOSS_TOKENS - 1) / LOSS_TOKENS, LOSS_THREADS, 0, st>>>(b.teacher, b.list, p.part, s.n_vt, s.N, p.picked, loss, lse);
+    return launch_status();
+}
+
+template <typename T, int PLANES>
+int run_backward(const DShape& s, const void* H, const void* W, const float* bias, const int32_t* ids, const float* logits, const float* given_lse,
+                 const uint8_t* mask, const float* lse, const float* dloss, void* dH, void* dW, float* db, char* ws, hipStream_t st) {
+    if (!dH && !dW && !db) return LSR_OK;
+    const DWs w = distill_ws(s, true);
+    const Begun b = begin<T, PLANES>(s, w, ws, H, W, ids, logits, given_lse, mask, nullptr, nullptr, st);
+    const Pieces pc = pieces(s);
+    const int pv = pc.tiles * TP_T;
+    uint16_t* const Ht = reinterpret_cast<uint16_t*>(ws + w.Ht);
+    uint16_t* const Wt = reinterpret_cast<uint16_t*>(ws + w.Wt);
+    if (dW)
+        distill_transpose_kernel<<<dim3(s.n_up / 64, (s.D + 63) / 64, PLANES), 256, 0, st>>>(
+            static_cast<const uint16_t*>(b.Hc), s.width, b.h_plane / 2, b.list, s.D, Ht, s.n_up, (size_t)s.D * s.n_up);
+    LogitsParams p = logits_params(s, w, ws, b, bias);
+    p.lse = lse;
+    p.dloss = dloss;
+    p.mass = b.teacher.mass;
+    p.G = dH ? reinterpret_cast<uint16_t*>(ws + w.G) : nullptr;
+    p.Gt = dW ? reinterpret_cast<uint16_t*>(ws + w.Gt) : nullptr;
+    p.g_pitch = pv;
+    p.gt_pitch = s.n_up;
+    p.g_plane = p.gt_plane = (size_t)s.n_up * pv;
+    p.db_part = db ? reinterpret_cast<float*>(ws + w.db_part) : nullptr;
+    p.db_pitch = s.n_vt * TP_T;
+    GradsParams g = {};
+    g.list = b.list;
+    g.Gt = p.Gt; g.Ht = Ht;
+    g.gt_pitch = g.ht_pitch = (size_t)s.n_up * 2;
+    g.gt_plane = p.gt_plane * 2; g.ht_plane = (size_t)s.D * s.n_up * 2;
+    g.G = p.G; g.Wt = Wt;
+    g.g_pitch = g.wt_pitch = (size_t)pv * 2;
+    g.g_plane = p.g_plane * 2; g.wt_plane = (size_t)s.D * pv * 2;
+    g.dh_part = dH ? reinterpret_cast<float*>(ws + w.dh_part) : nullptr;
+    g.dh_plane = (size_t)s.N * s.D;
+    g.splits = w.splits;
+    g.D = s.D;
+    g.nd = (s.D + TP_T - 1) / TP_T;
+    g.ga = 8;
+    for (int k = 0; k < pc.n; ++k) {
+        const int v0 = k * pv;
+        const int nv = s.V - v0 < pv ? s.V - v0 : pv;
+        p.vt0 = k * pc.tiles;
+        p.nvt = (nv + TP_T - 1) / TP_T;
+        if (dH)
+            distill_transpose_kernel<<<dim3((unsigned)up(nv, TP_T) / 64, (s.D + 63) / 64, PLANES), 256, 0, st>>>(
+                static_cast<const uint16_t*>(b.Wc) + (size_t)v0 * s.width, s.width, b.w_plane / 2, RowList{nullptr, nullptr, nv}, s.D, Wt, pv,
+                (size_t)s.D * pv);
+        distill_logits_kernel<PLANES == 3, true><<<xcd_grid((long long)p.nvt * s.n_tt), TP_THREADS, 0, st>>>(p);
+        if (dH || dW) {
+            g.dW = dW ? static_cast<char*>(dW) + (size_t)v0 * s.D * sizeof(T) : nullptr;
+            g.nv = nv;
+            g.accumulate = k > 0;
+            const long long units = (dW ? (long long)p.nvt * g.nd : 0) + (dH ? (long long)s.n_tt * g.nd * g.splits : 0);
+            distill_grads_kernel<PLANES == 3, T><<<xcd_grid(units), TP_THREADS, 0, st>>>(g);
+        }
+    }
+    if (dH)
+        distill_dh_kernel<T><<<(unsigned)(((int64_t)s.N * (s.D / 4) + 255) / 256), 256, 0, st>>>(g.dh_part, g.dh_plane, g.splits, b.place, s.N, s.D,
+                                                                                                static_cast<T*>(dH));
+    if (db) distill_db_kernel<<<(s.V + 255) / 256, 256, 0, st>>>(p.db_part, p.db_pitch, b.list, s.V, db);
+    return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t lsr_int8_row_bytes(int64_t cols) { return cols < 1 || cols > INT8_MAX_K ? 0 : up(cols, 128); }
+
+int lsr_quantize_rows(int64_t rows, int64_t cols, int32_t x_dtype, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, float* scale,
+                      lsr_stream_t stream) {
+    if (!float_type(x_dtype)) return LSR_ERR_DTYPE;
+    if (rows < 1 || rows >= (int64_t(1) << 31) || cols < 1 || cols > INT8_MAX_K) return LSR_ERR_SHAPE;
+    if (ldx < cols || ldq < lsr_int8_row_bytes(cols)) return LSR_ERR_SHAPE;
+    if (!X || !Q || !scale) return LSR_ERR_NULL;
+    if (off_type(X, type_bytes(x_dtype)) || misaligned(Q) || ldq % 16 != 0 || off_type(scale, 4)) return LSR_ERR_ALIGN;
+    int n_cus = 0;
+    const int rc = check_device(&n_cus);
+    if (rc != LSR_OK) return rc;
+    quantize(x_dtype, X, ldx, rows, (int)cols, Q, ldq, scale, stream);
+    return launch_status();
+}
+
+size_t lsr_int8_matmul_workspace_bytes(int64_t N, int64_t V, int64_t K, int32_t a_dtype) {
+    if (!float_type(a_dtype) || N < 1 || N >= MAX_INDEX || V < 1 || V >= MAX_INDEX || K < 1 || K > INT8_MAX_K) return 0;
+    return int8_ws(N, K).total;
+}
+
+int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out_dtype, const void* A, int64_t lda, const float* a_scale,
+                    const int8_t* W, int64_t ldw, const float* w_scale, const float* bias, void* out, int64_t ldo, void* workspace,
+                    size_t workspace_bytes, lsr_stream_t stream) {
+    if ((!float_type(a_dtype) && a_dtype != LSR_I8) || !float_type(out_dtype)) return LSR_ERR_DTYPE;
+    if (N < 1 || N >= MAX_INDEX || V < 1 || V >= MAX_INDEX || K < 1 || K > INT8_MAX_K) return LSR_ERR_SHAPE;
+    const int64_t row_bytes = up(K, 128);
+    const int64_t ld_max = int64_t(1) << 23;
+    if (lda < (a_dtype == LSR_I8 ? row_bytes : K) || ldw < row_bytes || ldo < V || ldw > ld_max || (a_dtype == LSR_I8 && lda > ld_max)) return LSR_ERR_SHAPE;
+    const int64_t na = (N + TP_T - 1) / TP_T, nb = (V + TP_T - 1) / TP_T;
+    if (na * nb > int64_t(1) << 30) return LSR_ERR_SHAPE;
+    if (!A || !W || !w_scale || !out || (a_dtype == LSR_I8 && !a_scale)) return LSR_ERR_NULL;
+    if (a_dtype != LSR_I8 && a_scale) return LSR_ERR_DTYPE;      // values bring no scales
+    if (misaligned(W) || ldw % 16 != 0 || off_type(w_scale, 4) || off_type(bias, 4) || off_type(a_scale, 4) || off_type(out, type_bytes(out_dtype)))
+        return LSR_ERR_ALIGN;
+    if (a_dtype == LSR_I8 ? misaligned(A) || lda % 16 != 0 : off_type(A, type_bytes(a_dtype))) return LSR_ERR_ALIGN;
+    const Int8Ws w = int8_ws(N, K);
+    if (a_dtype != LSR_I8) {
+        if (!workspace || workspace_bytes < w.total) return LSR_ERR_WORKSPACE;
+        if (misaligned(workspace)) return LSR_ERR_ALIGN;
+    }
+    int n_cus = 0;
+    const int rc = check_device(&n_cus);
+    if (rc != LSR_OK) return rc;
+    Int8Params p = {};
+    p.A = A; p.a_scale = a_scale; p.W = W; p.w_scale = w_scale; p.bias = bias; p.out = out;
+    p.lda = lda; p.ldw = ldw; p.ldo = ldo;
+    p.N = (int)N; p.V = (int)V; p.K = (int)K; p.row_bytes = (int)row_bytes;
+    p.na = (int)na; p.nb = (int)nb; p.ga = 8;
+    if (int8_few(N, K)) {
+        if (out_dtype == LSR_F32) launch_int8_few<float>(p, a_dtype, n_cus, stream);
+        else launch_int8_few<uint16_t>(p, a_dtype, n_cus, stream);
+        return launch_status();
+    }
+    if (a_dtype != LSR_I8) {
+        int8_t* const q = static_cast<int8_t*>(workspace) + w.q;
+        float* const scale = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.scale);
+        quantize(a_dtype, A, lda, N, (int)K, q, row_bytes, scale, stream);
+        p.A = q; p.lda = row_bytes; p.a_scale = scale;
+    }
+    const unsigned grid = xcd_grid((long long)na * nb);
+    if (out_dtype == LSR_F32) int8_tile_kernel<float><<<grid, TP_THREADS, 0, stream>>>(p);
+    else int8_tile_kernel<uint16_t><<<grid, TP_THREADS, 0, stream>>>(p);
+    return launch_status();
+}
+
+size_t lsr_top_logits_workspace_bytes(int64_t rows, int64_t V, int64_t K) {
+    if (!top_shape(rows, V, K)) return 0;
+    return top_ws(rows, top_plan(rows, V, K), K).total;
+}
+
+int lsr_top_logits(int64_t rows, int64_t V, int64_t K, int32_t x_dtype, float temperature, const void* X, int64_t ldx, float* values, int32_t* ids,
+                   float* lse, void* workspace, size_t workspace_bytes, lsr_stream_t stream) {
+    if (!float_type(x_dtype)) return LSR_ERR_DTYPE;
+    if (!top_shape(rows, V, K) || ldx < V) return LSR_ERR_SHAPE;
+    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return LSR_ERR_SHAPE;
+    if (!X || !values || !ids) return LSR_ERR_NULL;
+    if (off_type(X, type_bytes(x_dtype)) || off_type(values, 4) || off_type(ids, 4) || off_type(lse, 4)) return LSR_ERR_ALIGN;
+    const TopPlan plan = top_plan(rows, V, K);
+    const TopWs w = top_ws(rows, plan, K);
+    if (w.total) {
+        if (!workspace || workspace_bytes < w.total) return LSR_ERR_WORKSPACE;
+        if (misaligned(workspace)) return LSR_ERR_ALIGN;
+    }
+    int n_cus = 0;
+    const int rc = check_device(&n_cus);
+    if (rc != LSR_OK) return rc;
+    TopParams p = {};
+    p.X = X; p.ldx = ldx; p.values = values; p.ids = ids; p.lse = lse;
+    p.V = (int)V; p.K = (int)K; p.splits = plan.splits; p.seg = plan.seg; p.inv_t = 1.f / temperature;
+    if (plan.splits > 1) {
+        p.part_keys = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + w.keys);
+        p.part_sums = reinterpret_cast<ExpSum*>(static_cast<char*>(workspace) + w.sums);
+    }
+    const unsigned grid = (unsigned)(rows * plan.splits);
+    if (x_dtype == LSR_F32) top_logits_kernel<float><<<grid, TOP_THREADS, 0, stream>>>(p);
+    else top_logits_kernel<uint16_t><<<grid, TOP_THREADS, 0, stream>>>(p);
+    if (plan.splits > 1) top_merge_kernel<<<(unsigned)rows, TOP_THREADS, 0, stream>>>(p);
+    return launch_status();
+}
+
+size_t lsr_distill_workspace_bytes(const lsr_distill_desc* desc, int for_backward) {
+    DShape s;
+    if (check_distill(desc, &s) != LSR_OK) return 0;
+    return distill_ws(s, for_backward != 0).total;
+}
+
+int lsr_distill_forward(const lsr_distill_desc* desc, const void* H, const void* W, const float* bias, const int32_t* teacher_ids,
+                        const float* teacher_logits, const float* teacher_lse, const uint8_t* mask, float* loss, float* lse, void* workspace,
+                        size_t workspace_bytes, lsr_stream_t stream) {
+    DShape s;
+    int rc = check_distill(desc, &s);
+    if (rc != LSR_OK) return rc;
+    if (!H || !W || !bias || !teacher_ids || !teacher_logits || !loss || !lse) return LSR_ERR_NULL;
+    if (misaligned(H) || misaligned(W) || misaligned(bias) || misaligned(teacher_ids) || misaligned(teacher_logits) || misaligned(teacher_lse) ||
+        misaligned(mask) || misaligned(loss) || misaligned(lse) || misaligned(workspace))
+        return LSR_ERR_ALIGN;
+    if (!workspace || workspace_bytes < distill_ws(s, false).total) return LSR_ERR_WORKSPACE;
+    int n_cus = 0;
+    rc = check_device(&n_cus);
+    if (rc != LSR_OK) return rc;
+    char* const ws = static_cast<char*>(workspace);
+    if (s.dtype == LSR_F32)
+        return run_forward<float, 3>(s, H, W, bias, teacher_ids, teacher_logits, teacher_lse, mask, loss, lse, ws, stream);
+    return run_forward<uint16_t, 1>(s, H, W, bias, teacher_ids, teacher_logits, teacher_lse, mask, loss, lse, ws, stream);
+}
+
+int lsr_distill_backward(const lsr_distill_desc* desc, const void* H, const void* W, const float* bias, const int32_t* teacher_ids,
+                         const float* teacher_logits, const float* teacher_lse, const uint8_t* mask, const float* lse, const float* dloss, void* dH,
+                         void* dW, float* db, void* workspace, size_t workspace_bytes, lsr_stream_t stream) {
+    DShape s;
+    int rc = check_distill(desc, &s);
+    if (rc != LSR_OK) return rc;
+    if (!H || !W || !bias || !teacher_ids || !teacher_logits || !lse || !dloss) return LSR_ERR_NULL;
+    if (misaligned(H) || misaligned(W) || misaligned(bias) || misaligned(teacher_ids) || misaligned(teacher_logits) || misaligned(teacher_lse) ||
+        misaligned(mask) || misaligned(lse) || misaligned(dloss) || misaligned(dH) || misaligned(dW) || misaligned(db) || misaligned(workspace))
+        return LSR_ERR_ALIGN;
+    if (!workspace || workspace_bytes < distill_ws(s, true).total) return LSR_ERR_WORKSPACE;
+    int n_cus = 0;
+    rc = check_device(&n_cus);
+    if (rc != LSR_OK) return rc;
+    char* const ws = static_cast<char*>(workspace);
+    if (s.dtype == LSR_F32)
+        return run_backward<float, 3>(s, H, W, bias, teacher_ids, teacher_logits, teacher_lse, mask, lse, dloss, dH, dW, db, ws, stream);
+    return run_backward<uint16_t, 1>(s, H, W, bias, teacher_ids, teacher_logits, teacher_lse, mask, lse, dloss, dH, dW, db, ws, stream);
+}
+
+}  // extern "C"

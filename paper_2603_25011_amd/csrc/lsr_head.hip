@@ -13,6 +13,7 @@
 #include "fwd_few.hpp"
 #include "fwd_mfma.hpp"
 #include "fwd_misc.hpp"
+#include "host_checks.hpp"
 #include "probes.hpp"
 
 // Scratch of lsr_head_forward_static: device memory that lives in the library's code object, one copy
@@ -23,9 +24,6 @@ static __device__ __align__(256) unsigned char scratch[LSR_STATIC_SCRATCH_BYTES]
 namespace {
 
 using namespace lsr;
-
-constexpr size_t ALIGN = 256;
-inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 
 struct Shape {
     int B, S, D, V;
@@ -43,8 +41,6 @@ int check_desc(const lsr_head_desc* d, Shape* out) {
     out->dtype = d->hw_dtype;
     return LSR_OK;
 }
-
-inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 // Chunks of the packed forward (see fwd_mfma.hpp).  The host does not know the lengths, so it sizes the
 // grid and the workspace for the longest block list the shape allows (every sequence full:
@@ -358,20 +354,6 @@ int dw_stage_rows(const Shape& s) {
     return VT >= 16 && sliced_gathers(s) ? VT : 0;
 }
 
-int check_device(int* n_cus) {
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) { (void)hipGetLastError(); return LSR_ERR_ARCH; }
-    static int ok_dev[64] = {0};     // holds the CU count once a device has been checked
-    if (dev >= 0 && dev < 64 && ok_dev[dev]) { *n_cus = ok_dev[dev]; return LSR_OK; }
-    hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) { (void)hipGetLastError(); return LSR_ERR_ARCH; }
-    if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return LSR_ERR_ARCH;
-    if (prop.multiProcessorCount < 1) return LSR_ERR_ARCH;
-    *n_cus = prop.multiProcessorCount;
-    if (dev >= 0 && dev < 64) ok_dev[dev] = prop.multiProcessorCount;
-    return LSR_OK;
-}
-
 // Device address of `scratch` on the current device, looked up once per device with that device
 // current (every GPU holds its own copy at its own address).
 int static_scratch(void** out) {
@@ -420,8 +402,6 @@ struct Prof {
         return fail ? LSR_ERR_LAUNCH : LSR_OK;
     }
 };
-
-inline int launch_status() { return hipGetLastError() == hipSuccess ? LSR_OK : LSR_ERR_LAUNCH; }
 
 // (see fwd_pack_kernel)
 bool pack_in_one_launch(const Shape& s) {

@@ -1,0 +1,169 @@
+// One 256 x 256 tile of a product A B^T on the matrix cores, operands row-major with the contracted axis
+// contiguous, accumulators left in registers for the caller's epilogue.  Shared by the logits of the distillation loss,
+// its gradients, and the 8-bit product.
+//
+// A workgroup of 8 waves (2 wave rows x 4 wave columns); wave (wm, wn) holds the tile's 32-row blocks wm, wm + 2,
+// wm + 4, wm + 6 and its columns 64 wn .. 64 wn + 63 as 4 x 2 blocks of the 32x32 MFMA.  The contracted axis is walked in slabs of
+// 128 bytes per row (64 bfloat16 or 128 int8) through two LDS stages, filled by direct global -> LDS loads that ride inside the MFMAs of
+// the slab before (mma_rot).  Rows are a multiple of 128 bytes long, zero-filled by whoever laid them out, so no slab is short.
+//
+// Float32 operands come as three bfloat16 planes whose sum is the value (split_bf16 below): the product is then the six
+// plane products of order up to 2^-16, smallest first into the same accumulators.  What is left out is of order 2^-24 of a
+// product, a float32 rounding; the matrix cores do six bfloat16 products in 0.4 of the time of one float32 product.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fwd_mfma.hpp"
+
+namespace lsr {
+
+constexpr int TP_T = 256;                         // tile rows and columns
+constexpr int TP_THREADS = 512;
+constexpr int TP_RB = 128;                        // bytes of a row per slab
+constexpr int TP_SLAB = TP_T * TP_RB;             // bytes per stage and operand
+constexpr int TP_STAGE = 2 * TP_SLAB;
+constexpr int TP_PAIRS = 6;                       // plane products of a split operand
+
+// Slab i of a walk over the contracted axis: byte offsets into A and B.
+struct SlabWalk {
+    int nk;                                       // slabs in all
+    int nkp;                                      // slabs of one plane
+    size_t a_plane, b_plane;                      // bytes between planes
+    // the planes of pair i, from the smallest product to the largest: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
+    __device__ __forceinline__ void at(bool split, int kt, size_t& ka, size_t& kb) const {
+        if (!split) { ka = kb = (size_t)kt * TP_RB; return; }
+        const int pair = __builtin_amdgcn_readfirstlane(kt / nkp), k = __builtin_amdgcn_readfirstlane(kt - pair * nkp);
+        ka = ((0x001012u >> (4 * pair)) & 3u) * a_plane + (size_t)k * TP_RB;
+        kb = ((0x010210u >> (4 * pair)) & 3u) * b_plane + (size_t)k * TP_RB;
+    }
+};
+
+template <typename Frag> struct TileAcc { typedef floatx16 type; };
+template <> struct TileAcc<intx4> { typedef intx16 type; };
+
+// Geometry of a thread in the tile.
+struct TileLane {
+    int tid, lane, wave, wm, wn, half, l32;
+    __device__ __forceinline__ TileLane() {
+        tid = threadIdx.x; lane = tid & 63; wave = tid >> 6;
+        wm = wave >> 2; wn = wave & 3; half = lane >> 5; l32 = lane & 31;
+    }
+    __device__ __forceinline__ int row(int i, int r) const { return acc_row(2 * i + wm, r, half); }
+    __device__ __forceinline__ int col(int c) const { return wn * 64 + c * 32 + l32; }
+};
+
+// A pointer that is the same in every lane, in scalar registers.
+__device__ __forceinline__ const char* uniform(const char* p) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)a), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
+    return reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
+}
+
+// acc = rows [a_row0, a_row0 + 256) of A times rows [b_row0, ..) of B.  Rows at or behind a_rows / b_rows repeat the last one (they
+// are never looked at).  Pitches and planes in bytes, pitches below 2^23.  On return every wave is past its LDS reads
+// only after the caller's next barrier.
+template <typename Frag, bool SPLIT>
+__device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, const void* A, size_t a_pitch, int a_row0, int a_rows,
+                                             const void* B, size_t b_pitch, int b_row0, int b_rows, const SlabWalk& walk,
+                                             typename TileAcc<Frag>::type (&acc)[4][2]) {
+    constexpr int KS = TP_RB / 32, LPT = 8, SPREAD = 2, CPR = TP_RB / 16, RPI = 64 / CPR, NW = 8;
+    const TileLane t;
+    const int nk = __builtin_amdgcn_readfirstlane(walk.nk);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][c][r] = 0;
+    if (nk <= 0) return;
+
+    // access j of wave w covers tile rows (8 j + w) 8 .. + 8; lane -> (row, LDS chunk lp), which holds global chunk lp ^ swizzle
+    const int lrow = t.wave * RPI + t.lane / CPR;
+    const uint32_t gch = (uint32_t)((t.lane % CPR) ^ lds_swz<TP_RB>(lrow));
+    const char* const Ab = uniform(reinterpret_cast<const char*>(A) + (size_t)a_row0 * a_pitch);
+    const char* const Bb = uniform(reinterpret_cast<const char*>(B) + (size_t)b_row0 * b_pitch);
+    uint32_t ao[4], bo[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = lrow + NW * RPI * j;
+        ao[j] = (uint32_t)min(r, a_rows - 1 - a_row0) * (uint32_t)a_pitch + gch * 16;
+        bo[j] = (uint32_t)min(r, b_rows - 1 - b_row0) * (uint32_t)b_pitch + gch * 16;
+    }
+    const uint32_t wave_lds = __builtin_amdgcn_readfirstlane(t.wave * 1024);
+    const int fa_row = t.wm * 32 + t.l32, fb_row = t.wn * 64 + t.l32;
+    int fsw[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) fsw[ks] = ((ks * 2 + t.half) ^ lds_swz<TP_RB>(t.l32)) << 4;
+
+    auto issue_one = [&](uint8_t* st, const char* ab, const char* bb, int n) {
+        const uint32_t dst = lds_addr(st) + wave_lds;
+        if (n < 4) dma16_to_lds(ab, ao[n], dst + n * 8192);
+        else dma16_to_lds(bb, bo[n - 4], dst + TP_SLAB + (n - 4) * 8192);
+    };
+    {
+        size_t ka, kb;
+        walk.at(SPLIT, 0, ka, kb);
+#pragma unroll
+        for (int n = 0; n < LPT; ++n) issue_one(ring0, Ab + ka, Bb + kb, n);
+    }
+    Frag fa[2][4], fb[2][2];
+    auto step = [&](uint8_t* st, uint8_t* other, auto mode_c, int kt) {
+        // every fragment read of the slab before has returned, and slab kt has landed
+        __builtin_amdgcn_s_waitcnt(0xC07F);     // lgkmcnt(0)
+        wait_vmcnt<0>();
+        __syncthreads();
+        const int more = __builtin_amdgcn_readfirstlane(kt + 1 < nk ? 1 : 0);
+        size_t ka, kb;
+        walk.at(SPLIT, kt + 1, ka, kb);
+        const char* ab = Ab + ka;
+        const char* bb = Bb + kb;
+        auto dma = [&](int n) {
+            if (more != 0) issue_one(other, ab, bb, n);
+        };
+        mma_rot<4, KS, decltype(mode_c)::value, LPT, SPREAD>(st + fa_row * TP_RB, 64 * TP_RB, st + TP_SLAB + fb_row * TP_RB, 32 * TP_RB,
+                                                             fsw, fa, fb, acc, dma);
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> steady{};
+    step(ring0, ring1, first, 0);
+    for (int kt = 1; kt < nk; kt += 2) {
+        step(ring1, ring0, steady, kt);
+        if (kt + 1 < nk) step(ring0, ring1, steady, kt + 1);
+    }
+    mma_rot<4, KS, 2, LPT, SPREAD>(ring0, 0, ring0, 0, fsw, fa, fb, acc, [](int) {});
+}
+
+// Units of work in the order they are handed out: workgroup ids go round-robin over the 8 XCDs, and each XCD
+// takes a contiguous eighth of the units, so that units next to each other share operand rows in its L2.
+__device__ __forceinline__ bool xcd_unit(int n_units, int& u) {
+    const int x = blockIdx.x & 7;
+    u = (int)((long long)n_units * x / 8) + (int)(blockIdx.x >> 3);
+    return u < (int)((long long)n_units * (x + 1) / 8);
+}
+inline unsigned xcd_grid(long long n_units) { return (unsigned)((n_units + 7) / 8 * 8); }
+
+// Unit u of an na x nb grid of tiles, in groups of `ga` A-tiles by all B-tiles.
+__device__ __forceinline__ void tile_of_unit(int u, int na, int nb, int ga, int& at, int& bt) {
+    const int span = ga * nb;
+    const int g = u / span, rem = u - g * span;
+    const int w = min(ga, na - g * ga);
+    bt = rem / w;
+    at = g * ga + rem - bt * w;
+}
+
+__device__ __forceinline__ uint16_t bf16_bits(float x) {
+    const __bf16 b = (__bf16)x;                   // to nearest, ties to even
+    return __builtin_bit_cast(uint16_t, b);
+}
+// x as the sum of three bfloat16: the first two cut off (exact), the rest rounded.
+__device__ __forceinline__ void split_bf16(float x, uint16_t (&p)[3]) {
+    const uint32_t b0 = __float_as_uint(x) & 0xffff0000u;
+    const float r1 = x - __uint_as_float(b0);
+    const uint32_t b1 = __float_as_uint(r1) & 0xffff0000u;
+    p[0] = (uint16_t)(b0 >> 16);
+    p[1] = (uint16_t)(b1 >> 16);
+    p[2] = bf16_bits(r1 - __uint_as_float(b1));
+}
+
+}  // namespace lsr
