@@ -105,7 +105,7 @@ typedef struct {
 } lsr_distill_desc;
 
 /* Bytes of workspace of the forward (for_backward = 0) or the backward; 0 for an invalid desc.  Neither holds an array of
- * N * V elements beyond a bounded piece: O(N (D + K + V/32) + V D) and, for the backward, two pieces of at most 2^28 + 256 N
+ * N * V elements beyond a bounded piece: O(N (D + K + V/32) + V D) and, for the backward, two pieces of at most 2^28 + 256 (N + 256)
  * bfloat16 values (three times that for LSR_F32). */
 size_t lsr_distill_workspace_bytes(const lsr_distill_desc* desc, int for_backward);
 

@@ -151,16 +151,17 @@ __global__ __launch_bounds__(256) void distill_rows_kernel(const T* __restrict__
     }
 }
 
-// dst[q][c][i] = src[q][i][c] for i < rows, 0 for rows <= i < rows_up (both in elements of bfloat16); 64 x 64 pieces.
-// rows comes from the list (hidden states) or is a constant (a piece of the matrix).
+// The transpose of rows, by slab: dst[q][c / 256][i / 64][c % 256][i % 64] = src[q][i][c] for i < rows, 0 for rows <= i < rows up to whole tiles
+// (what lies behind `cols` is never looked at).  64 x 64 pieces, planes along z.  rows comes from the list (hidden states) or is a constant (a piece of the
+// matrix); src_pitch and planes in elements, `slabs` per tile of dst.
 __global__ __launch_bounds__(256) void distill_transpose_kernel(const uint16_t* __restrict__ src, int src_pitch, size_t src_plane, RowList list,
-                                                                int cols, uint16_t* __restrict__ dst, int dst_pitch, size_t dst_plane) {
+                                                                int cols, uint16_t* __restrict__ dst, int slabs, size_t dst_plane) {
     __shared__ uint16_t s[64][66];
     const int n = list.n();
     const int i0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
-    if (i0 >= (n + 255) / 256 * 256) return;      // whole tiles: what lies behind n is zero
+    if (i0 >= (n + TP_T - 1) / TP_T * TP_T) return;
     src += blockIdx.z * src_plane;
-    dst += blockIdx.z * dst_plane;
+    dst += blockIdx.z * dst_plane + ((size_t)(c0 / TP_T) * slabs + blockIdx.x) * (TP_BLOCK / 2) + (c0 % TP_T) * 64;
     const int a = threadIdx.x & 31, b = threadIdx.x >> 5;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -173,9 +174,8 @@ __global__ __launch_bounds__(256) void distill_transpose_kernel(const uint16_t* 
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int c = c0 + k * 8 + b;
-        if (c < cols)
-            *reinterpret_cast<uint32_t*>(dst + (size_t)c * dst_pitch + i0 + 2 * a) = s[2 * a][k * 8 + b] | (uint32_t)s[2 * a + 1][k * 8 + b] << 16;
+        const int c = k * 8 + b;
+        *reinterpret_cast<uint32_t*>(dst + c * 64 + 2 * a) = s[2 * a][c] | (uint32_t)s[2 * a + 1][c] << 16;
     }
 }
 
@@ -247,7 +247,8 @@ struct LogitsParams {
     const void* W;             // bfloat16 planes, whole slabs
     const void* Hc;            // valid rows, the same
     size_t w_pitch, h_pitch;   // bytes of a row
-    SlabWalk walk;             // A = W
+    size_t w_plane, h_plane;   // bytes of a plane
+    int slabs;                 // of a row
     const float* bias;
     RowList list;
     const int2* hits;
@@ -264,56 +265,43 @@ struct LogitsParams {
     const float* lse;          // [N]
     const float* dloss;        // [N]
     const float* mass;         // [places]
-    uint16_t* G;               // [planes][places up to 256][g_pitch]: g of this piece, vocabulary contiguous; null if not wanted
-    uint16_t* Gt;              // [planes][vocabulary of the piece][gt_pitch]: tokens contiguous; null if not wanted
-    int g_pitch, gt_pitch;
-    size_t g_plane, gt_plane;
+    uint16_t* G;               // g of this piece by slab, [planes][token tiles][slabs of the piece][256 tokens][64]; null if not wanted
+    uint16_t* Gt;              // the same transposed, [planes][tiles of the piece][slabs of all tokens][256 entries][64]; null if not wanted
+    int g_slabs, gt_slabs;     // slabs of a tile
+    size_t g_plane, gt_plane;  // elements of a plane
     float* db_part;            // [token tiles][V up to 256]; null if not wanted
     int db_pitch;
 };
 
-// Sets element = f(element, owner, hit, p) for the hits of this wave: the entries of the tile's bucket that lie in its 128 x 64 part, one after
-// the other; `element` is the accumulator of the entry, in lane `owner`.  The bucket is read 64 entries at a time; the accumulator's
-// index is wave-uniform, so the choice is a jump, not a search.
-template <typename F>
-__device__ __forceinline__ void for_hits(const LogitsParams& p, int tt, int vt, const TileLane& t, floatx16 (&acc)[4][2], F&& f) {
-    const int* const first = p.first + (size_t)tt * (p.n_vt + 1) + vt;
-    const int lo = first[0], hi = first[1];
-    const int2* const hits = p.hits + (size_t)tt * TP_T * p.K;
-    for (int h0 = lo; h0 < hi; h0 += 64) {
-        int2 e = make_int2(0, 0);
-        const bool in = h0 + t.lane < hi;
-        if (in) e = hits[h0 + t.lane];
-        const int tok = e.x >> 16, v = e.x >> 8 & 255;
-        unsigned long long mine = __ballot(in && (tok >> 6) == t.wn && ((v >> 5) & 1) == t.wm);
-        while (mine) {
-            const int l = __builtin_ctzll(mine);
-            mine &= mine - 1;
-            const int hx = __builtin_amdgcn_readlane(e.x, l), hy = __builtin_amdgcn_readlane(e.y, l);
-            const int htok = hx >> 16, hv = hx >> 8 & 255;
-            const int owner = ((hv >> 2) & 1) * 32 + (htok & 31);
-            // accumulator (i, c, r): block hv / 64, column block (htok / 32) % 2, register 4 ((hv % 32) / 8) + hv % 4
-            const int at = (hv >> 6) * 32 + ((htok >> 5) & 1) * 16 + ((hv & 31) >> 3) * 4 + (hv & 3);
-#define LSR_HIT1(n) case n: acc[(n) >> 5][((n) >> 4) & 1][(n) & 15] = f(acc[(n) >> 5][((n) >> 4) & 1][(n) & 15], owner, hx, hy); break;
-#define LSR_HIT4(n) LSR_HIT1(n) LSR_HIT1(n + 1) LSR_HIT1(n + 2) LSR_HIT1(n + 3)
-#define LSR_HIT16(n) LSR_HIT4(n) LSR_HIT4(n + 4) LSR_HIT4(n + 8) LSR_HIT4(n + 12)
-            switch (at) {
-                LSR_HIT16(0) LSR_HIT16(16) LSR_HIT16(32) LSR_HIT16(48)
-                LSR_HIT16(64) LSR_HIT16(80) LSR_HIT16(96) LSR_HIT16(112)
-            }
-#undef LSR_HIT16
-#undef LSR_HIT4
-#undef LSR_HIT1
-        }
+// Half of a tile in float32 through LDS: tokens 128 h .. 128 h + 127, a row of 256 vocabulary entries each, in the ring (which
+// is free behind the product).  16-byte chunks are XORed with the token, so that writes (lanes on 32 tokens), reads along a row and reads down
+// columns (16 entries by 4 groups of 8 tokens) all spread over the banks.
+struct HalfTile {
+    uint8_t *ring0, *ring1;
+    __device__ __forceinline__ float* at(int tok, int v) const {       // tok: 0 .. 127
+        const int swz = (tok & 15) ^ ((tok >> 2) & 4);
+        return reinterpret_cast<float*>((tok < 64 ? ring0 + tok * 1024 : ring1 + (tok - 64) * 1024) + (((v >> 2) ^ swz) << 4)) + (v & 3);
     }
-}
+    __device__ __forceinline__ void write(const TileLane& t, int h, const floatx16 (&acc)[4][2]) const {
+        if (t.wn >> 1 != h) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *reinterpret_cast<float4*>(at(t.col(c) & 127, t.row(i, r))) =
+                        make_float4(acc[i][c][r], acc[i][c][r + 1], acc[i][c][r + 2], acc[i][c][r + 3]);
+    }
+};
 
 template <bool SPLIT, bool BWD>
 __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsParams p) {
     __shared__ __attribute__((aligned(1024))) uint8_t s_ring0[TP_STAGE];
     __shared__ __attribute__((aligned(1024))) uint8_t s_ring1[TP_STAGE];
     __shared__ __attribute__((aligned(16))) float s_bias[TP_T];
-    __shared__ __attribute__((aligned(16))) float2 s_stat[2][TP_T];       // forward: per wave row; backward: db per wave column
+    __shared__ float2 s_stat[BWD ? 1 : 2][BWD ? 1 : TP_T];                 // forward: (maximum, sum) per wave row
+    __shared__ float s_gs[BWD ? TP_T : 1];                                 // backward: dloss / T
     const int n = p.list.n();
     const int ntt = (n + TP_T - 1) / TP_T;
     int u, vt, tt;
@@ -326,7 +314,8 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsPar
     if (t.tid < TP_T) s_bias[t.tid] = v0 + t.tid < p.V ? p.bias[v0 + t.tid] : -INFINITY;
 
     floatx16 acc[4][2];
-    tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, p.W, p.w_pitch, v0, p.V, p.Hc, p.h_pitch, i0, n, p.walk, acc);
+    tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, row_operand(p.W, p.w_pitch, p.w_plane, v0, p.V),
+                                row_operand(p.Hc, p.h_pitch, p.h_plane, i0, n), p.slabs, acc);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -339,11 +328,24 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsPar
             }
         }
 
+    // the teacher's entries in this tile
+    const int* const first = p.first + (size_t)tt * (p.n_vt + 1) + vt;
+    const int hit0 = first[0], hit1 = first[1];
+    const int2* const hits = p.hits + (size_t)i0 * p.K;
+    const HalfTile half = {s_ring0, s_ring1};
     if constexpr (!BWD) {
-        for_hits(p, tt, vt, t, acc, [&](float z, int owner, int hx, int) -> float {
-            if (t.lane == owner) p.picked[(size_t)(i0 + (hx >> 16)) * p.K + (hx & 255)] = z;
-            return z;
-        });
+        if (hit1 > hit0) {
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                if (h) __syncthreads();
+                half.write(t, h, acc);
+                __syncthreads();
+                for (int e = hit0 + t.tid; e < hit1; e += TP_THREADS) {
+                    const int x = hits[e].x, tok = x >> 16;
+                    if (tok >> 7 == h) p.picked[(size_t)(i0 + tok) * p.K + (x & 255)] = *half.at(tok & 127, x >> 8 & 255);
+                }
+            }
+        }
         const float cc = p.inv_t * LOG2E;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -370,114 +372,93 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsPar
         }
     } else {
         // g: dloss / T (mass exp(z - lse) - p), the subtraction before any rounding
-        float gs[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int i = i0 + t.col(c);
-            float ga = 0.f, lse = 0.f;
-            gs[c] = 0.f;
+            float gs = 0.f, ga = 0.f, lse = 0.f;
             if (i < n) {
                 const int r = p.list.row(i);
-                gs[c] = p.dloss[r] * p.inv_t;
-                ga = gs[c] * p.mass[i];
+                gs = p.dloss[r] * p.inv_t;
+                ga = gs * p.mass[i];
                 lse = p.lse[r];
             }
+            if (t.wm == 0 && t.half == 0) s_gs[t.col(c)] = gs;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     acc[k][c][r] = i < n ? ga * __builtin_amdgcn_exp2f(fmaf(acc[k][c][r], p.inv_t, -lse) * LOG2E) : 0.f;
         }
-        for_hits(p, tt, vt, t, acc, [&](float g, int owner, int hx, int hy) -> float {
-            const float s = (hx >> 16) & 32 ? gs[1] : gs[0];
-            return t.lane == owner ? g - s * __int_as_float(hy) : g;
-        });
-
-        if (p.db_part) {
-            // sums over the wave's 64 tokens: 64 row sums, folded over the 32 lanes of a half-wave so that lane l ends with those of
-            // rows 2 l and 2 l + 1 of its half's 64
-            float x[64];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) x[i * 16 + r] = acc[i][0][r] + acc[i][1][r];
-#pragma unroll
-            for (int k = 0; k < 5; ++k) {
-                const int o = 16 >> k, len = 32 >> k;
-                const bool up = t.lane & o;
-#pragma unroll
-                for (int q = 0; q < len; ++q) {
-                    const float keep = up ? x[q + len] : x[q], send = up ? x[q] : x[q + len];
-                    x[q] = keep + __shfl_xor(send, o);
-                }
-            }
-            float* const s_db = reinterpret_cast<float*>(&s_stat[0][0]);      // [4][TP_T]
-            static_assert(sizeof(s_stat) >= 4 * TP_T * sizeof(float), "db of four wave columns");
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int e = t.l32 * 2 + q;                                  // element 16 i + r
-                s_db[t.wn * TP_T + acc_row(2 * (e >> 4) + t.wm, e & 15, t.half)] = x[q];
-            }
-            __syncthreads();
-            if (t.tid < TP_T)
-                p.db_part[(size_t)tt * p.db_pitch + v0 + t.tid] = (s_db[t.tid] + s_db[TP_T + t.tid]) + (s_db[2 * TP_T + t.tid] + s_db[3 * TP_T + t.tid]);
-        }
-
-        // the tile through LDS (the ring is free), in whole 512-byte rows of either layout
-        auto half_tile = [&](int row) -> uint8_t* { return row < TP_T / 2 ? s_ring0 + row * 512 : s_ring1 + (row - TP_T / 2) * 512; };
-        const int vp = (vt - p.vt0) * TP_T;
+        // where this tile's four blocks lie in either layout
+        uint16_t* const g_out = p.G + ((size_t)tt * p.g_slabs + (vt - p.vt0) * 4) * (TP_BLOCK / 2);
+        uint16_t* const gt_out = p.Gt + ((size_t)(vt - p.vt0) * p.gt_slabs + tt * 4) * (TP_BLOCK / 2);
         constexpr int PLANES = SPLIT ? 3 : 1;
+        // eight values as one plane's 16 bytes
+        auto pack = [&](const float (&g)[8], int q) -> uint4 {
+            uint32_t w[4];
 #pragma unroll
-        for (int q = 0; q < PLANES; ++q) {
-            auto plane_bits = [&](float g) -> uint16_t {
-                if constexpr (!SPLIT) return bf16_bits(g);
-                else {
-                    uint16_t b[3];
-                    split_bf16(g, b);
-                    return b[q];
+            for (int e = 0; e < 4; ++e) {
+                uint16_t b[2][3];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if constexpr (SPLIT) split_bf16(g[2 * e + k], b[k]);
+                    else b[k][0] = bf16_bits(g[2 * e + k]);
                 }
-            };
+                w[e] = b[0][q] | (uint32_t)b[1][q] << 16;
+            }
+            return make_uint4(w[0], w[1], w[2], w[3]);
+        };
+        float db[2] = {0.f, 0.f};
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            if (h) __syncthreads();
+            half.write(t, h, acc);
+            __syncthreads();
+            for (int e = hit0 + t.tid; e < hit1; e += TP_THREADS) {
+                const int2 x = hits[e];
+                const int tok = x.x >> 16;
+                if (tok >> 7 == h) atomicAdd(half.at(tok & 127, x.x >> 8 & 255), -s_gs[tok] * __int_as_float(x.y));
+            }
+            if (hit1 > hit0) __syncthreads();
             if (p.G) {
-                __syncthreads();
-                // token rows; 16-byte chunks (8 entries) XORed with the token, so that the 32 tokens of a store lie on different banks
+#pragma unroll 2
+                for (int k = 0; k < 8; ++k) {
+                    const int tok = t.wave * 16 + k * 2 + t.half;
+                    float g[8];
+                    *reinterpret_cast<float4*>(&g[0]) = *reinterpret_cast<const float4*>(half.at(tok, t.l32 * 8));
+                    *reinterpret_cast<float4*>(&g[4]) = *reinterpret_cast<const float4*>(half.at(tok, t.l32 * 8 + 4));
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int r = 0; r < 16; r += 4) {
-                            const int v = t.row(i, r), tok = t.col(c);
-                            const uint32_t lo = plane_bits(acc[i][c][r]) | (uint32_t)plane_bits(acc[i][c][r + 1]) << 16;
-                            const uint32_t hi = plane_bits(acc[i][c][r + 2]) | (uint32_t)plane_bits(acc[i][c][r + 3]) << 16;
-                            *reinterpret_cast<uint2*>(half_tile(tok) + (((v >> 3) ^ (tok & 31)) << 4) + (v & 4) * 2) = make_uint2(lo, hi);
-                        }
-                __syncthreads();
-#pragma unroll 4
-                for (int k = 0; k < 16; ++k) {
-                    const int tok = k * 16 + t.wave * 2 + t.half;
-                    const uint4 w = *reinterpret_cast<const uint4*>(half_tile(tok) + ((t.l32 ^ (tok & 31)) << 4));
-                    *reinterpret_cast<uint4*>(p.G + q * p.g_plane + (size_t)(i0 + tok) * p.g_pitch + vp + t.l32 * 8) = w;
+                    for (int q = 0; q < PLANES; ++q)
+                        *reinterpret_cast<uint4*>(g_out + q * p.g_plane + (t.l32 >> 3) * (TP_BLOCK / 2) + (h * 128 + tok) * 64 + (t.l32 & 7) * 8) = pack(g, q);
                 }
             }
-            if (p.Gt) {
-                __syncthreads();
-                // vocabulary rows; the half-waves, four rows apart, XORed onto different banks
+            if (p.Gt || p.db_part) {
+                // a lane has one entry of the vocabulary and 8 tokens at a time: 16 entries by 32 tokens per wave and step
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int vv = 0; vv < 2; ++vv) {
+                    const int v = t.wave * 32 + vv * 16 + (t.lane & 15);
+#pragma unroll 2
+                    for (int k = 0; k < 4; ++k) {
+                        const int tok = (k * 4 + (t.lane >> 4)) * 8;
+                        float g[8];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
+                        for (int j = 0; j < 8; ++j) g[j] = *half.at(tok + j, v);
+                        db[vv] += ((g[0] + g[1]) + (g[2] + g[3])) + ((g[4] + g[5]) + (g[6] + g[7]));
+                        if (p.Gt) {
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int v = t.row(i, r), tok = t.col(c);
-                            *reinterpret_cast<uint16_t*>(half_tile(v) + (((tok >> 3) ^ (v & 4)) << 4) + (tok & 7) * 2) = plane_bits(acc[i][c][r]);
+                            for (int q = 0; q < PLANES; ++q)
+                                *reinterpret_cast<uint4*>(gt_out + q * p.gt_plane + (h * 2 + (tok >> 6)) * (TP_BLOCK / 2) + v * 64 + (tok & 63)) = pack(g, q);
                         }
-                __syncthreads();
-#pragma unroll 4
-                for (int k = 0; k < 16; ++k) {
-                    const int v = k * 16 + t.wave * 2 + t.half;
-                    const uint4 w = *reinterpret_cast<const uint4*>(half_tile(v) + ((t.l32 ^ (v & 4)) << 4));
-                    *reinterpret_cast<uint4*>(p.Gt + q * p.gt_plane + (size_t)(vp + v) * p.gt_pitch + i0 + t.l32 * 8) = w;
+                    }
                 }
+            }
+        }
+        if (p.db_part) {
+#pragma unroll
+            for (int vv = 0; vv < 2; ++vv) {
+                db[vv] += __shfl_xor(db[vv], 16);
+                db[vv] += __shfl_xor(db[vv], 32);
+                if (t.lane < 16) p.db_part[(size_t)tt * p.db_pitch + v0 + t.wave * 32 + vv * 16 + t.lane] = db[vv];
             }
         }
     }
@@ -539,14 +520,19 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_loss_kernel(Teacher t, R
 struct GradsParams {
     RowList list;
     // dW [piece, D] = Gt Ht^T over the tokens
-    const void* Gt; const void* Ht; size_t gt_pitch, ht_pitch, gt_plane, ht_plane;     // bytes
+    const void *Gt, *Ht;       // by slab
+    size_t gt_plane, ht_plane; // bytes
+    int t_slabs;               // slabs of all tokens
     void* dW;                  // of the piece; null if not wanted
     int nv;                    // vocabulary entries of the piece
     // dH_part[split] [places, D] (+)= G Wt^T over the piece
-    const void* G; const void* Wt; size_t g_pitch, wt_pitch, g_plane, wt_plane;        // bytes
+    const void *G, *Wt;
+    size_t g_plane, wt_plane;
+    int v_slabs;               // slabs of a piece
     float* dh_part;            // null if not wanted
     size_t dh_plane;           // elements
     int splits, accumulate;
+    bool dh_first;             // which units are handed out first
     int D, nd;                 // hidden size, tiles of it
     int ga;
 };
@@ -572,7 +558,7 @@ __device__ __forceinline__ void store_tile(const TileLane& t, const floatx16 (&a
         }
 }
 
-// Both products of a piece of the vocabulary: units of dW first, then those of dH, whose contracted axis (the piece) is cut into
+// Both products of a piece of the vocabulary in one launch: units of dW, and units of dH, whose contracted axis (the piece) is cut into
 // `splits`, each with a plane of partial sums of its own.
 template <bool SPLIT, typename OT>
 __global__ __launch_bounds__(TP_THREADS, 2) void distill_grads_kernel(GradsParams p) {
@@ -584,31 +570,26 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_grads_kernel(GradsParam
     const int w_units = p.dW ? nvt * p.nd : 0;
     const int h_units = p.dh_part ? ntt * p.nd : 0;
     int u;
-    if (!xcd_unit(w_units + h_units * p.splits, u)) return;
+    const int hs_units = h_units * p.splits;
+    if (!xcd_unit(p.dh_first ? hs_units : w_units, p.dh_first ? w_units : hs_units, u)) return;
+    if (p.dh_first) u = u < hs_units ? u + w_units : u - hs_units;       // counted as dW's first either way
+
     const TileLane t;
     floatx16 acc[4][2];
     int at, bt;
-    SlabWalk walk;
     if (u < w_units) {
         tile_of_unit(u, nvt, p.nd, p.ga, at, bt);
-        walk.nkp = (n + 63) / 64;
-        walk.nk = SPLIT ? walk.nkp * TP_PAIRS : walk.nkp;
-        walk.a_plane = p.gt_plane;
-        walk.b_plane = p.ht_plane;
-        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, p.Gt, p.gt_pitch, at * TP_T, p.nv, p.Ht, p.ht_pitch, bt * TP_T, p.D, walk, acc);
+        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, block_operand(p.Gt, p.gt_plane, at, p.t_slabs, 0), block_operand(p.Ht, p.ht_plane, bt, p.t_slabs, 0),
+                                    (n + 63) / 64, acc);
         store_tile(t, acc, reinterpret_cast<OT*>(p.dW) + (size_t)at * TP_T * p.D + bt * TP_T, p.D, p.nv - at * TP_T, p.D - bt * TP_T, false);
     } else {
         u -= w_units;
         const int s = u / h_units;
         tile_of_unit(u - s * h_units, ntt, p.nd, p.ga, at, bt);
         const int slabs = (p.nv + 63) / 64;
-        const int k0 = (int)((long long)slabs * s / p.splits);
-        walk.nkp = (int)((long long)slabs * (s + 1) / p.splits) - k0;
-        walk.nk = SPLIT ? walk.nkp * TP_PAIRS : walk.nkp;
-        walk.a_plane = p.g_plane;
-        walk.b_plane = p.wt_plane;
-        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, reinterpret_cast<const char*>(p.G) + (size_t)k0 * TP_RB, p.g_pitch, at * TP_T, n,
-                                    reinterpret_cast<const char*>(p.Wt) + (size_t)k0 * TP_RB, p.wt_pitch, bt * TP_T, p.D, walk, acc);
+        const int k0 = (int)((long long)slabs * s / p.splits), k1 = (int)((long long)slabs * (s + 1) / p.splits);
+        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, block_operand(p.G, p.g_plane, at, p.v_slabs, k0), block_operand(p.Wt, p.wt_plane, bt, p.v_slabs, k0),
+                                    k1 - k0, acc);
         store_tile(t, acc, p.dh_part + s * p.dh_plane + (size_t)at * TP_T * p.D + bt * TP_T, p.D, n - at * TP_T, p.D - bt * TP_T, p.accumulate != 0);
     }
 }

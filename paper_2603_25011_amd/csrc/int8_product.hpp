@@ -47,10 +47,9 @@ __global__ __launch_bounds__(TP_THREADS, 2) void int8_tile_kernel(Int8Params p) 
         ws[c] = p.w_scale[v];
         bs[c] = p.bias ? p.bias[v] : 0.f;
     }
-    SlabWalk walk;
-    walk.nk = walk.nkp = p.row_bytes / TP_RB;
     intx16 acc[4][2];
-    tile_product<intx4, false>(s_ring0, s_ring1, p.A, (size_t)p.lda, n0, p.N, p.W, (size_t)p.ldw, v0, p.V, walk, acc);
+    tile_product<intx4, false>(s_ring0, s_ring1, row_operand(p.A, (size_t)p.lda, 0, n0, p.N), row_operand(p.W, (size_t)p.ldw, 0, v0, p.V),
+                               p.row_bytes / TP_RB, acc);
     __syncthreads();
     OT* const out = reinterpret_cast<OT*>(p.out);
 #pragma unroll

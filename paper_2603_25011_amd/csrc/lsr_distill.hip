@@ -108,6 +108,7 @@ struct DShape {
     int planes;         // bfloat16 planes of an operand
     int width;          // elements of a laid-out row: whole slabs
     int n_up;           // N up to whole tiles
+    int d_up;           // D up to whole tiles
     int n_vt, n_tt;
     float inv_t;
 };
@@ -121,6 +122,7 @@ int check_distill(const lsr_distill_desc* d, DShape* s) {
     s->planes = s->dtype == LSR_F32 ? 3 : 1;
     s->width = (int)up(d->D, 64);
     s->n_up = (int)up(d->N, TP_T);
+    s->d_up = (int)up(d->D, TP_T);
     s->n_vt = (s->V + TP_T - 1) / TP_T;
     s->n_tt = s->n_up / TP_T;
     s->inv_t = 1.f / d->temperature;
@@ -140,17 +142,33 @@ Pieces pieces(const DShape& s) {
     p.n = (s.n_vt + p.tiles - 1) / p.tiles;
     return p;
 }
-// Cuts of the piece as the contracted axis of dH: units of about an eighth of a CU's share of the piece's slabs, so that the last round of
-// workgroups is short; no unit below 16 slabs.
-int dh_splits(const DShape& s, const Pieces& p, int n_cus) {
-    const int64_t nd = (s.D + TP_T - 1) / TP_T;
-    const int64_t slabs = (int64_t)p.tiles * TP_T / 64;
-    const int64_t share = ((int64_t)p.tiles * nd * (s.n_up / 64) + (int64_t)s.n_tt * nd * slabs) / n_cus;
-    int64_t want = share / 8;
-    want = want < 16 ? 16 : want;
-    int64_t k = (slabs + want - 1) / want;
-    k = k < 1 ? 1 : k;
-    return (int)(k > 8 ? 8 : k);
+// The launch of a piece's two products: the units of dW (one per tile, the tokens as contracted axis) and of dH (the piece as contracted axis, cut
+// into `splits`, each with partial sums of its own).  The longer kind is handed out first.  The launch then ends about half a short unit behind the
+// average of its CUs, or when the CUs are through with the long ones; a unit costs its slabs and UNIT_COST slabs' time for its start and
+// its store.  The number of cuts is the one that this puts lowest.  (B=4096 D=1024, piece of 62720: 8 cuts behind dW 980 us, 25 cuts 1230, because partial sums
+// are read and written again for every piece.)
+struct GradsPlan { int splits; bool dh_first; };
+constexpr int GRADS_CUS = 256;       // CUs that it is made for: the size of the workspace does not depend on the device
+constexpr int MAX_SPLITS = 32;
+constexpr double UNIT_COST = 10;
+GradsPlan grads_plan(const DShape& s, const Pieces& p) {
+    const int nd = (s.D + TP_T - 1) / TP_T;
+    const double each = s.planes == 3 ? TP_PAIRS : 1;
+    const int slabs = p.tiles * (TP_T / 64);
+    const double w_units = (double)p.tiles * nd, w_len = (s.N + 63) / 64 * each + UNIT_COST;
+    GradsPlan best = {1, true};
+    double least = 0;
+    for (int k = 1; k <= MAX_SPLITS; ++k) {
+        if (k > 1 && (slabs / k < 8 || (int64_t)s.N * s.D * k > int64_t(1) << 28)) break;
+        const double h_units = (double)s.n_tt * nd * k, h_len = slabs * each / k + UNIT_COST;
+        const bool first = h_len >= w_len;
+        const double long_units = first ? h_units : w_units, long_len = first ? h_len : w_len, short_len = first ? w_len : h_len;
+        const double average = (w_units * w_len + h_units * h_len) / GRADS_CUS + 0.5 * short_len;
+        const double longs = ceil(long_units / GRADS_CUS) * long_len;
+        const double t = average > longs ? average : longs;
+        if (k == 1 || t < least) { least = t; best = {k, first}; }
+    }
+    return best;
 }
 
 struct DWs {
@@ -158,9 +176,8 @@ struct DWs {
     size_t part, picked;                                          // forward
     size_t Ht, Wt, G, Gt, db_part, dh_part;                       // backward
     size_t total;
-    int splits;
+    GradsPlan grads;
 };
-constexpr int DH_CUS = 256;      // CUs that the number of partial sums is chosen for (a size that must not depend on the device)
 DWs distill_ws(const DShape& s, bool backward) {
     DWs w = {};
     size_t at = 0;
@@ -180,13 +197,13 @@ DWs distill_ws(const DShape& s, bool backward) {
     } else {
         const Pieces p = pieces(s);
         const size_t pv = (size_t)p.tiles * TP_T;
-        w.splits = dh_splits(s, p, DH_CUS);
-        w.Ht = take((size_t)s.planes * s.D * s.n_up * 2);
-        w.Wt = take((size_t)s.planes * s.D * pv * 2);
+        w.grads = grads_plan(s, p);
+        w.Ht = take((size_t)s.planes * s.d_up * s.n_up * 2);
+        w.Wt = take((size_t)s.planes * s.d_up * pv * 2);
         w.G = take((size_t)s.planes * s.n_up * pv * 2);
         w.Gt = take((size_t)s.planes * s.n_up * pv * 2);
         w.db_part = take((size_t)s.n_tt * s.n_vt * TP_T * 4);
-        w.dh_part = take((size_t)w.splits * s.N * s.D * 4);
+        w.dh_part = take((size_t)w.grads.splits * s.N * s.D * 4);
     }
     w.total = at;
     return w;
@@ -233,9 +250,8 @@ LogitsParams logits_params(const DShape& s, const DWs& w, char* ws, const Begun&
     LogitsParams p = {};
     p.W = b.Wc; p.Hc = b.Hc;
     p.w_pitch = p.h_pitch = b.pitch;
-    p.walk.nkp = s.width / 64;
-    p.walk.nk = p.walk.nkp * (s.planes == 3 ? TP_PAIRS : 1);
-    p.walk.a_plane = b.w_plane; p.walk.b_plane = b.h_plane;
+    p.w_plane = b.w_plane; p.h_plane = b.h_plane;
+    p.slabs = s.width / 64;
     p.bias = bias;
     p.list = b.list;
     p.hits = reinterpret_cast<const int2*>(ws + w.hits);
@@ -271,29 +287,30 @@ int run_backward(const DShape& s, const void* H, const void* W, const float* bia
     uint16_t* const Wt = reinterpret_cast<uint16_t*>(ws + w.Wt);
     if (dW)
         distill_transpose_kernel<<<dim3(s.n_up / 64, (s.D + 63) / 64, PLANES), 256, 0, st>>>(
-            static_cast<const uint16_t*>(b.Hc), s.width, b.h_plane / 2, b.list, s.D, Ht, s.n_up, (size_t)s.D * s.n_up);
+            static_cast<const uint16_t*>(b.Hc), s.width, b.h_plane / 2, b.list, s.D, Ht, s.n_up / 64, (size_t)s.d_up * s.n_up);
     LogitsParams p = logits_params(s, w, ws, b, bias);
     p.lse = lse;
     p.dloss = dloss;
     p.mass = b.teacher.mass;
     p.G = dH ? reinterpret_cast<uint16_t*>(ws + w.G) : nullptr;
     p.Gt = dW ? reinterpret_cast<uint16_t*>(ws + w.Gt) : nullptr;
-    p.g_pitch = pv;
-    p.gt_pitch = s.n_up;
+    p.g_slabs = pv / 64;
+    p.gt_slabs = s.n_up / 64;
     p.g_plane = p.gt_plane = (size_t)s.n_up * pv;
     p.db_part = db ? reinterpret_cast<float*>(ws + w.db_part) : nullptr;
     p.db_pitch = s.n_vt * TP_T;
     GradsParams g = {};
     g.list = b.list;
     g.Gt = p.Gt; g.Ht = Ht;
-    g.gt_pitch = g.ht_pitch = (size_t)s.n_up * 2;
-    g.gt_plane = p.gt_plane * 2; g.ht_plane = (size_t)s.D * s.n_up * 2;
+    g.gt_plane = p.gt_plane * 2; g.ht_plane = (size_t)s.d_up * s.n_up * 2;
+    g.t_slabs = s.n_up / 64;
     g.G = p.G; g.Wt = Wt;
-    g.g_pitch = g.wt_pitch = (size_t)pv * 2;
-    g.g_plane = p.g_plane * 2; g.wt_plane = (size_t)s.D * pv * 2;
+    g.g_plane = p.g_plane * 2; g.wt_plane = (size_t)s.d_up * pv * 2;
+    g.v_slabs = pv / 64;
     g.dh_part = dH ? reinterpret_cast<float*>(ws + w.dh_part) : nullptr;
     g.dh_plane = (size_t)s.N * s.D;
-    g.splits = w.splits;
+    g.splits = w.grads.splits;
+    g.dh_first = w.grads.dh_first;
     g.D = s.D;
     g.nd = (s.D + TP_T - 1) / TP_T;
     g.ga = 8;
@@ -304,15 +321,15 @@ int run_backward(const DShape& s, const void* H, const void* W, const float* bia
         p.nvt = (nv + TP_T - 1) / TP_T;
         if (dH)
             distill_transpose_kernel<<<dim3((unsigned)up(nv, TP_T) / 64, (s.D + 63) / 64, PLANES), 256, 0, st>>>(
-                static_cast<const uint16_t*>(b.Wc) + (size_t)v0 * s.width, s.width, b.w_plane / 2, RowList{nullptr, nullptr, nv}, s.D, Wt, pv,
-                (size_t)s.D * pv);
+                static_cast<const uint16_t*>(b.Wc) + (size_t)v0 * s.width, s.width, b.w_plane / 2, RowList{nullptr, nullptr, nv}, s.D, Wt, pv / 64,
+                (size_t)s.d_up * pv);
         distill_logits_kernel<PLANES == 3, true><<<xcd_grid((long long)p.nvt * s.n_tt), TP_THREADS, 0, st>>>(p);
         if (dH || dW) {
             g.dW = dW ? static_cast<char*>(dW) + (size_t)v0 * s.D * sizeof(T) : nullptr;
             g.nv = nv;
             g.accumulate = k > 0;
-            const long long units = (dW ? (long long)p.nvt * g.nd : 0) + (dH ? (long long)s.n_tt * g.nd * g.splits : 0);
-            distill_grads_kernel<PLANES == 3, T><<<xcd_grid(units), TP_THREADS, 0, st>>>(g);
+            const unsigned grid = xcd_grid(dW ? (long long)p.nvt * g.nd : 0) + xcd_grid(dH ? (long long)s.n_tt * g.nd * g.splits : 0);
+            distill_grads_kernel<PLANES == 3, T><<<grid, TP_THREADS, 0, st>>>(g);
         }
     }
     if (dH)

@@ -25,19 +25,34 @@ constexpr int TP_SLAB = TP_T * TP_RB;             // bytes per stage and operand
 constexpr int TP_STAGE = 2 * TP_SLAB;
 constexpr int TP_PAIRS = 6;                       // plane products of a split operand
 
-// Slab i of a walk over the contracted axis: byte offsets into A and B.
-struct SlabWalk {
-    int nk;                                       // slabs in all
-    int nkp;                                      // slabs of one plane
-    size_t a_plane, b_plane;                      // bytes between planes
-    // the planes of pair i, from the smallest product to the largest: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
-    __device__ __forceinline__ void at(bool split, int kt, size_t& ka, size_t& kb) const {
-        if (!split) { ka = kb = (size_t)kt * TP_RB; return; }
-        const int pair = __builtin_amdgcn_readfirstlane(kt / nkp), k = __builtin_amdgcn_readfirstlane(kt - pair * nkp);
-        ka = ((0x001012u >> (4 * pair)) & 3u) * a_plane + (size_t)k * TP_RB;
-        kb = ((0x010210u >> (4 * pair)) & 3u) * b_plane + (size_t)k * TP_RB;
-    }
+// One operand of a tile: its first row, the bytes from row to row, the last row there is (tile rows behind it repeat it; they are never looked
+// at), the bytes from slab to slab and, for split operands, from plane to plane.  Rows as a caller has them lie whole behind each other (step 128).
+// Operands that only these kernels see are laid out by slab instead, 256 rows of 128 bytes behind each other (tile_block below): a slab
+// is then 32 KiB in one piece, whatever the length of the contracted axis.
+struct TileOperand {
+    const char* base;
+    size_t pitch;
+    int last;
+    size_t step, plane;
 };
+constexpr size_t TP_BLOCK = (size_t)TP_SLAB;      // bytes of a block of 256 rows by one slab
+// Rows of a caller's matrix from row0 on.
+__device__ __forceinline__ TileOperand row_operand(const void* p, size_t pitch, size_t plane, int row0, int rows) {
+    return TileOperand{reinterpret_cast<const char*>(p) + (size_t)row0 * pitch, pitch, rows - 1 - row0, TP_RB, plane};
+}
+// Tile `tile` of an operand laid out by slab, `slabs` of them per tile, from slab k0 on.
+__device__ __forceinline__ TileOperand block_operand(const void* p, size_t plane, int tile, int slabs, int k0) {
+    return TileOperand{reinterpret_cast<const char*>(p) + ((size_t)tile * slabs + k0) * TP_BLOCK, TP_RB, TP_T - 1, TP_BLOCK, plane};
+}
+
+// The walk over the contracted axis: the slabs of one plane, and for split operands (TP_PAIRS times as many slabs) the planes of pair i, from the smallest
+// product to the largest: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0).
+__device__ __forceinline__ void slab_at(bool split, int kt, int nkp, const TileOperand& A, const TileOperand& B, size_t& ka, size_t& kb) {
+    if (!split) { ka = kt * A.step; kb = kt * B.step; return; }
+    const int pair = __builtin_amdgcn_readfirstlane(kt / nkp), k = __builtin_amdgcn_readfirstlane(kt - pair * nkp);
+    ka = ((0x001012u >> (4 * pair)) & 3u) * A.plane + k * A.step;
+    kb = ((0x010210u >> (4 * pair)) & 3u) * B.plane + k * B.step;
+}
 
 template <typename Frag> struct TileAcc { typedef floatx16 type; };
 template <> struct TileAcc<intx4> { typedef intx16 type; };
@@ -60,16 +75,14 @@ __device__ __forceinline__ const char* uniform(const char* p) {
     return reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
 }
 
-// acc = rows [a_row0, a_row0 + 256) of A times rows [b_row0, ..) of B.  Rows at or behind a_rows / b_rows repeat the last one (they
-// are never looked at).  Pitches and planes in bytes, pitches below 2^23.  On return every wave is past its LDS reads
-// only after the caller's next barrier.
+// acc = A B^T over nkp slabs (per plane).  Pitches below 2^23.  On return every wave is past its LDS reads only after the caller's next barrier.
 template <typename Frag, bool SPLIT>
-__device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, const void* A, size_t a_pitch, int a_row0, int a_rows,
-                                             const void* B, size_t b_pitch, int b_row0, int b_rows, const SlabWalk& walk,
+__device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, const TileOperand& A, const TileOperand& B, int nkp,
                                              typename TileAcc<Frag>::type (&acc)[4][2]) {
     constexpr int KS = TP_RB / 32, LPT = 8, SPREAD = 2, CPR = TP_RB / 16, RPI = 64 / CPR, NW = 8;
     const TileLane t;
-    const int nk = __builtin_amdgcn_readfirstlane(walk.nk);
+    nkp = __builtin_amdgcn_readfirstlane(nkp);
+    const int nk = SPLIT ? nkp * TP_PAIRS : nkp;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -81,14 +94,14 @@ __device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, con
     // access j of wave w covers tile rows (8 j + w) 8 .. + 8; lane -> (row, LDS chunk lp), which holds global chunk lp ^ swizzle
     const int lrow = t.wave * RPI + t.lane / CPR;
     const uint32_t gch = (uint32_t)((t.lane % CPR) ^ lds_swz<TP_RB>(lrow));
-    const char* const Ab = uniform(reinterpret_cast<const char*>(A) + (size_t)a_row0 * a_pitch);
-    const char* const Bb = uniform(reinterpret_cast<const char*>(B) + (size_t)b_row0 * b_pitch);
+    const char* const Ab = uniform(A.base);
+    const char* const Bb = uniform(B.base);
     uint32_t ao[4], bo[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int r = lrow + NW * RPI * j;
-        ao[j] = (uint32_t)min(r, a_rows - 1 - a_row0) * (uint32_t)a_pitch + gch * 16;
-        bo[j] = (uint32_t)min(r, b_rows - 1 - b_row0) * (uint32_t)b_pitch + gch * 16;
+        ao[j] = (uint32_t)min(r, A.last) * (uint32_t)A.pitch + gch * 16;
+        bo[j] = (uint32_t)min(r, B.last) * (uint32_t)B.pitch + gch * 16;
     }
     const uint32_t wave_lds = __builtin_amdgcn_readfirstlane(t.wave * 1024);
     const int fa_row = t.wm * 32 + t.l32, fb_row = t.wn * 64 + t.l32;
@@ -103,7 +116,7 @@ __device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, con
     };
     {
         size_t ka, kb;
-        walk.at(SPLIT, 0, ka, kb);
+        slab_at(SPLIT, 0, nkp, A, B, ka, kb);
 #pragma unroll
         for (int n = 0; n < LPT; ++n) issue_one(ring0, Ab + ka, Bb + kb, n);
     }
@@ -115,7 +128,7 @@ __device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, con
         __syncthreads();
         const int more = __builtin_amdgcn_readfirstlane(kt + 1 < nk ? 1 : 0);
         size_t ka, kb;
-        walk.at(SPLIT, kt + 1, ka, kb);
+        slab_at(SPLIT, kt + 1, nkp, A, B, ka, kb);
         const char* ab = Ab + ka;
         const char* bb = Bb + kb;
         auto dma = [&](int n) {
@@ -140,6 +153,15 @@ __device__ __forceinline__ bool xcd_unit(int n_units, int& u) {
     const int x = blockIdx.x & 7;
     u = (int)((long long)n_units * x / 8) + (int)(blockIdx.x >> 3);
     return u < (int)((long long)n_units * (x + 1) / 8);
+}
+// The same for a launch of two jobs (a grid of xcd_grid of either): every XCD takes an eighth of either, those of the first job first.  Units of the
+// second are counted from n_first on.
+__device__ __forceinline__ bool xcd_unit(int n_first, int n_second, int& u) {
+    const int x = blockIdx.x & 7, j = blockIdx.x >> 3;
+    const int lo = (int)((long long)n_first * x / 8), len = (int)((long long)n_first * (x + 1) / 8) - lo;
+    if (j < len) { u = lo + j; return true; }
+    u = n_first + (int)((long long)n_second * x / 8) + j - len;
+    return u < n_first + (int)((long long)n_second * (x + 1) / 8);
 }
 inline unsigned xcd_grid(long long n_units) { return (unsigned)((n_units + 7) / 8 * 8); }
 
