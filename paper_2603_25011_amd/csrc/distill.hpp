@@ -5,7 +5,7 @@
 //   g_nv   = dloss_n / T (mass_n exp(z_nv - lse_n) - sum_{j: id = v} p_nj),   dH = g W,  dW = g^T H,  db_v = sum_n g_nv
 //
 // Passes.  Rows that the mask leaves out are dropped first (distill_compact_kernel), the others laid out densely with whole
-// slabs (distill_rows_kernel; three planes each for float32).  The teacher's entries are bucketed by logit tile (distill_hits_kernel),
+// slabs (distill_rows_kernel; three planes each for float32).  The teacher's entries are bucketed by logit tile (distill_teacher_kernel),
 // so that the workgroup which holds a tile in registers also finds the entries that fall into it: the forward picks their logits
 // there, the backward subtracts their probabilities there, before anything is rounded.
 //   forward   distill_logits_kernel<false>: per tile and token one (maximum, sum of exp); distill_loss_kernel joins them
@@ -78,76 +78,39 @@ struct Teacher {
     __device__ __forceinline__ bool valid(int id, float t) const { return (unsigned)id < (unsigned)V && t != -INFINITY; }
 };
 
-// One wave per valid row: the row's hidden states into whole slabs (PLANES planes of `width` elements, zeros behind D; dst null:
-// they are used where they are), and the teacher's L and mass (ids null: a matrix without a teacher).
+// One wave per row of the list: PLANES planes of `width` elements, zeros behind D.
 template <typename T, int PLANES>
 __global__ __launch_bounds__(256) void distill_rows_kernel(const T* __restrict__ X, int D, RowList list, uint16_t* __restrict__ dst,
-                                                           int width, size_t plane, Teacher t) {
+                                                           int width, size_t plane) {
     const int lane = threadIdx.x & 63;
     const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (i >= list.n()) return;
     const int64_t r = list.row(i);
-    if (dst) {
-        for (int d = lane * 8; d < width; d += 512) {
-            uint16_t o[PLANES][8];
+    for (int d = lane * 8; d < width; d += 512) {
+        uint16_t o[PLANES][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 8; ++e)
 #pragma unroll
-                for (int q = 0; q < PLANES; ++q) o[q][e] = 0;
-            if (d < D) {                         // (D is a multiple of 8)
-                if constexpr (PLANES == 1) {
-                    *reinterpret_cast<uint4*>(&o[0][0]) = *reinterpret_cast<const uint4*>(X + r * D + d);
-                } else {
-                    float f[8];
-                    *reinterpret_cast<float4*>(&f[0]) = *reinterpret_cast<const float4*>(X + r * D + d);
-                    *reinterpret_cast<float4*>(&f[4]) = *reinterpret_cast<const float4*>(X + r * D + d + 4);
+            for (int q = 0; q < PLANES; ++q) o[q][e] = 0;
+        if (d < D) {                             // (D is a multiple of 8)
+            if constexpr (PLANES == 1) {
+                *reinterpret_cast<uint4*>(&o[0][0]) = *reinterpret_cast<const uint4*>(X + r * D + d);
+            } else {
+                float f[8];
+                *reinterpret_cast<float4*>(&f[0]) = *reinterpret_cast<const float4*>(X + r * D + d);
+                *reinterpret_cast<float4*>(&f[4]) = *reinterpret_cast<const float4*>(X + r * D + d + 4);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        uint16_t p[3];
-                        split_bf16(f[e], p);
+                for (int e = 0; e < 8; ++e) {
+                    uint16_t p[3];
+                    split_bf16(f[e], p);
 #pragma unroll
-                        for (int q = 0; q < PLANES; ++q) o[q][e] = p[q];
-                    }
+                    for (int q = 0; q < PLANES; ++q) o[q][e] = p[q];
                 }
             }
-#pragma unroll
-            for (int q = 0; q < PLANES; ++q)
-                *reinterpret_cast<uint4*>(dst + q * plane + (size_t)i * width + d) = *reinterpret_cast<const uint4*>(&o[q][0]);
-        }
-    }
-    if (t.ids) {
-        float x[TOP_MAX_K / 64];
-        float m = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < TOP_MAX_K / 64; ++k) {
-            const int j = k * 64 + lane;
-            x[k] = -INFINITY;
-            if (j < t.K) {
-                const float tl = t.logits[r * t.K + j];
-                if (t.valid(t.ids[r * t.K + j], tl)) x[k] = tl;
-            }
-            m = fmaxf(m, x[k]);
         }
 #pragma unroll
-        for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-        float L = 0.f;
-        if (t.given_lse) {
-            L = t.given_lse[r];
-        } else {
-            const float z = finite_or_zero(m);
-            float s = 0.f;
-#pragma unroll
-            for (int k = 0; k < TOP_MAX_K / 64; ++k) s += __builtin_amdgcn_exp2f((x[k] - z) * (t.inv_t * LOG2E));
-#pragma unroll
-            for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-            L = s == 0.f ? 0.f : fmaf(z, t.inv_t, logf(s));
-        }
-        float mass = 0.f;
-#pragma unroll
-        for (int k = 0; k < TOP_MAX_K / 64; ++k) mass += x[k] == -INFINITY ? 0.f : teacher_p(x[k], t.inv_t, L);
-#pragma unroll
-        for (int o = 32; o; o >>= 1) mass += __shfl_xor(mass, o);
-        if (lane == 0) { t.L[i] = L; t.mass[i] = mass; }
+        for (int q = 0; q < PLANES; ++q)
+            *reinterpret_cast<uint4*>(dst + q * plane + (size_t)i * width + d) = *reinterpret_cast<const uint4*>(&o[q][0]);
     }
 }
 
@@ -181,50 +144,92 @@ __global__ __launch_bounds__(256) void distill_transpose_kernel(const uint16_t* 
 
 // ---- the teacher's entries by logit tile ----
 
-// hits[tt 256 K + first[tt][vt] .. first[tt][vt + 1]) = the entries of token tile tt that fall into vocabulary tile vt: .x = place in the
-// token tile << 16 | place in the vocabulary tile << 8 | j, .y = p.  Entries with p = 0 are left out.  One workgroup per token tile: a count,
-// a prefix sum, a placement (the order within a bucket is free: every entry has its own result).
-constexpr int HITS_THREADS = 1024;
-__global__ __launch_bounds__(HITS_THREADS) void distill_hits_kernel(Teacher t, RowList list, int n_vt, int2* __restrict__ hits,
-                                                                    int* __restrict__ first) {
+// Per valid row, the teacher's L and mass; and its entries in buckets, one for each group of 64 rows (a wave column of a logit tile) and vocabulary tile:
+//   hits[64 K grp + first[grp][vt] .. 64 K grp + first[grp][vt + 1]): .x = place in the token tile << 16 | place in the vocabulary tile << 8 | j, .y = p
+// Entries with p = 0 are left out.  One workgroup per group, four rows per wave, a row's entries across the lanes and kept in registers from the
+// statistics to the placement: a count in LDS, a prefix sum, the placement (the order within a bucket is free: every entry has its own result).
+constexpr int GROUP = 64;
+constexpr int TEACHER_THREADS = 1024;
+template <int PER>                               // entries per lane and row: K <= 64 PER
+__global__ __launch_bounds__(TEACHER_THREADS) void distill_teacher_kernel(Teacher t, RowList list, int n_vt, int2* __restrict__ hits,
+                                                                          int* __restrict__ first) {
     extern __shared__ int s_cnt[];               // [n_vt]
-    __shared__ int s_wave[HITS_THREADS / 64];
+    __shared__ int s_wave[TEACHER_THREADS / 64];
+    constexpr int ROWS = GROUP / (TEACHER_THREADS / 64);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = list.n();
-    const int i0 = blockIdx.x * TP_T;
+    const int i0 = blockIdx.x * GROUP;
     if (i0 >= n) return;
-    const int live = min(TP_T, n - i0) * t.K;
-    for (int v = tid; v < n_vt; v += HITS_THREADS) s_cnt[v] = 0;
+    for (int v = tid; v < n_vt; v += TEACHER_THREADS) s_cnt[v] = 0;
+    float x[ROWS][PER], given[ROWS];
+    int id[ROWS][PER];
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) {
+        const int i = i0 + wave * ROWS + q;
+        given[q] = 0.f;
+        const int64_t r = i < n ? list.row(i) : 0;
+        if (i < n && t.given_lse) given[q] = t.given_lse[r];
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int j = k * 64 + lane;
+            x[q][k] = -INFINITY;
+            id[q][k] = -1;
+            if (i < n && j < t.K) {
+                id[q][k] = t.ids[r * t.K + j];
+                x[q][k] = t.logits[r * t.K + j];
+            }
+        }
+    }
     __syncthreads();
-    auto entry = [&](int e, int& id, int& tok, int& j) -> float {
-        tok = e / t.K;
-        j = e - tok * t.K;
-        const int64_t at = (int64_t)list.row(i0 + tok) * t.K + j;
-        id = t.ids[at];
-        const float tl = t.logits[at];
-        return t.valid(id, tl) ? teacher_p(tl, t.inv_t, t.L[i0 + tok]) : 0.f;
-    };
-    for (int e = tid; e < live; e += HITS_THREADS) {
-        int id, tok, j;
-        if (entry(e, id, tok, j) != 0.f) atomicAdd(&s_cnt[id >> 8], 1);
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) {
+        const int i = i0 + wave * ROWS + q;
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (!t.valid(id[q][k], x[q][k])) x[q][k] = -INFINITY;
+            m = fmaxf(m, x[q][k]);
+        }
+        float L = given[q];
+        if (!t.given_lse) {
+#pragma unroll
+            for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+            const float z = finite_or_zero(m);
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) s += __builtin_amdgcn_exp2f((x[q][k] - z) * (t.inv_t * LOG2E));
+#pragma unroll
+            for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+            L = s == 0.f ? 0.f : fmaf(z, t.inv_t, logf(s));
+        }
+        float mass = 0.f;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            x[q][k] = x[q][k] == -INFINITY ? 0.f : teacher_p(x[q][k], t.inv_t, L);       // from here on p
+            mass += x[q][k];
+            if (x[q][k] != 0.f) atomicAdd(&s_cnt[id[q][k] >> 8], 1);
+        }
+#pragma unroll
+        for (int o = 32; o; o >>= 1) mass += __shfl_xor(mass, o);
+        if (lane == 0 && i < n) { t.L[i] = L; t.mass[i] = mass; }
     }
     __syncthreads();
     int base = 0;
     int* const out = first + (size_t)blockIdx.x * (n_vt + 1);
-    for (int v0 = 0; v0 < n_vt; v0 += HITS_THREADS) {
+    for (int v0 = 0; v0 < n_vt; v0 += TEACHER_THREADS) {
         const int v = v0 + tid;
         const int c = v < n_vt ? s_cnt[v] : 0;
-        int x = c;
+        int s = c;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(x, o);
-            if (lane >= o) x += y;
+            const int y = __shfl_up(s, o);
+            if (lane >= o) s += y;
         }
-        if (lane == 63) s_wave[wave] = x;
+        if (lane == 63) s_wave[wave] = s;
         __syncthreads();
-        int at = base + x - c, all = 0;
+        int at = base + s - c, all = 0;
 #pragma unroll
-        for (int w = 0; w < HITS_THREADS / 64; ++w) {
+        for (int w = 0; w < TEACHER_THREADS / 64; ++w) {
             at += w < wave ? s_wave[w] : 0;
             all += s_wave[w];
         }
@@ -234,11 +239,13 @@ __global__ __launch_bounds__(HITS_THREADS) void distill_hits_kernel(Teacher t, R
     }
     if (tid == 0) out[n_vt] = base;
     int2* const list_out = hits + (size_t)i0 * t.K;
-    for (int e = tid; e < live; e += HITS_THREADS) {
-        int id, tok, j;
-        const float p = entry(e, id, tok, j);
-        if (p != 0.f) list_out[atomicAdd(&s_cnt[id >> 8], 1)] = make_int2(tok << 16 | (id & 255) << 8 | j, __float_as_int(p));
-    }
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q)
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (x[q][k] != 0.f)
+                list_out[atomicAdd(&s_cnt[id[q][k] >> 8], 1)] =
+                    make_int2(((i0 & (TP_T - 1)) + wave * ROWS + q) << 16 | (id[q][k] & 255) << 8 | (k * 64 + lane), __float_as_int(x[q][k]));
 }
 
 // ---- logits ----
@@ -328,22 +335,33 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsPar
             }
         }
 
-    // the teacher's entries in this tile
-    const int* const first = p.first + (size_t)tt * (p.n_vt + 1) + vt;
-    const int hit0 = first[0], hit1 = first[1];
-    const int2* const hits = p.hits + (size_t)i0 * p.K;
+    // the teacher's entries in this tile: a bucket for each group of 64 tokens, two of them in each half of the tile
+    bool any = false;
+#pragma unroll
+    for (int g = 0; g < TP_T / GROUP; ++g)
+        if (i0 + g * GROUP < n) {
+            const int* const first = p.first + (size_t)(tt * (TP_T / GROUP) + g) * (p.n_vt + 1) + vt;
+            any |= first[1] > first[0];
+        }
+    auto for_hits = [&](int h, auto f) {
+        const int g = h * 2 + (t.tid >> 8);
+        if (i0 + g * GROUP >= n) return;
+        const int* const first = p.first + (size_t)(tt * (TP_T / GROUP) + g) * (p.n_vt + 1) + vt;
+        const int2* const hits = p.hits + (size_t)(i0 + g * GROUP) * p.K;
+        for (int e = first[0] + (t.tid & 255); e < first[1]; e += 256) {
+            const int2 x = hits[e];
+            f(x.x >> 16, x.x >> 8 & 255, x.x & 255, __int_as_float(x.y));
+        }
+    };
     const HalfTile half = {s_ring0, s_ring1};
     if constexpr (!BWD) {
-        if (hit1 > hit0) {
+        if (any) {
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
                 if (h) __syncthreads();
                 half.write(t, h, acc);
                 __syncthreads();
-                for (int e = hit0 + t.tid; e < hit1; e += TP_THREADS) {
-                    const int x = hits[e].x, tok = x >> 16;
-                    if (tok >> 7 == h) p.picked[(size_t)(i0 + tok) * p.K + (x & 255)] = *half.at(tok & 127, x >> 8 & 255);
-                }
+                for_hits(h, [&](int tok, int v, int j, float) { p.picked[(size_t)(i0 + tok) * p.K + j] = *half.at(tok & 127, v); });
             }
         }
         const float cc = p.inv_t * LOG2E;
@@ -414,12 +432,10 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsPar
             if (h) __syncthreads();
             half.write(t, h, acc);
             __syncthreads();
-            for (int e = hit0 + t.tid; e < hit1; e += TP_THREADS) {
-                const int2 x = hits[e];
-                const int tok = x.x >> 16;
-                if (tok >> 7 == h) atomicAdd(half.at(tok & 127, x.x >> 8 & 255), -s_gs[tok] * __int_as_float(x.y));
+            if (any) {
+                for_hits(h, [&](int tok, int v, int, float prob) { atomicAdd(half.at(tok & 127, v), -s_gs[tok] * prob); });
+                __syncthreads();
             }
-            if (hit1 > hit0) __syncthreads();
             if (p.G) {
 #pragma unroll 2
                 for (int k = 0; k < 8; ++k) {
@@ -466,9 +482,9 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsPar
 
 // ---- loss ----
 
-// One group of 16 threads per token: the tiles' statistics joined, then the teacher's entries.
+// LOSS_GROUPS threads per token: the tiles' statistics joined, then the teacher's entries.
 constexpr int LOSS_THREADS = 1024;
-constexpr int LOSS_TOKENS = 64;
+constexpr int LOSS_TOKENS = 16;
 constexpr int LOSS_GROUPS = LOSS_THREADS / LOSS_TOKENS;
 __global__ __launch_bounds__(LOSS_THREADS) void distill_loss_kernel(Teacher t, RowList list, const float2* __restrict__ part, int n_vt, int places,
                                                                     const float* __restrict__ picked, float* __restrict__ loss,
@@ -482,15 +498,23 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_loss_kernel(Teacher t, R
     const float cc = t.inv_t * LOG2E;
     ExpSum e = {-INFINITY, 0.f};
     if (i < n)
-        for (int v = grp; v < n_vt; v += LOSS_GROUPS) {
-            const float2 x = part[(size_t)v * places + i];
-            e = join(e, ExpSum{x.x, x.y}, cc);
+        for (int v = grp; v < n_vt; v += 4 * LOSS_GROUPS) {
+            float2 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[k] = make_float2(-INFINITY, 0.f);
+                if (v + k * LOSS_GROUPS < n_vt) x[k] = part[(size_t)(v + k * LOSS_GROUPS) * places + i];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) e = join(e, ExpSum{x[k].x, x[k].y}, cc);
         }
     s_part[grp][tok] = make_float2(e.m, e.s);
     __syncthreads();
     e = {-INFINITY, 0.f};
-#pragma unroll
-    for (int g = 0; g < LOSS_GROUPS; ++g) e = join(e, ExpSum{s_part[g][tok].x, s_part[g][tok].y}, cc);
+#pragma unroll 8
+    for (int g = 0; g < LOSS_GROUPS; ++g) e.m = fmaxf(e.m, s_part[g][tok].x);
+#pragma unroll 8
+    for (int g = 0; g < LOSS_GROUPS; ++g) e.s += s_part[g][tok].y * __builtin_amdgcn_exp2f((s_part[g][tok].x - finite_or_zero(e.m)) * cc);
     const float lse = e.m == -INFINITY ? e.m : fmaf(e.m, t.inv_t, logf(e.s));
     float sum = 0.f;
     if (i < n) {
@@ -507,7 +531,7 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_loss_kernel(Teacher t, R
     __syncthreads();
     if (grp == 0 && i < n) {
         float all = 0.f;
-#pragma unroll
+#pragma unroll 8
         for (int g = 0; g < LOSS_GROUPS; ++g) all += s_sum[g][tok];
         const int64_t r = list.row(i);
         loss[r] = all;
@@ -537,25 +561,32 @@ struct GradsParams {
     int ga;
 };
 
+// (what is added to is read 16 values at a time: a load behind each store would wait for it)
 template <typename OT>
 __device__ __forceinline__ void store_tile(const TileLane& t, const floatx16 (&acc)[4][2], OT* out, size_t pitch, int rows, int cols, bool add) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int c = 0; c < 2; ++c) {
+        const int col = t.col(c);
+        if (col < cols) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = t.row(i, r);
-            if (row < rows) {
+            for (int i = 0; i < 4; ++i) {
+                OT* o[16];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int col = t.col(c);
-                    if (col < cols) {
-                        OT* const o = out + (size_t)row * pitch + col;
-                        if constexpr (sizeof(OT) == 4) *o = add ? *o + acc[i][c][r] : acc[i][c][r];
-                        else *o = bf16_bits(acc[i][c][r]);
-                    }
+                for (int r = 0; r < 16; ++r) o[r] = out + (size_t)min(t.row(i, r), rows - 1) * pitch + col;
+                float x[16];
+                if (sizeof(OT) == 4 && add) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[r] = acc[i][c][r] + *reinterpret_cast<const float*>(o[r]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[r] = acc[i][c][r];
                 }
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (t.row(i, r) < rows) *o[r] = as_type<OT>(x[r]);
             }
         }
+    }
 }
 
 // Both products of a piece of the vocabulary in one launch: units of dW, and units of dH, whose contracted axis (the piece) is cut into

@@ -21,12 +21,6 @@ struct Int8Params {
     int na, nb, ga;            // tiles of rows and of vocabulary entries, row tiles per group
 };
 
-template <typename OT>
-__device__ __forceinline__ OT logit_as(float x) {
-    if constexpr (sizeof(OT) == 4) return x;
-    else return bf16_bits(x);
-}
-
 // Many rows: one 256 x 256 tile per workgroup, tokens as tile rows, vocabulary entries as columns (lanes hold
 // neighbouring columns, so a store is whole 32-column pieces of a row).
 template <typename OT>
@@ -62,7 +56,7 @@ __global__ __launch_bounds__(TP_THREADS, 2) void int8_tile_kernel(Int8Params p) 
                 const float a = s_scale[row];
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
-                    if (v0 + t.col(c) < p.V) o[t.col(c)] = logit_as<OT>(fmaf((float)acc[i][c][r], a * ws[c], bs[c]));
+                    if (v0 + t.col(c) < p.V) o[t.col(c)] = as_type<OT>(fmaf((float)acc[i][c][r], a * ws[c], bs[c]));
             }
         }
     }
@@ -179,7 +173,7 @@ __global__ __launch_bounds__(FEW8_THREADS) void int8_few_kernel(Int8Params p, in
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int n = acc_row(i, r, half);
-                        if (n < p.N) out[(int64_t)n * p.ldo + v_here] = logit_as<OT>(fmaf((float)acc[i][r], s_scale[n] * ws, bs));
+                        if (n < p.N) out[(int64_t)n * p.ldo + v_here] = as_type<OT>(fmaf((float)acc[i][r], s_scale[n] * ws, bs));
                     }
             }
         }

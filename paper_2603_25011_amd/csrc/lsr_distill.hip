@@ -188,7 +188,7 @@ DWs distill_ws(const DShape& s, bool backward) {
     w.L = take((size_t)s.N * 4);
     w.mass = take((size_t)s.N * 4);
     w.hits = take((size_t)s.n_up * s.K * 8);
-    w.first = take((size_t)s.n_tt * (s.n_vt + 1) * 4);
+    w.first = take((size_t)s.n_tt * (TP_T / GROUP) * (s.n_vt + 1) * 4);
     w.Hc = take((size_t)s.planes * s.N * s.width * 2);
     w.Wc = in_place(s) ? 0 : take((size_t)s.planes * s.V * s.width * 2);
     if (!backward) {
@@ -234,15 +234,17 @@ Begun begin(const DShape& s, const DWs& w, char* ws, const void* H, const void* 
     b.pitch = (size_t)s.width * 2;
     b.h_plane = (size_t)s.N * s.width * 2;
     b.w_plane = (size_t)s.V * s.width * 2;
-    distill_rows_kernel<T, PLANES><<<(s.N + 3) / 4, 256, 0, st>>>(static_cast<const T*>(H), s.D, b.list,
-        h_here ? nullptr : reinterpret_cast<uint16_t*>(ws + w.Hc), s.width, b.h_plane / 2, b.teacher);
-    if (!in_place(s)) {
-        Teacher none = {};
+    if (!h_here)
+        distill_rows_kernel<T, PLANES><<<(s.N + 3) / 4, 256, 0, st>>>(static_cast<const T*>(H), s.D, b.list, reinterpret_cast<uint16_t*>(ws + w.Hc),
+                                                                      s.width, b.h_plane / 2);
+    if (!in_place(s))
         distill_rows_kernel<T, PLANES><<<(s.V + 3) / 4, 256, 0, st>>>(static_cast<const T*>(W), s.D, RowList{nullptr, nullptr, s.V},
-            reinterpret_cast<uint16_t*>(ws + w.Wc), s.width, b.w_plane / 2, none);
-    }
-    distill_hits_kernel<<<s.n_tt, HITS_THREADS, (size_t)s.n_vt * 4, st>>>(b.teacher, b.list, s.n_vt, reinterpret_cast<int2*>(ws + w.hits),
-                                                                          reinterpret_cast<int*>(ws + w.first));
+                                                                      reinterpret_cast<uint16_t*>(ws + w.Wc), s.width, b.w_plane / 2);
+    int2* const hits = reinterpret_cast<int2*>(ws + w.hits);
+    int* const first = reinterpret_cast<int*>(ws + w.first);
+    const unsigned groups = (unsigned)((s.N + GROUP - 1) / GROUP);
+    if (s.K <= 64) distill_teacher_kernel<1><<<groups, TEACHER_THREADS, (size_t)s.n_vt * 4, st>>>(b.teacher, b.list, s.n_vt, hits, first);
+    else distill_teacher_kernel<TOP_MAX_K / 64><<<groups, TEACHER_THREADS, (size_t)s.n_vt * 4, st>>>(b.teacher, b.list, s.n_vt, hits, first);
     return b;
 }
 

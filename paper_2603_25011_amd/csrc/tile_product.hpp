@@ -178,6 +178,11 @@ __device__ __forceinline__ uint16_t bf16_bits(float x) {
     const __bf16 b = (__bf16)x;                   // to nearest, ties to even
     return __builtin_bit_cast(uint16_t, b);
 }
+template <typename OT>
+__device__ __forceinline__ OT as_type(float x) {
+    if constexpr (sizeof(OT) == 4) return x;
+    else return bf16_bits(x);
+}
 // x as the sum of three bfloat16: the first two cut off (exact), the rest rounded.
 __device__ __forceinline__ void split_bf16(float x, uint16_t (&p)[3]) {
     const uint32_t b0 = __float_as_uint(x) & 0xffff0000u;

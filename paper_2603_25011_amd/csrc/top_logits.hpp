@@ -8,8 +8,8 @@ namespace lsr {
 // A workgroup takes a segment of a row (the whole row, where there are enough rows to fill the chip) in batches of TOP_BATCH
 // logits held in registers.  Every logit has a 64-bit key, its value as an ordered integer above its index complemented: larger
 // key = earlier in the result, and no two are equal.  The workgroup keeps the keys that beat a threshold in an LDS list.  The first
-// threshold is the K-th largest of the threads' maxima over the first batch: at least K logits are no smaller, and only
-// about K (1 + ln(V / TOP_BATCH)) of a row pass it.  When the list is full it is cut to its K largest, whose last is the next threshold.
+// threshold comes from the threads' maxima over the first batch: the smallest over the waves of the K/4-th largest of a wave's 64, so at least K
+// logits are no smaller, and few more are.  When the list has grown it is cut to its K largest, whose last is the next threshold.
 // A key's place is the number of larger keys (counted, the list is short; no sort).  The maximum and sum of exp of the row
 // run along in registers.  Segments of one row are joined by a second launch.
 // Bound by reading the logits once.
@@ -17,6 +17,7 @@ constexpr int TOP_THREADS = 256;
 constexpr int TOP_PER = 32;                            // logits per thread and batch
 constexpr int TOP_BATCH = TOP_THREADS * TOP_PER;
 constexpr int TOP_CAP = 1024;                          // keys in the list
+constexpr int TOP_WAVES = TOP_THREADS / 64;
 constexpr int TOP_MAX_K = 256;                         // (no more than threads: the first threshold)
 constexpr int TOP_MERGE_KEYS = 2048;                   // keys that the segments of one row hand over
 constexpr float LOG2E = 1.44269504088896340736f;
@@ -51,20 +52,27 @@ __device__ __forceinline__ float log_normaliser(ExpSum e, float inv_t, bool nan)
 }
 
 struct TopShared {
-    uint64_t list[TOP_MERGE_KEYS];
+    __attribute__((aligned(16))) uint64_t list[TOP_MERGE_KEYS];
     uint64_t best[TOP_MAX_K];
-    uint32_t most[TOP_THREADS];
-    ExpSum part[TOP_THREADS / 64];
-    uint64_t threshold;
+    uint32_t most[TOP_WAVES];
+    ExpSum part[TOP_WAVES];
     int count;
 };
 
-// best[0 .. min(K, n)) = the largest of list[0 .. n), in order.  Whole workgroup; barriers inside.
+// best[0 .. min(K, n)) = the largest of list[0 .. n), in order.  Whole workgroup; the list is complete (a barrier behind its last write); a barrier at the end.
 __device__ __forceinline__ void top_rank(TopShared& sh, int n, int K) {
     for (int i = threadIdx.x; i < n; i += TOP_THREADS) {
         const uint64_t k = sh.list[i];
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += sh.list[j] > k ? 1 : 0;
+        int j = 0;
+        for (; j + 8 <= n; j += 8) {             // 16-byte reads, the same address in every lane
+            ulonglong2 q[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[e] = *reinterpret_cast<const ulonglong2*>(&sh.list[j + 2 * e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rank += (q[e].x > k ? 1 : 0) + (q[e].y > k ? 1 : 0);
+        }
+        for (; j < n; ++j) rank += sh.list[j] > k ? 1 : 0;
         if (rank < K) sh.best[rank] = k;
     }
     __syncthreads();
@@ -106,11 +114,11 @@ __device__ __forceinline__ void top_store(const TopParams& p, int64_t row, const
 }
 
 template <typename T>
-__global__ __launch_bounds__(TOP_THREADS) void top_logits_kernel(TopParams p) {
+__global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p) {
     __shared__ TopShared sh;
     constexpr int EPV = 16 / sizeof(T);          // logits per 16-byte load
     constexpr int U = TOP_PER / EPV;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x / p.splits;
     const int split = (int)(blockIdx.x - row * p.splits);
     const int first = split * p.seg;
@@ -119,106 +127,140 @@ __global__ __launch_bounds__(TOP_THREADS) void top_logits_kernel(TopParams p) {
     const float c = p.inv_t * LOG2E;
     const int K = p.K;
 
-    // logits in front of the first 16-byte boundary and behind the last whole 16 bytes are loaded one by one, by the threads of the
-    // first batch in place of a vector of their own
+    // logits in front of the first 16-byte boundary and behind the last whole 16 bytes: one for each of the first threads
     const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(T));
     const int nvec = (n - head) / EPV;
     const int tail = n - head - nvec * EPV;
-    auto as_float = [](T b) -> float {
-        if constexpr (sizeof(T) == 4) return b;
-        else return __uint_as_float((uint32_t)b << 16);
-    };
-    ExpSum run = {-INFINITY, 0.f};
-    if (tid == 0) { sh.count = 0; sh.threshold = 0; }
-    __syncthreads();
-
-    auto take = [&](const float (&f)[TOP_PER], uint32_t live, auto index_of) {
-        // live: bit e set where f[e] is a logit
-        float m = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < TOP_PER; ++e) m = fmaxf(m, f[e]);      // what is not live holds -inf
-        const float mn = fmaxf(run.m, m), z = finite_or_zero(mn);
-        float s = run.s * __builtin_amdgcn_exp2f((run.m - z) * c);
-#pragma unroll
-        for (int e = 0; e < TOP_PER; ++e) s += __builtin_amdgcn_exp2f((f[e] - z) * c);
-        run.m = mn;
-        run.s = s;
-        for (;;) {
-            const uint64_t thr = sh.threshold;
-            const float tv = value_of((uint32_t)(thr >> 32));      // (threshold 0: NaN, which nothing is below)
-#pragma unroll
-            for (int e = 0; e < TOP_PER; ++e) {
-                if (!(f[e] < tv) && (live >> e & 1u)) {
-                    const uint64_t k = key_of(ordered(f[e]), (uint32_t)index_of(e));
-                    if (k > thr) {
-                        const int at = atomicAdd(&sh.count, 1);
-                        if (at < TOP_CAP) { sh.list[at] = k; live &= ~(1u << e); }
-                    } else {
-                        live &= ~(1u << e);
-                    }
-                } else {
-                    live &= ~(1u << e);
-                }
-            }
-            __syncthreads();
-            const int have = sh.count;
-            if (have <= TOP_CAP) break;              // everyone's logits are in the list or below the threshold
-            top_rank(sh, TOP_CAP, K);                // (K < TOP_CAP: there are K of them)
-            for (int i = tid; i < K; i += TOP_THREADS) sh.list[i] = sh.best[i];
-            if (tid == 0) { sh.count = K; sh.threshold = sh.best[K - 1]; }
-            __syncthreads();
-        }
-        __syncthreads();
-    };
-
-    for (int b0 = 0; b0 == 0 || b0 < nvec; b0 += TOP_THREADS * U) {
-        float f[TOP_PER];
-        uint32_t live = 0;
+    auto load = [&](int b0, uint4 (&w)[U]) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = b0 + u * TOP_THREADS + tid;
-            if (i < nvec) {
-                const uint4 w = *reinterpret_cast<const uint4*>(x + head + (int64_t)i * EPV);
-                const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < EPV; ++e) {
-                    if constexpr (sizeof(T) == 4) f[u * EPV + e] = __uint_as_float(q[e]);
-                    else f[u * EPV + e] = __uint_as_float(e & 1 ? q[e >> 1] & 0xffff0000u : q[e >> 1] << 16);
-                }
-                live |= ((1u << EPV) - 1u) << (u * EPV);
-            } else {
-#pragma unroll
-                for (int e = 0; e < EPV; ++e) f[u * EPV + e] = -INFINITY;
-            }
+            w[u] = make_uint4(0, 0, 0, 0);
+            if (i < nvec) w[u] = *reinterpret_cast<const uint4*>(x + head + (int64_t)i * EPV);
         }
-        if (b0 == 0) {
-            // first threshold: the K-th largest of the threads' maxima
-            uint32_t o = 0;
-#pragma unroll
-            for (int e = 0; e < TOP_PER; ++e) o = (live >> e & 1u) ? max(o, ordered(f[e])) : o;
-            sh.most[tid] = o;
-            __syncthreads();
-            int rank = 0;
-            for (int j = 0; j < TOP_THREADS; ++j) {
-                const uint32_t m = sh.most[j];
-                rank += (m > o || (m == o && j < tid)) ? 1 : 0;
-            }
-            if (rank == K - 1) sh.threshold = o ? ((uint64_t)o << 32) - 1 : 0;
-            __syncthreads();
-        }
-        take(f, live, [&](int e) { return first + head + (b0 + (e / EPV) * TOP_THREADS + tid) * EPV + e % EPV; });
+    };
+    auto value = [&](const uint4 (&w)[U], int e) -> float {
+        const uint4 v = w[e / EPV];
+        const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+        if constexpr (sizeof(T) == 4) return __uint_as_float(q[e % 4]);
+        else return __uint_as_float(e & 1 ? q[(e % 8) >> 1] & 0xffff0000u : q[(e % 8) >> 1] << 16);
+    };
+    uint4 w[U];
+    load(0, w);
+    float odd = -INFINITY;                       // this thread's logit of the ends
+    const bool has_odd = tid < head + tail;
+    const int odd_at = tid < head ? tid : n - tail + (tid - head);
+    if (has_odd) {
+        if constexpr (sizeof(T) == 4) odd = x[odd_at];
+        else odd = __uint_as_float((uint32_t)x[odd_at] << 16);
     }
-    if (head + tail > 0) {
-        float f[TOP_PER];
+    if (tid == 0) sh.count = 0;
+    ExpSum run = {-INFINITY, 0.f};
+    uint64_t thr = 0;                            // keys above it are kept
+    int before = 0;                              // keys in the list
+
+    for (int b0 = 0; b0 == 0 || b0 < nvec; b0 += TOP_THREADS * U) {
+        const int left = nvec - b0 - tid;        // slot u of this thread holds logits where u TOP_THREADS < left
+        float m = b0 == 0 ? odd : -INFINITY;
 #pragma unroll
-        for (int e = 0; e < TOP_PER; ++e) f[e] = -INFINITY;
-        const int at = tid < head ? tid : n - tail + (tid - head);
-        const bool mine = tid < head + tail;
-        if (mine) f[0] = as_float(x[at]);
-        take(f, mine ? 1u : 0u, [&](int) { return first + at; });
+        for (int u = 0; u < U; ++u)
+            if (u * TOP_THREADS < left) {
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) m = fmaxf(m, value(w, u * EPV + e));
+            }
+        const float mn = fmaxf(run.m, m), z = finite_or_zero(mn);
+        float s = run.s * __builtin_amdgcn_exp2f((run.m - z) * c);
+        if (b0 == 0) s += __builtin_amdgcn_exp2f((odd - z) * c);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u * TOP_THREADS < left) {
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f((value(w, u * EPV + e) - z) * c);
+            }
+        run.m = mn;
+        run.s = s;
+        if (b0 == 0) {
+            // (a NaN is not among the maxima: the threshold may be lower than it could be)
+            uint32_t o = left > 0 || has_odd ? ordered(m) >> 16 : 0;
+            const int want = (K + TOP_WAVES - 1) / TOP_WAVES;
+            uint32_t t = 0;                      // the largest prefix that `want` maxima of the wave reach
+#pragma unroll
+            for (int bit = 15; bit >= 0; --bit) {
+                const uint32_t q = t | 1u << bit;
+                t = __popcll(__ballot(o >= q)) >= want ? q : t;
+            }
+            if (lane == 0) sh.most[tid >> 6] = t;
+            __syncthreads();
+            t = sh.most[0];
+#pragma unroll
+            for (int k = 1; k < TOP_WAVES; ++k) t = min(t, sh.most[k]);
+            thr = t ? ((uint64_t)t << 48) - 1 : 0;
+        }
+        for (;;) {
+            const float tv = value_of((uint32_t)(thr >> 32));      // (threshold 0: NaN, which nothing is below)
+            auto keep = [&](bool on, float f, int index) {
+                on = on && !(f < tv);
+                if (__any(on)) {
+                    const uint64_t k = key_of(ordered(f), (uint32_t)index);
+                    on = on && k > thr;
+                    const unsigned long long b = __ballot(on);
+                    int base = 0;
+                    if (lane == 0 && b) base = atomicAdd(&sh.count, __popcll(b));
+                    base = __builtin_amdgcn_readfirstlane(base) + __popcll(b & ((1ull << lane) - 1ull));
+                    if (on && base < TOP_CAP) sh.list[base] = k;
+                }
+            };
+            if (b0 == 0) keep(has_odd, odd, first + odd_at);
+            // (opaque, so that 32 values and indexes are not all worked out ahead and held in registers)
+            int at = first + head + (b0 + tid) * EPV;
+            asm volatile("" : "+v"(at));
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                asm volatile("" : "+v"(w[u].x), "+v"(w[u].y), "+v"(w[u].z), "+v"(w[u].w));
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) keep(u * TOP_THREADS < left, value(w, u * EPV + e), at + e);
+                at += TOP_THREADS * EPV;
+            }
+            __syncthreads();
+            const int have = sh.count;
+            if (have <= max(TOP_THREADS, 2 * K)) {
+                before = have;
+                __syncthreads();                 // everyone has read the count
+                break;
+            }
+            const bool fits = have <= TOP_CAP;
+            top_rank(sh, min(have, TOP_CAP), K);
+            const uint64_t kth = sh.best[K - 1];
+            if (fits) {
+                for (int i = tid; i < K; i += TOP_THREADS) sh.list[i] = sh.best[i];
+                if (tid == 0) sh.count = K;
+                before = K;
+                thr = kth;
+                __syncthreads();
+                break;
+            }
+            // too many of this batch for the list: what was there before it stays as far as it beats the new threshold, and the batch is
+            // gone through again (the K-th key itself may be one of the batch)
+            thr = kth - 1;
+            uint64_t mine[TOP_CAP / TOP_THREADS];
+#pragma unroll
+            for (int q = 0; q < TOP_CAP / TOP_THREADS; ++q) {
+                const int i = q * TOP_THREADS + tid;
+                mine[q] = i < before ? sh.list[i] : 0;
+            }
+            if (tid == 0) sh.count = 0;
+            __syncthreads();
+#pragma unroll
+            for (int q = 0; q < TOP_CAP / TOP_THREADS; ++q)
+                if (mine[q] > thr) sh.list[atomicAdd(&sh.count, 1)] = mine[q];
+            __syncthreads();
+            before = sh.count;
+            __syncthreads();
+        }
+        if (b0 + TOP_THREADS * U < nvec) load(b0 + TOP_THREADS * U, w);
     }
     const ExpSum e = block_join(sh, run, c);
-    const int have = sh.count;
+    const int have = before;
     for (int i = have + tid; i < K; i += TOP_THREADS) sh.best[i] = 0;      // a segment shorter than K
     top_rank(sh, have, K);
     if (p.splits == 1) {
@@ -237,9 +279,11 @@ __global__ __launch_bounds__(TOP_THREADS) void top_merge_kernel(TopParams p) {
     const int64_t row = blockIdx.x;
     const uint64_t* const keys = p.part_keys + row * p.splits * p.K;
     const float c = p.inv_t * LOG2E;
-    uint64_t thr = 0;
-    for (int s = 0; s < p.splits; ++s) {
-        const uint64_t k = keys[(int64_t)s * p.K + p.K - 1];
+    uint64_t thr = 0;                            // (at most 64 segments: one for each lane)
+    if ((tid & 63) < p.splits) thr = keys[(int64_t)(tid & 63) * p.K + p.K - 1];
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        const uint64_t k = (uint64_t)__shfl_xor((unsigned long long)thr, o);
         thr = k > thr ? k : thr;
     }
     if (tid == 0) sh.count = 0;
