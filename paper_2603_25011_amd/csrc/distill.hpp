@@ -194,13 +194,13 @@ __global__ __launch_bounds__(TEACHER_THREADS) void distill_teacher_kernel(Teache
         if (!t.given_lse) {
 #pragma unroll
             for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-            const float z = finite_or_zero(m);
+            const float cc = t.inv_t * LOG2E, z = finite_or_zero(m);
             float s = 0.f;
 #pragma unroll
-            for (int k = 0; k < PER; ++k) s += __builtin_amdgcn_exp2f((x[q][k] - z) * (t.inv_t * LOG2E));
+            for (int k = 0; k < PER; ++k) s += __builtin_amdgcn_exp2f((x[q][k] - z) * cc);
 #pragma unroll
             for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-            L = s == 0.f ? 0.f : fmaf(z, t.inv_t, logf(s));
+            L = s == 0.f ? 0.f : log_sum(ExpSum{z, s}, t.inv_t);
         }
         float mass = 0.f;
 #pragma unroll
@@ -265,7 +265,7 @@ struct LogitsParams {
     int V, K, ga;
     float inv_t;
     // forward
-    float2* part;              // [n_vt][places]: (maximum, sum of exp) of a tile's logits of a token
+    float2* part;              // [n_vt][places]: sum of exp (ExpSum) of a tile's logits of a token
     int places;                // pitch of part: N
     float* picked;             // [N, K] logits at the teacher's ids (times temperature: as the product gives them)
     // backward
@@ -515,7 +515,7 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_loss_kernel(Teacher t, R
     for (int g = 0; g < LOSS_GROUPS; ++g) e.m = fmaxf(e.m, s_part[g][tok].x);
 #pragma unroll 8
     for (int g = 0; g < LOSS_GROUPS; ++g) e.s += s_part[g][tok].y * __builtin_amdgcn_exp2f((s_part[g][tok].x - finite_or_zero(e.m)) * cc);
-    const float lse = e.m == -INFINITY ? e.m : fmaf(e.m, t.inv_t, logf(e.s));
+    const float lse = log_sum(e, t.inv_t);
     float sum = 0.f;
     if (i < n) {
         const int64_t r = list.row(i);

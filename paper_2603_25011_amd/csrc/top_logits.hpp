@@ -34,7 +34,8 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 }
 __device__ __forceinline__ uint64_t key_of(uint32_t o, uint32_t index) { return (uint64_t)o << 32 | (uint32_t)~index; }
 
-// Running maximum and sum of exp2((x - m) c), c = log2(e) / temperature.  m = -inf: no finite logit yet.
+// Running maximum and sum of exp2((x - m) c), c = log2(e) / temperature.  m = -inf: no finite logit yet.  (The difference is formed first: with one
+// fused multiply-add x c - m c instead, the rounding of m c overflows the sum where a mask holds the type's lowest value.)
 struct ExpSum { float m, s; };
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ ExpSum join(ExpSum a, ExpSum b, float c) {
@@ -44,11 +45,8 @@ __device__ __forceinline__ ExpSum join(ExpSum a, ExpSum b, float c) {
     r.s = a.s * __builtin_amdgcn_exp2f((a.m - z) * c) + b.s * __builtin_amdgcn_exp2f((b.m - z) * c);
     return r;
 }
-// log of the normaliser: NaN where a logit is NaN, else +inf where one is +inf
-__device__ __forceinline__ float log_normaliser(ExpSum e, float inv_t, bool nan) {
-    if (nan) return __uint_as_float(0x7fc00000u);
-    if (e.m == INFINITY || e.m == -INFINITY) return e.m;
-    return fmaf(e.m, inv_t, logf(e.s));
+__device__ __forceinline__ float log_sum(ExpSum e, float inv_t) {
+    return fabsf(e.m) == INFINITY ? e.m : fmaf(e.m, inv_t, logf(e.s));
 }
 
 struct TopShared {
@@ -110,7 +108,8 @@ __device__ __forceinline__ void top_store(const TopParams& p, int64_t row, const
         p.values[row * p.K + i] = value_of((uint32_t)(k >> 32));
         p.ids[row * p.K + i] = (int)~(uint32_t)k;
     }
-    if (threadIdx.x == 0 && p.lse) p.lse[row] = log_normaliser(e, p.inv_t, (sh.best[0] >> 32) == 0xffffffffu);
+    // NaN where a logit is NaN (which is then the first key); else +inf where one is +inf
+    if (threadIdx.x == 0 && p.lse) p.lse[row] = (sh.best[0] >> 32) == 0xffffffffu ? __uint_as_float(0x7fc00000u) : log_sum(e, p.inv_t);
 }
 
 template <typename T>
@@ -223,7 +222,7 @@ __global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p)
             }
             __syncthreads();
             const int have = sh.count;
-            if (have <= max(TOP_THREADS, 2 * K)) {
+            if (have <= K + K / 4 + 8) {
                 before = have;
                 __syncthreads();                 // everyone has read the count
                 break;
@@ -272,20 +271,27 @@ __global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p)
     }
 }
 
-// Joins the segments of a row: only keys that are no smaller than the largest of the segments' K-th keys can be among the K.
+// Joins the segments of a row.  K keys are no smaller than the largest of the segments' K-th keys, and K are no smaller than the smallest of
+// their (K / segments)-th: only what reaches both is looked at.
 __global__ __launch_bounds__(TOP_THREADS) void top_merge_kernel(TopParams p) {
     __shared__ TopShared sh;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
     const uint64_t* const keys = p.part_keys + row * p.splits * p.K;
     const float c = p.inv_t * LOG2E;
-    uint64_t thr = 0;                            // (at most 64 segments: one for each lane)
-    if ((tid & 63) < p.splits) thr = keys[(int64_t)(tid & 63) * p.K + p.K - 1];
+    // (at most 64 segments: one for each lane)
+    uint64_t kth = 0, share = ~0ull;
+    if ((tid & 63) < p.splits) {
+        kth = keys[(int64_t)(tid & 63) * p.K + p.K - 1];
+        share = keys[(int64_t)(tid & 63) * p.K + (p.K + p.splits - 1) / p.splits - 1];
+    }
 #pragma unroll
     for (int o = 32; o; o >>= 1) {
-        const uint64_t k = (uint64_t)__shfl_xor((unsigned long long)thr, o);
-        thr = k > thr ? k : thr;
+        const uint64_t a = (uint64_t)__shfl_xor((unsigned long long)kth, o), b = (uint64_t)__shfl_xor((unsigned long long)share, o);
+        kth = a > kth ? a : kth;
+        share = b < share ? b : share;
     }
+    const uint64_t thr = kth > share ? kth : share;
     if (tid == 0) sh.count = 0;
     __syncthreads();
     for (int i = tid; i < p.splits * p.K; i += TOP_THREADS) {
