@@ -6,7 +6,7 @@
 namespace lsr {
 
 // A workgroup takes a segment of a row (the whole row, where there are enough rows to fill the chip) in batches of TOP_BATCH
-// logits held in registers.  Every logit has a 64-bit key, its value as an ordered integer above its index complemented: larger
+// logits.  Every logit has a 64-bit key, its value as an ordered integer above its index complemented: larger
 // key = earlier in the result, and no two are equal.  The workgroup keeps the keys that beat a threshold in an LDS list.  The first
 // threshold comes from the threads' maxima over the first batch: the smallest over the waves of the K/4-th largest of a wave's 64, so at least K
 // logits are no smaller, and few more are.  When the list has grown it is cut to its K largest, whose last is the next threshold.
@@ -113,7 +113,7 @@ __device__ __forceinline__ void top_store(const TopParams& p, int64_t row, const
 }
 
 template <typename T>
-__global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p) {
+__global__ __launch_bounds__(TOP_THREADS, 8) void top_logits_kernel(TopParams p) {
     __shared__ TopShared sh;
     constexpr int EPV = 16 / sizeof(T);          // logits per 16-byte load
     constexpr int U = TOP_PER / EPV;
@@ -130,22 +130,14 @@ __global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p)
     const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(T));
     const int nvec = (n - head) / EPV;
     const int tail = n - head - nvec * EPV;
-    auto load = [&](int b0, uint4 (&w)[U]) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = b0 + u * TOP_THREADS + tid;
-            w[u] = make_uint4(0, 0, 0, 0);
-            if (i < nvec) w[u] = *reinterpret_cast<const uint4*>(x + head + (int64_t)i * EPV);
-        }
+    auto fetch = [&](int i) -> uint4 {
+        return i < nvec ? *reinterpret_cast<const uint4*>(x + head + (int64_t)i * EPV) : make_uint4(0, 0, 0, 0);
     };
-    auto value = [&](const uint4 (&w)[U], int e) -> float {
-        const uint4 v = w[e / EPV];
-        const uint32_t q[4] = {v.x, v.y, v.z, v.w};
-        if constexpr (sizeof(T) == 4) return __uint_as_float(q[e % 4]);
-        else return __uint_as_float(e & 1 ? q[(e % 8) >> 1] & 0xffff0000u : q[(e % 8) >> 1] << 16);
+    auto value = [](const uint4& w, int e) -> float {
+        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+        if constexpr (sizeof(T) == 4) return __uint_as_float(q[e]);
+        else return __uint_as_float(e & 1 ? q[e >> 1] & 0xffff0000u : q[e >> 1] << 16);
     };
-    uint4 w[U];
-    load(0, w);
     float odd = -INFINITY;                       // this thread's logit of the ends
     const bool has_odd = tid < head + tail;
     const int odd_at = tid < head ? tid : n - tail + (tid - head);
@@ -154,71 +146,89 @@ __global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p)
         else odd = __uint_as_float((uint32_t)x[odd_at] << 16);
     }
     if (tid == 0) sh.count = 0;
-    ExpSum run = {-INFINITY, 0.f};
+
+    // first threshold, from the maxima over the first batch (a NaN is not among them: the threshold may then be lower than it could be)
     uint64_t thr = 0;                            // keys above it are kept
+    ExpSum run = {odd, has_odd && odd != -INFINITY ? 1.f : 0.f};
+    {
+        float m = odd;
+#pragma unroll 2
+        for (int u = 0; u < U; ++u) {
+            const int i = u * TOP_THREADS + tid;
+            const uint4 w = fetch(i);
+            float mv = value(w, 0);
+#pragma unroll
+            for (int e = 1; e < EPV; ++e) mv = fmaxf(mv, value(w, e));
+            m = i < nvec ? fmaxf(m, mv) : m;
+        }
+        const uint32_t o = tid < nvec || has_odd ? ordered(m) >> 16 : 0;
+        const int want = (K + TOP_WAVES - 1) / TOP_WAVES;
+        uint32_t t = 0;                          // the largest prefix that `want` maxima of the wave reach
+#pragma unroll 4
+        for (uint32_t bit = 1u << 15; bit; bit >>= 1) t = __popcll(__ballot(o >= (t | bit))) >= want ? t | bit : t;
+        if (lane == 0) sh.most[tid >> 6] = t;
+        __syncthreads();
+        t = sh.most[0];
+#pragma unroll
+        for (int k = 1; k < TOP_WAVES; ++k) t = min(t, sh.most[k]);
+        thr = t ? ((uint64_t)t << 48) - 1 : 0;
+        if (has_odd && !(odd == odd)) run = {-INFINITY, odd};     // (a NaN stays in the sum)
+    }
     int before = 0;                              // keys in the list
 
-    for (int b0 = 0; b0 == 0 || b0 < nvec; b0 += TOP_THREADS * U) {
-        const int left = nvec - b0 - tid;        // slot u of this thread holds logits where u TOP_THREADS < left
-        float m = b0 == 0 ? odd : -INFINITY;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u * TOP_THREADS < left) {
-#pragma unroll
-                for (int e = 0; e < EPV; ++e) m = fmaxf(m, value(w, u * EPV + e));
-            }
-        const float mn = fmaxf(run.m, m), z = finite_or_zero(mn);
-        float s = run.s * __builtin_amdgcn_exp2f((run.m - z) * c);
-        if (b0 == 0) s += __builtin_amdgcn_exp2f((odd - z) * c);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u * TOP_THREADS < left) {
-#pragma unroll
-                for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f((value(w, u * EPV + e) - z) * c);
-            }
-        run.m = mn;
-        run.s = s;
-        if (b0 == 0) {
-            // (a NaN is not among the maxima: the threshold may be lower than it could be)
-            uint32_t o = left > 0 || has_odd ? ordered(m) >> 16 : 0;
-            const int want = (K + TOP_WAVES - 1) / TOP_WAVES;
-            uint32_t t = 0;                      // the largest prefix that `want` maxima of the wave reach
-#pragma unroll
-            for (int bit = 15; bit >= 0; --bit) {
-                const uint32_t q = t | 1u << bit;
-                t = __popcll(__ballot(o >= q)) >= want ? q : t;
-            }
-            if (lane == 0) sh.most[tid >> 6] = t;
-            __syncthreads();
-            t = sh.most[0];
-#pragma unroll
-            for (int k = 1; k < TOP_WAVES; ++k) t = min(t, sh.most[k]);
-            thr = t ? ((uint64_t)t << 48) - 1 : 0;
+    // one logit of every lane into the list, where it beats the threshold
+    auto keep = [&](bool on, float f, float tv, int index) {
+        on = on && !(f < tv);
+        if (__any(on)) {
+            const uint64_t k = key_of(ordered(f), (uint32_t)index);
+            on = on && k > thr;
+            const unsigned long long b = __ballot(on);
+            int base = 0;
+            if (lane == 0 && b) base = atomicAdd(&sh.count, __popcll(b));
+            base = __builtin_amdgcn_readfirstlane(base) + __popcll(b & ((1ull << lane) - 1ull));
+            if (on && base < TOP_CAP) sh.list[base] = k;
         }
+    };
+    for (int b0 = 0; b0 == 0 || b0 < nvec; b0 += TOP_THREADS * U) {
+        bool again = false;                      // the batch is gone through again: its sum is done
         for (;;) {
             const float tv = value_of((uint32_t)(thr >> 32));      // (threshold 0: NaN, which nothing is below)
-            auto keep = [&](bool on, float f, int index) {
-                on = on && !(f < tv);
-                if (__any(on)) {
-                    const uint64_t k = key_of(ordered(f), (uint32_t)index);
-                    on = on && k > thr;
-                    const unsigned long long b = __ballot(on);
-                    int base = 0;
-                    if (lane == 0 && b) base = atomicAdd(&sh.count, __popcll(b));
-                    base = __builtin_amdgcn_readfirstlane(base) + __popcll(b & ((1ull << lane) - 1ull));
-                    if (on && base < TOP_CAP) sh.list[base] = k;
+            if (b0 == 0) keep(has_odd, odd, tv, first + odd_at);
+            auto one = [&](const uint4& w, int i) {
+                const bool in = i < nvec;
+                if (!again) {
+                    float m = value(w, 0);
+#pragma unroll
+                    for (int e = 1; e < EPV; ++e) m = fmaxf(m, value(w, e));
+                    m = in ? m : -INFINITY;
+                    if (__any(m > run.m)) {      // (seldom, behind the first few)
+                        const float mn = fmaxf(run.m, m), z = finite_or_zero(mn);
+                        run.s *= __builtin_amdgcn_exp2f((run.m - z) * c);
+                        run.m = mn;
+                    }
+                    const float z = finite_or_zero(run.m);
+                    float s = 0.f;
+#pragma unroll
+                    for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f((value(w, e) - z) * c);
+                    run.s += in ? s : 0.f;
                 }
+                const int at = first + head + i * EPV;
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) keep(in, value(w, e), tv, at + e);
             };
-            if (b0 == 0) keep(has_odd, odd, first + odd_at);
-            // (opaque, so that 32 values and indexes are not all worked out ahead and held in registers)
-            int at = first + head + (b0 + tid) * EPV;
-            asm volatile("" : "+v"(at));
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                asm volatile("" : "+v"(w[u].x), "+v"(w[u].y), "+v"(w[u].z), "+v"(w[u].w));
-#pragma unroll
-                for (int e = 0; e < EPV; ++e) keep(u * TOP_THREADS < left, value(w, u * EPV + e), at + e);
-                at += TOP_THREADS * EPV;
+            int i = b0 + tid;
+            uint4 w0 = fetch(i), w1 = fetch(i + TOP_THREADS);
+#pragma unroll 1
+            for (int u = 0; u < U; u += 2, i += 2 * TOP_THREADS) {
+                uint4 n0 = w0, n1 = w1;
+                if (u + 2 < U) {
+                    n0 = fetch(i + 2 * TOP_THREADS);
+                    n1 = fetch(i + 3 * TOP_THREADS);
+                }
+                one(w0, i);
+                one(w1, i + TOP_THREADS);
+                w0 = n0;
+                w1 = n1;
             }
             __syncthreads();
             const int have = sh.count;
@@ -231,7 +241,7 @@ __global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p)
             top_rank(sh, min(have, TOP_CAP), K);
             const uint64_t kth = sh.best[K - 1];
             if (fits) {
-                for (int i = tid; i < K; i += TOP_THREADS) sh.list[i] = sh.best[i];
+                for (int q = tid; q < K; q += TOP_THREADS) sh.list[q] = sh.best[q];
                 if (tid == 0) sh.count = K;
                 before = K;
                 thr = kth;
@@ -240,12 +250,13 @@ __global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p)
             }
             // too many of this batch for the list: what was there before it stays as far as it beats the new threshold, and the batch is
             // gone through again (the K-th key itself may be one of the batch)
+            again = true;
             thr = kth - 1;
             uint64_t mine[TOP_CAP / TOP_THREADS];
 #pragma unroll
             for (int q = 0; q < TOP_CAP / TOP_THREADS; ++q) {
-                const int i = q * TOP_THREADS + tid;
-                mine[q] = i < before ? sh.list[i] : 0;
+                const int k = q * TOP_THREADS + tid;
+                mine[q] = k < before ? sh.list[k] : 0;
             }
             if (tid == 0) sh.count = 0;
             __syncthreads();
@@ -256,7 +267,6 @@ __global__ __launch_bounds__(TOP_THREADS, 6) void top_logits_kernel(TopParams p)
             before = sh.count;
             __syncthreads();
         }
-        if (b0 + TOP_THREADS * U < nvec) load(b0 + TOP_THREADS * U, w);
     }
     const ExpSum e = block_join(sh, run, c);
     const int have = before;
