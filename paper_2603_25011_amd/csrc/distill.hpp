@@ -280,28 +280,6 @@ struct LogitsParams {
     int db_pitch;
 };
 
-// Half of a tile in float32 through LDS: tokens 128 h .. 128 h + 127, a row of 256 vocabulary entries each, in the ring (which
-// is free behind the product).  16-byte chunks are XORed with the token, so that writes (lanes on 32 tokens), reads along a row and reads down
-// columns (16 entries by 4 groups of 8 tokens) all spread over the banks.
-struct HalfTile {
-    uint8_t *ring0, *ring1;
-    __device__ __forceinline__ float* at(int tok, int v) const {       // tok: 0 .. 127
-        const int swz = (tok & 15) ^ ((tok >> 2) & 4);
-        return reinterpret_cast<float*>((tok < 64 ? ring0 + tok * 1024 : ring1 + (tok - 64) * 1024) + (((v >> 2) ^ swz) << 4)) + (v & 3);
-    }
-    __device__ __forceinline__ void write(const TileLane& t, int h, const floatx16 (&acc)[4][2]) const {
-        if (t.wn >> 1 != h) return;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4)
-                    *reinterpret_cast<float4*>(at(t.col(c) & 127, t.row(i, r))) =
-                        make_float4(acc[i][c][r], acc[i][c][r + 1], acc[i][c][r + 2], acc[i][c][r + 3]);
-    }
-};
-
 template <bool SPLIT, bool BWD>
 __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsParams p) {
     __shared__ __attribute__((aligned(1024))) uint8_t s_ring0[TP_STAGE];

@@ -21,63 +21,102 @@ struct Int8Params {
     int na, nb, ga;            // tiles of rows and of vocabulary entries, row tiles per group
 };
 
-// Many rows: one 256 x 256 tile per workgroup, tokens as tile rows, vocabulary entries as columns (lanes hold
-// neighbouring columns, so a store is whole 32-column pieces of a row).
+// Eight logits of a row from entry v, of which `left` exist; the row may begin at any element.
+template <typename OT>
+__device__ __forceinline__ void store8(OT* o, const float (&x)[8], int left) {
+    if (left >= 8) {
+        if constexpr (sizeof(OT) == 4) {
+            struct __attribute__((packed, aligned(4))) F4 { float v[4]; };
+            *reinterpret_cast<F4*>(o) = F4{x[0], x[1], x[2], x[3]};
+            *reinterpret_cast<F4*>(o + 4) = F4{x[4], x[5], x[6], x[7]};
+        } else {
+            struct __attribute__((packed, aligned(2))) U4 { uint32_t v[4]; };
+            U4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w.v[e] = bf16_bits(x[2 * e]) | (uint32_t)bf16_bits(x[2 * e + 1]) << 16;
+            *reinterpret_cast<U4*>(o) = w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) o[e] = as_type<OT>(x[e]);
+    }
+}
+
+// Many rows: one 256 x 256 tile per workgroup, the vocabulary along the tile's rows.  The logits go through LDS, so that a row of the result leaves in pieces of
+// 512 bytes or more: straight from the accumulators, as 2-byte stores of 32 columns, the stores took twice as long as the products (8192 x 768 x 30522
+// to bfloat16, 430 us).
 template <typename OT>
 __global__ __launch_bounds__(TP_THREADS, 2) void int8_tile_kernel(Int8Params p) {
     __shared__ __attribute__((aligned(1024))) uint8_t s_ring0[TP_STAGE];
     __shared__ __attribute__((aligned(1024))) uint8_t s_ring1[TP_STAGE];
-    __shared__ float s_scale[TP_T];
+    __shared__ __attribute__((aligned(16))) float s_ws[TP_T], s_bs[TP_T];
     int u, at, bt;
     if (!xcd_unit(p.na * p.nb, u)) return;
     tile_of_unit(u, p.na, p.nb, p.ga, at, bt);
     const TileLane t;
     const int n0 = at * TP_T, v0 = bt * TP_T;
-    if (t.tid < TP_T) s_scale[t.tid] = p.a_scale[min(n0 + t.tid, p.N - 1)];
-    float ws[2], bs[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int v = min(v0 + t.col(c), p.V - 1);
-        ws[c] = p.w_scale[v];
-        bs[c] = p.bias ? p.bias[v] : 0.f;
+    if (t.tid < TP_T) {
+        const int v = min(v0 + t.tid, p.V - 1);
+        s_ws[t.tid] = p.w_scale[v];
+        s_bs[t.tid] = p.bias ? p.bias[v] : 0.f;
     }
+    float as[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) as[c] = p.a_scale[min(n0 + t.col(c), p.N - 1)];
     intx16 acc[4][2];
-    tile_product<intx4, false>(s_ring0, s_ring1, row_operand(p.A, (size_t)p.lda, 0, n0, p.N), row_operand(p.W, (size_t)p.ldw, 0, v0, p.V),
+    tile_product<intx4, false>(s_ring0, s_ring1, row_operand(p.W, (size_t)p.ldw, 0, v0, p.V), row_operand(p.A, (size_t)p.lda, 0, n0, p.N),
                                p.row_bytes / TP_RB, acc);
-    __syncthreads();
     OT* const out = reinterpret_cast<OT*>(p.out);
+    const HalfTile half = {s_ring0, s_ring1};
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+        if (n0 + h * 128 >= p.N) break;
+        __syncthreads();
+        if (t.wn >> 1 == h) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = t.row(i, r);
-            if (n0 + row < p.N) {
-                OT* const o = out + (int64_t)(n0 + row) * p.ldo + v0;
-                const float a = s_scale[row];
+                for (int r = 0; r < 16; r += 4) {
+                    const int v = t.row(i, r);
+                    const float4 w = *reinterpret_cast<const float4*>(&s_ws[v]), b = *reinterpret_cast<const float4*>(&s_bs[v]);
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (v0 + t.col(c) < p.V) o[t.col(c)] = as_type<OT>(fmaf((float)acc[i][c][r], a * ws[c], bs[c]));
-            }
+                    for (int c = 0; c < 2; ++c)
+                        *reinterpret_cast<float4*>(half.at(t.col(c) & 127, v)) =
+                            make_float4(fmaf((float)acc[i][c][r], as[c] * w.x, b.x), fmaf((float)acc[i][c][r + 1], as[c] * w.y, b.y),
+                                        fmaf((float)acc[i][c][r + 2], as[c] * w.z, b.z), fmaf((float)acc[i][c][r + 3], as[c] * w.w, b.w));
+                }
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int k = 0; k < 8; ++k) {
+            const int tok = t.wave * 16 + k * 2 + t.half, n = n0 + h * 128 + tok;
+            float x[8];
+            *reinterpret_cast<float4*>(&x[0]) = *reinterpret_cast<const float4*>(half.at(tok, t.l32 * 8));
+            *reinterpret_cast<float4*>(&x[4]) = *reinterpret_cast<const float4*>(half.at(tok, t.l32 * 8 + 4));
+            if (n < p.N) store8<OT>(out + (int64_t)n * p.ldo + v0 + t.l32 * 8, x, p.V - v0 - t.l32 * 8);
         }
     }
 }
 
 // Few rows (the tokens of one decoding or query step): what bounds the call is reading W once.  A wave owns 32 vocabulary
 // entries at a time and takes their rows straight into registers as MFMA fragments, FEW8_U k-steps (32 bytes of a row
-// each) requested while the FEW8_U before them are multiplied; the rows of A lie in LDS, quantised there by every
-// workgroup from the values if the caller has not done it (the first loads of W are in flight meanwhile), so the call is one launch.
+// each) requested while those before them are multiplied; the rows of A lie in LDS.  Up to FEW8_OWN rows are quantised there by every
+// workgroup from the values (the first loads of W are in flight meanwhile), so the call is one launch.
 constexpr int FEW8_THREADS = 256;
 constexpr int FEW8_COLS = 32 * FEW8_THREADS / 64;
 constexpr int FEW8_ROWS = 64;
+constexpr int FEW8_OWN = 16;
 constexpr int FEW8_U = 12;
-constexpr int FEW8_LDS = 60 * 1024;               // of the rows of A
+constexpr int FEW8_LDS = 156 * 1024;              // of the rows of A at most; up to FEW8_LDS_TWO two workgroups share a CU
+constexpr int FEW8_LDS_TWO = 76 * 1024;
 // LDS bytes of a row: padded so that the 32 rows of a fragment read lie on different banks
 inline int few8_stride(int row_bytes) { return row_bytes + 16; }
 
-template <typename T, typename OT, bool VEC>
-__global__ __launch_bounds__(FEW8_THREADS) void int8_few_kernel(Int8Params p, int stride, int n_tiles) {
-    extern __shared__ __attribute__((aligned(16))) uint8_t s_a[];       // [N][stride]
-    __shared__ float s_scale[FEW8_ROWS];
+template <typename T, typename OT, bool VEC, int NB, bool TWO>
+__global__ __launch_bounds__(FEW8_THREADS, TWO ? 2 : 1) void int8_few_kernel(Int8Params p, int stride, int n_tiles) {
+    __shared__ __attribute__((aligned(16))) uint8_t s_a[TWO ? FEW8_LDS_TWO : FEW8_LDS];       // [N][stride]
+    __shared__ float s_scale[32 * NB];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
     const int nks = p.row_bytes / 32;
     int tile = blockIdx.x;
@@ -131,8 +170,7 @@ __global__ __launch_bounds__(FEW8_THREADS) void int8_few_kernel(Int8Params p, in
     }
     __syncthreads();
     OT* const out = reinterpret_cast<OT*>(p.out);
-    auto blocks = [&](auto nb_c) {
-        constexpr int NB = decltype(nb_c)::value;
+    {
         const uint8_t* sa[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) sa[i] = s_a + min(i * 32 + l32, p.N - 1) * stride + half * 16;
@@ -177,9 +215,7 @@ __global__ __launch_bounds__(FEW8_THREADS) void int8_few_kernel(Int8Params p, in
                     }
             }
         }
-    };
-    if (p.N > 32) blocks(std::integral_constant<int, 2>{});
-    else blocks(std::integral_constant<int, 1>{});
+    }
 }
 
 }  // namespace lsr

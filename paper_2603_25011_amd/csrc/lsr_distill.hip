@@ -38,9 +38,11 @@ void quantize(int32_t type, const void* X, int64_t ldx, int64_t rows, int cols, 
     else launch_quantize<uint16_t>(X, ldx, rows, cols, Q, ldq, scale, st);
 }
 
-// Few rows: their quantised form fits the LDS of the kernel that reads W straight into registers.
+// Few rows: their quantised form fits the LDS of the kernel that reads W straight into registers.  Against tiles of 256 x 256 (us): 64 rows, 384 x 30522
+// 10.6 / 16, 1024 x 250002 82 / 100.  (With 96 or 128 rows its accumulators leave one workgroup per CU: 384 x 30522 15.3 / 16.5 and 18.2 / 17,
+// 1024 x 250002 142 / 105 and 168 / 114; not kept.)
 bool int8_few(int64_t N, int64_t K) {
-    return N <= FEW8_ROWS && N * few8_stride((int)up(K, 128)) <= FEW8_LDS;
+    return N <= FEW8_ROWS && N * few8_stride((int)up(K, 128)) <= (N <= 32 ? FEW8_LDS_TWO : FEW8_LDS);
 }
 
 struct Int8Ws { size_t q, scale, total; };
@@ -52,19 +54,28 @@ Int8Ws int8_ws(int64_t N, int64_t K) {
     return w;
 }
 
-template <typename OT>
-void launch_int8_few(const Int8Params& p, int32_t a_type, int n_cus, hipStream_t st) {
+template <typename T, typename OT, bool VEC>
+void launch_int8_few(const Int8Params& p, int n_cus, hipStream_t st) {
     const int stride = few8_stride(p.row_bytes);
     const int n_tiles = (p.V + FEW8_COLS - 1) / FEW8_COLS;
-    const unsigned grid = (unsigned)(n_tiles < 2 * n_cus ? n_tiles : 2 * n_cus);
-    const size_t lds = (size_t)p.N * stride;
-    if (a_type == LSR_I8) int8_few_kernel<int8_t, OT, true><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
+    const bool two = p.N * stride <= FEW8_LDS_TWO;
+    const int resident = two ? 2 * n_cus : n_cus;
+    const unsigned grid = (unsigned)(n_tiles < resident ? n_tiles : resident);
+    if (p.N <= 32) int8_few_kernel<T, OT, VEC, 1, true><<<grid, FEW8_THREADS, 0, st>>>(p, stride, n_tiles);
+    else if constexpr (sizeof(T) == 1) {
+        if (two) int8_few_kernel<T, OT, VEC, 2, true><<<grid, FEW8_THREADS, 0, st>>>(p, stride, n_tiles);
+        else int8_few_kernel<T, OT, VEC, 2, false><<<grid, FEW8_THREADS, 0, st>>>(p, stride, n_tiles);
+    }
+}
+template <typename OT>
+void int8_few_of_type(const Int8Params& p, int32_t a_type, int n_cus, hipStream_t st) {
+    if (a_type == LSR_I8) launch_int8_few<int8_t, OT, true>(p, n_cus, st);
     else if (a_type == LSR_F32) {
-        if (rows_on_16(p.A, p.lda, 4)) int8_few_kernel<float, OT, true><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
-        else int8_few_kernel<float, OT, false><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
+        if (rows_on_16(p.A, p.lda, 4)) launch_int8_few<float, OT, true>(p, n_cus, st);
+        else launch_int8_few<float, OT, false>(p, n_cus, st);
     } else {
-        if (rows_on_16(p.A, p.lda, 2)) int8_few_kernel<uint16_t, OT, true><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
-        else int8_few_kernel<uint16_t, OT, false><<<grid, FEW8_THREADS, lds, st>>>(p, stride, n_tiles);
+        if (rows_on_16(p.A, p.lda, 2)) launch_int8_few<uint16_t, OT, true>(p, n_cus, st);
+        else launch_int8_few<uint16_t, OT, false>(p, n_cus, st);
     }
 }
 
@@ -394,16 +405,18 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
     p.lda = lda; p.ldw = ldw; p.ldo = ldo;
     p.N = (int)N; p.V = (int)V; p.K = (int)K; p.row_bytes = (int)row_bytes;
     p.na = (int)na; p.nb = (int)nb; p.ga = 8;
-    if (int8_few(N, K)) {
-        if (out_dtype == LSR_F32) launch_int8_few<float>(p, a_dtype, n_cus, stream);
-        else launch_int8_few<uint16_t>(p, a_dtype, n_cus, stream);
-        return launch_status();
-    }
-    if (a_dtype != LSR_I8) {
+    const bool few = int8_few(N, K);
+    if (a_dtype != LSR_I8 && !(few && N <= FEW8_OWN)) {
         int8_t* const q = static_cast<int8_t*>(workspace) + w.q;
         float* const scale = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.scale);
         quantize(a_dtype, A, lda, N, (int)K, q, row_bytes, scale, stream);
         p.A = q; p.lda = row_bytes; p.a_scale = scale;
+        a_dtype = LSR_I8;
+    }
+    if (few) {
+        if (out_dtype == LSR_F32) int8_few_of_type<float>(p, a_dtype, n_cus, stream);
+        else int8_few_of_type<uint16_t>(p, a_dtype, n_cus, stream);
+        return launch_status();
     }
     const unsigned grid = xcd_grid((long long)na * nb);
     if (out_dtype == LSR_F32) int8_tile_kernel<float><<<grid, TP_THREADS, 0, stream>>>(p);

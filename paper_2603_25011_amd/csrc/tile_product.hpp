@@ -147,6 +147,28 @@ __device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, con
     mma_rot<4, KS, 2, LPT, SPREAD>(ring0, 0, ring0, 0, fsw, fa, fb, acc, [](int) {});
 }
 
+// Half of a tile of logits (vocabulary along the rows, tokens along the columns) in float32 through LDS: tokens 128 h .. 128 h + 127, a row of 256
+// vocabulary entries each, in the ring (which is free behind the product).  16-byte chunks are XORed with the token, so that writes (lanes on 32 tokens), reads along a row and reads down
+// columns (16 entries by 4 groups of 8 tokens) all spread over the banks.
+struct HalfTile {
+    uint8_t *ring0, *ring1;
+    __device__ __forceinline__ float* at(int tok, int v) const {       // tok: 0 .. 127
+        const int swz = (tok & 15) ^ ((tok >> 2) & 4);
+        return reinterpret_cast<float*>((tok < 64 ? ring0 + tok * 1024 : ring1 + (tok - 64) * 1024) + (((v >> 2) ^ swz) << 4)) + (v & 3);
+    }
+    __device__ __forceinline__ void write(const TileLane& t, int h, const floatx16 (&acc)[4][2]) const {
+        if (t.wn >> 1 != h) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *reinterpret_cast<float4*>(at(t.col(c) & 127, t.row(i, r))) =
+                        make_float4(acc[i][c][r], acc[i][c][r + 1], acc[i][c][r + 2], acc[i][c][r + 3]);
+    }
+};
+
 // Units of work in the order they are handed out: workgroup ids go round-robin over the 8 XCDs, and each XCD
 // takes a contiguous eighth of the units, so that units next to each other share operand rows in its L2.
 __device__ __forceinline__ bool xcd_unit(int n_units, int& u) {

@@ -175,7 +175,15 @@ __global__ __launch_bounds__(TOP_THREADS, 8) void top_logits_kernel(TopParams p)
         if (has_odd && !(odd == odd)) run = {-INFINITY, odd};     // (a NaN stays in the sum)
     }
     int before = 0;                              // keys in the list
+    bool ordered_list = false;                   // the list is its K largest, in order
 
+    // which of a vector's logits are not below tv: bit EPV - 1 - e.  Two instructions each: a compare, and the carry shifted in.
+    auto not_below = [&](const uint4& w, float tv, uint32_t bits) -> uint32_t {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+            asm("v_cmp_nlt_f32_e32 vcc, %1, %2\n\tv_addc_co_u32_e32 %0, vcc, %0, %0, vcc" : "+v"(bits) : "v"(value(w, e)), "v"(tv) : "vcc");
+        return bits;
+    };
     // one logit of every lane into the list, where it beats the threshold
     auto keep = [&](bool on, float f, float tv, int index) {
         on = on && !(f < tv);
@@ -194,27 +202,43 @@ __global__ __launch_bounds__(TOP_THREADS, 8) void top_logits_kernel(TopParams p)
         for (;;) {
             const float tv = value_of((uint32_t)(thr >> 32));      // (threshold 0: NaN, which nothing is below)
             if (b0 == 0) keep(has_odd, odd, tv, first + odd_at);
-            auto one = [&](const uint4& w, int i) {
+            auto sum = [&](const uint4& w, int i) {
                 const bool in = i < nvec;
-                if (!again) {
-                    float m = value(w, 0);
+                float m = value(w, 0);
 #pragma unroll
-                    for (int e = 1; e < EPV; ++e) m = fmaxf(m, value(w, e));
-                    m = in ? m : -INFINITY;
-                    if (__any(m > run.m)) {      // (seldom, behind the first few)
-                        const float mn = fmaxf(run.m, m), z = finite_or_zero(mn);
-                        run.s *= __builtin_amdgcn_exp2f((run.m - z) * c);
-                        run.m = mn;
-                    }
-                    const float z = finite_or_zero(run.m);
-                    float s = 0.f;
-#pragma unroll
-                    for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f((value(w, e) - z) * c);
-                    run.s += in ? s : 0.f;
+                for (int e = 1; e < EPV; ++e) m = fmaxf(m, value(w, e));
+                m = in ? m : -INFINITY;
+                if (__any(m > run.m)) {          // (seldom, behind the first few)
+                    const float mn = fmaxf(run.m, m), z = finite_or_zero(mn);
+                    run.s *= __builtin_amdgcn_exp2f((run.m - z) * c);
+                    run.m = mn;
                 }
-                const int at = first + head + i * EPV;
+                const float z = finite_or_zero(run.m);
+                float s = 0.f;
 #pragma unroll
-                for (int e = 0; e < EPV; ++e) keep(in, value(w, e), tv, at + e);
+                for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f((value(w, e) - z) * c);
+                run.s += in ? s : 0.f;
+            };
+            // the logits of two vectors that are not below the threshold, one of each lane at a time (few lanes have any, fewer have two)
+            auto pick = [&](const uint4& w0, const uint4& w1, int i) {
+                uint32_t bits = not_below(w1, tv, not_below(w0, tv, 0));
+                const uint32_t none1 = (1u << EPV) - 1u;
+                bits &= i + TOP_THREADS < nvec ? ~0u : i < nvec ? ~none1 : 0u;
+                while (__any(bits != 0)) {
+                    const bool on = bits != 0;
+                    const int e = __builtin_clz(bits | 1u) - (32 - 2 * EPV);       // place among the 2 EPV
+                    bits &= ~(1u << (2 * EPV - 1 - e));
+                    const uint4 w = e >= EPV ? w1 : w0;
+                    const int h = e & (EPV - 1);
+                    float f;
+                    if constexpr (sizeof(T) == 4) {
+                        f = __uint_as_float(h & 2 ? (h & 1 ? w.w : w.z) : (h & 1 ? w.y : w.x));
+                    } else {
+                        const uint32_t d = h & 4 ? (h & 2 ? w.w : w.z) : (h & 2 ? w.y : w.x);
+                        f = __uint_as_float(h & 1 ? d & 0xffff0000u : d << 16);
+                    }
+                    keep(on, f, tv, first + head + (i + (e >= EPV ? TOP_THREADS : 0)) * EPV + h);
+                }
             };
             int i = b0 + tid;
             uint4 w0 = fetch(i), w1 = fetch(i + TOP_THREADS);
@@ -225,14 +249,18 @@ __global__ __launch_bounds__(TOP_THREADS, 8) void top_logits_kernel(TopParams p)
                     n0 = fetch(i + 2 * TOP_THREADS);
                     n1 = fetch(i + 3 * TOP_THREADS);
                 }
-                one(w0, i);
-                one(w1, i + TOP_THREADS);
+                if (!again) {
+                    sum(w0, i);
+                    sum(w1, i + TOP_THREADS);
+                }
+                pick(w0, w1, i);
                 w0 = n0;
                 w1 = n1;
             }
             __syncthreads();
             const int have = sh.count;
             if (have <= K + K / 4 + 8) {
+                ordered_list = ordered_list && have == before;
                 before = have;
                 __syncthreads();                 // everyone has read the count
                 break;
@@ -244,6 +272,7 @@ __global__ __launch_bounds__(TOP_THREADS, 8) void top_logits_kernel(TopParams p)
                 for (int q = tid; q < K; q += TOP_THREADS) sh.list[q] = sh.best[q];
                 if (tid == 0) sh.count = K;
                 before = K;
+                ordered_list = true;
                 thr = kth;
                 __syncthreads();
                 break;
@@ -251,6 +280,7 @@ __global__ __launch_bounds__(TOP_THREADS, 8) void top_logits_kernel(TopParams p)
             // too many of this batch for the list: what was there before it stays as far as it beats the new threshold, and the batch is
             // gone through again (the K-th key itself may be one of the batch)
             again = true;
+            ordered_list = false;
             thr = kth - 1;
             uint64_t mine[TOP_CAP / TOP_THREADS];
 #pragma unroll
@@ -271,7 +301,7 @@ __global__ __launch_bounds__(TOP_THREADS, 8) void top_logits_kernel(TopParams p)
     const ExpSum e = block_join(sh, run, c);
     const int have = before;
     for (int i = have + tid; i < K; i += TOP_THREADS) sh.best[i] = 0;      // a segment shorter than K
-    top_rank(sh, have, K);
+    if (!ordered_list) top_rank(sh, have, K);    // (else `best` holds them already)
     if (p.splits == 1) {
         top_store(p, row, sh, e);
     } else {
