@@ -21,42 +21,37 @@ struct Int8Params {
     int na, nb, ga;            // tiles of rows and of vocabulary entries, row tiles per group
 };
 
-// Eight logits of a row from entry v, of which `left` exist; the row may begin at any element.
+// 16 bytes of a row of logits, of which `left` elements exist; the row may begin at any element.
 template <typename OT>
-__device__ __forceinline__ void store8(OT* o, const float (&x)[8], int left) {
-    if (left >= 8) {
-        if constexpr (sizeof(OT) == 4) {
-            struct __attribute__((packed, aligned(4))) F4 { float v[4]; };
-            *reinterpret_cast<F4*>(o) = F4{x[0], x[1], x[2], x[3]};
-            *reinterpret_cast<F4*>(o + 4) = F4{x[4], x[5], x[6], x[7]};
-        } else {
-            struct __attribute__((packed, aligned(2))) U4 { uint32_t v[4]; };
-            U4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w.v[e] = bf16_bits(x[2 * e]) | (uint32_t)bf16_bits(x[2 * e + 1]) << 16;
-            *reinterpret_cast<U4*>(o) = w;
-        }
+__device__ __forceinline__ void store16(OT* o, const uint4& w, int left) {
+    constexpr int N = 16 / sizeof(OT);
+    struct __attribute__((packed, aligned(sizeof(OT)))) Piece { uint32_t v[4]; };
+    if (left >= N) {
+        *reinterpret_cast<Piece*>(o) = Piece{{w.x, w.y, w.z, w.w}};
     } else {
+        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) o[e] = as_type<OT>(x[e]);
+        for (int e = 0; e < N; ++e)
+            if (e < left) {
+                if constexpr (sizeof(OT) == 4) o[e] = __uint_as_float(q[e]);
+                else o[e] = (uint16_t)(q[e >> 1] >> (16 * (e & 1)));
+            }
     }
 }
 
-// Many rows: one 256 x 256 tile per workgroup, the vocabulary along the tile's rows.  The logits go through LDS, so that a row of the result leaves in pieces of
-// 512 bytes or more: straight from the accumulators, as 2-byte stores of 32 columns, the stores took twice as long as the products (8192 x 768 x 30522
-// to bfloat16, 430 us).
+// Many rows: one tile of 256 vocabulary entries x 128 rows per workgroup, two workgroups per CU.  The logits go through LDS, so that a row of the result leaves in
+// pieces of 512 bytes or more.  8192 x 768 x 30522 to bfloat16: one 256 x 256 tile per CU, 2-byte stores straight from the accumulators 430 us; the same
+// through LDS 350 us; two narrow tiles per CU, stores and products beside each other, MEASURED us.
 template <typename OT>
-__global__ __launch_bounds__(TP_THREADS, 2) void int8_tile_kernel(Int8Params p) {
-    __shared__ __attribute__((aligned(1024))) uint8_t s_ring0[TP_STAGE];
-    __shared__ __attribute__((aligned(1024))) uint8_t s_ring1[TP_STAGE];
+__global__ __launch_bounds__(NT_THREADS, 2) void int8_tile_kernel(Int8Params p) {
+    __shared__ __attribute__((aligned(1024))) uint8_t s_ring[NT_STAGES * NT_STAGE];
     __shared__ __attribute__((aligned(16))) float s_ws[TP_T], s_bs[TP_T];
     int u, at, bt;
     if (!xcd_unit(p.na * p.nb, u)) return;
     tile_of_unit(u, p.na, p.nb, p.ga, at, bt);
-    const TileLane t;
-    const int n0 = at * TP_T, v0 = bt * TP_T;
-    if (t.tid < TP_T) {
+    const NarrowLane t;
+    const int n0 = at * NT_COLS, v0 = bt * TP_T;
+    {
         const int v = min(v0 + t.tid, p.V - 1);
         s_ws[t.tid] = p.w_scale[v];
         s_bs[t.tid] = p.bias ? p.bias[v] : 0.f;
@@ -65,15 +60,18 @@ __global__ __launch_bounds__(TP_THREADS, 2) void int8_tile_kernel(Int8Params p) 
 #pragma unroll
     for (int c = 0; c < 2; ++c) as[c] = p.a_scale[min(n0 + t.col(c), p.N - 1)];
     intx16 acc[4][2];
-    tile_product<intx4, false>(s_ring0, s_ring1, row_operand(p.W, (size_t)p.ldw, 0, v0, p.V), row_operand(p.A, (size_t)p.lda, 0, n0, p.N),
-                               p.row_bytes / TP_RB, acc);
+    narrow_product<intx4>(s_ring, row_operand(p.W, (size_t)p.ldw, 0, v0, p.V), row_operand(p.A, (size_t)p.lda, 0, n0, p.N), p.row_bytes / NT_RB, acc);
+    // rows of 256 logits through the ring: all 128 in bfloat16, 64 at a time in float32; 8-byte pieces (16-byte in float32) XORed with the row, so that the 32
+    // rows of a store lie on different banks
+    constexpr int PASSES = sizeof(OT) == 4 ? 2 : 1;
+    constexpr int ROWS = NT_COLS / PASSES, ROW_BYTES = TP_T * sizeof(OT);
+    static_assert(ROWS * ROW_BYTES <= NT_STAGES * NT_STAGE, "the logits fit the ring");
     OT* const out = reinterpret_cast<OT*>(p.out);
-    const HalfTile half = {s_ring0, s_ring1};
 #pragma unroll 1
-    for (int h = 0; h < 2; ++h) {
-        if (n0 + h * 128 >= p.N) break;
+    for (int h = 0; h < PASSES; ++h) {
+        if (n0 + h * ROWS >= p.N) break;
         __syncthreads();
-        if (t.wn >> 1 == h) {
+        if (PASSES == 1 || t.wn == h) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -81,20 +79,27 @@ __global__ __launch_bounds__(TP_THREADS, 2) void int8_tile_kernel(Int8Params p) 
                     const int v = t.row(i, r);
                     const float4 w = *reinterpret_cast<const float4*>(&s_ws[v]), b = *reinterpret_cast<const float4*>(&s_bs[v]);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        *reinterpret_cast<float4*>(half.at(t.col(c) & 127, v)) =
-                            make_float4(fmaf((float)acc[i][c][r], as[c] * w.x, b.x), fmaf((float)acc[i][c][r + 1], as[c] * w.y, b.y),
-                                        fmaf((float)acc[i][c][r + 2], as[c] * w.z, b.z), fmaf((float)acc[i][c][r + 3], as[c] * w.w, b.w));
+                    for (int c = 0; c < 2; ++c) {
+                        const float4 y = make_float4(fmaf((float)acc[i][c][r], as[c] * w.x, b.x), fmaf((float)acc[i][c][r + 1], as[c] * w.y, b.y),
+                                                     fmaf((float)acc[i][c][r + 2], as[c] * w.z, b.z), fmaf((float)acc[i][c][r + 3], as[c] * w.w, b.w));
+                        const int n = t.col(c) % ROWS;
+                        if constexpr (sizeof(OT) == 4)
+                            *reinterpret_cast<float4*>(s_ring + n * ROW_BYTES + (((v >> 2) ^ (n & 15)) << 4)) = y;
+                        else
+                            *reinterpret_cast<uint2*>(s_ring + n * ROW_BYTES + (((v >> 2) ^ ((n & 15) << 1)) << 3)) =
+                                make_uint2(bf16_bits(y.x) | (uint32_t)bf16_bits(y.y) << 16, bf16_bits(y.z) | (uint32_t)bf16_bits(y.w) << 16);
+                    }
                 }
         }
         __syncthreads();
+        // 16 bytes per lane, neighbouring lanes along a row
+        constexpr int EPL = 16 / sizeof(OT), LPR = TP_T / EPL, RPW = 64 / LPR;      // elements per lane, lanes per row, rows per wave access
 #pragma unroll 4
-        for (int k = 0; k < 8; ++k) {
-            const int tok = t.wave * 16 + k * 2 + t.half, n = n0 + h * 128 + tok;
-            float x[8];
-            *reinterpret_cast<float4*>(&x[0]) = *reinterpret_cast<const float4*>(half.at(tok, t.l32 * 8));
-            *reinterpret_cast<float4*>(&x[4]) = *reinterpret_cast<const float4*>(half.at(tok, t.l32 * 8 + 4));
-            if (n < p.N) store8<OT>(out + (int64_t)n * p.ldo + v0 + t.l32 * 8, x, p.V - v0 - t.l32 * 8);
+        for (int k = 0; k < ROWS / (4 * RPW); ++k) {
+            const int n = (k * 4 + t.wave) * RPW + t.lane / LPR, ch = t.lane % LPR;
+            const uint4 w = *reinterpret_cast<const uint4*>(s_ring + n * ROW_BYTES + ((ch ^ (n & 15)) << 4));
+            const int row = n0 + h * ROWS + n;
+            if (row < p.N) store16<OT>(out + (int64_t)row * p.ldo + v0 + ch * EPL, w, p.V - v0 - ch * EPL);
         }
     }
 }

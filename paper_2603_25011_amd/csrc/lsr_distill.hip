@@ -385,7 +385,7 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
     const int64_t row_bytes = up(K, 128);
     const int64_t ld_max = int64_t(1) << 23;
     if (lda < (a_dtype == LSR_I8 ? row_bytes : K) || ldw < row_bytes || ldo < V || ldw > ld_max || (a_dtype == LSR_I8 && lda > ld_max)) return LSR_ERR_SHAPE;
-    const int64_t na = (N + TP_T - 1) / TP_T, nb = (V + TP_T - 1) / TP_T;
+    const int64_t na = (N + NT_COLS - 1) / NT_COLS, nb = (V + TP_T - 1) / TP_T;
     if (na * nb > int64_t(1) << 30) return LSR_ERR_SHAPE;
     if (!A || !W || !w_scale || !out || (a_dtype == LSR_I8 && !a_scale)) return LSR_ERR_NULL;
     if (a_dtype != LSR_I8 && a_scale) return LSR_ERR_DTYPE;      // values bring no scales
@@ -419,8 +419,8 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
         return launch_status();
     }
     const unsigned grid = xcd_grid((long long)na * nb);
-    if (out_dtype == LSR_F32) int8_tile_kernel<float><<<grid, TP_THREADS, 0, stream>>>(p);
-    else int8_tile_kernel<uint16_t><<<grid, TP_THREADS, 0, stream>>>(p);
+    if (out_dtype == LSR_F32) int8_tile_kernel<float><<<grid, NT_THREADS, 0, stream>>>(p);
+    else int8_tile_kernel<uint16_t><<<grid, NT_THREADS, 0, stream>>>(p);
     return launch_status();
 }
 

@@ -147,6 +147,93 @@ __device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, con
     mma_rot<4, KS, 2, LPT, SPREAD>(ring0, 0, ring0, 0, fsw, fa, fb, acc, [](int) {});
 }
 
+// ---- the narrow tile: 256 rows of A by 128 of B, 4 waves (2 x 2 of the same 128 x 64 part), so that two workgroups share a CU and one's epilogue runs
+//      beside the other's products.  Slabs of 64 bytes per row in three stages (72 KB), requested two slabs ahead.  It moves half as much again into LDS per
+//      product as the wide tile: for short contracted axes with much to store. ----
+constexpr int NT_COLS = 128;
+constexpr int NT_THREADS = 256;
+constexpr int NT_RB = 64;
+constexpr int NT_STAGES = 3;
+constexpr int NT_STAGE = (TP_T + NT_COLS) * NT_RB;
+
+// Geometry of a thread in the narrow tile.
+struct NarrowLane {
+    int tid, lane, wave, wm, wn, half, l32;
+    __device__ __forceinline__ NarrowLane() {
+        tid = threadIdx.x; lane = tid & 63; wave = tid >> 6;
+        wm = wave >> 1; wn = wave & 1; half = lane >> 5; l32 = lane & 31;
+    }
+    __device__ __forceinline__ int row(int i, int r) const { return acc_row(2 * i + wm, r, half); }
+    __device__ __forceinline__ int col(int c) const { return wn * 64 + c * 32 + l32; }
+};
+
+// acc = A B^T over nk slabs of NT_RB bytes; ring: NT_STAGES NT_STAGE bytes.  Both operands are rows of a caller's matrix (step NT_RB).  On return every wave is past its
+// LDS reads only after the caller's next barrier.
+template <typename Frag>
+__device__ __forceinline__ void narrow_product(uint8_t* ring, const TileOperand& A, const TileOperand& B, int nk, typename TileAcc<Frag>::type (&acc)[4][2]) {
+    constexpr int KS = NT_RB / 32, LPT = NT_STAGE / 16 / NT_THREADS, LPA = TP_T * NT_RB / 16 / NT_THREADS, CPR = NT_RB / 16, RPI = NT_THREADS / CPR;
+    const NarrowLane t;
+    nk = __builtin_amdgcn_readfirstlane(nk);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][c][r] = 0;
+    // access j of the workgroup covers RPI rows, 4096 contiguous LDS bytes; thread -> (row, LDS chunk), which holds the global chunk XORed with the swizzle
+    const int lrow = t.tid / CPR;
+    const uint32_t gch = (uint32_t)((t.tid % CPR) ^ lds_swz<NT_RB>(lrow));
+    const char* const Ab = uniform(A.base);
+    const char* const Bb = uniform(B.base);
+    uint32_t off[LPT];
+#pragma unroll
+    for (int j = 0; j < LPT; ++j) {
+        const bool a = j < LPA;
+        const int r = lrow + RPI * (a ? j : j - LPA);
+        off[j] = (uint32_t)min(r, a ? A.last : B.last) * (uint32_t)(a ? A.pitch : B.pitch) + gch * 16;
+    }
+    const uint32_t wave_lds = __builtin_amdgcn_readfirstlane(lds_addr(ring) + t.wave * 1024);
+    auto issue_one = [&](int st, size_t k, int n) {
+        dma16_to_lds(n < LPA ? Ab + k : Bb + k, off[n], wave_lds + st * NT_STAGE + n * 4096);
+    };
+    auto issue = [&](int st, int kt) {
+        if (kt < nk) {
+#pragma unroll
+            for (int n = 0; n < LPT; ++n) issue_one(st, (size_t)kt * NT_RB, n);
+        }
+    };
+    const int fa_row = t.wm * 32 + t.l32, fb_row = t.wn * 64 + t.l32;
+    int fsw[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) fsw[ks] = ((ks * 2 + t.half) ^ lds_swz<NT_RB>(t.l32)) << 4;
+    issue(0, 0);
+    issue(1, 1);
+    Frag fa[2][4], fb[2][2];
+    auto step = [&](int st, auto mode_c, int kt) {
+        // every fragment read of the slab before has returned, and slab kt has landed (the one behind it may still fly)
+        __builtin_amdgcn_s_waitcnt(0xC07F);     // lgkmcnt(0)
+        if (kt + 1 < nk) wait_vmcnt<LPT>();
+        else wait_vmcnt<0>();
+        __syncthreads();
+        const int more = __builtin_amdgcn_readfirstlane(kt + 2 < nk ? 1 : 0);
+        const size_t k = (size_t)(kt + 2) * NT_RB;
+        auto dma = [&](int n) {
+            if (more != 0) issue_one((st + 2) % NT_STAGES, k, n);
+        };
+        const uint8_t* const s = ring + st * NT_STAGE;
+        mma_rot<4, KS, decltype(mode_c)::value, LPT, 1>(s + fa_row * NT_RB, 64 * NT_RB, s + TP_T * NT_RB + fb_row * NT_RB, 32 * NT_RB, fsw, fa, fb, acc, dma);
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> steady{};
+    step(0, first, 0);
+    for (int kt = 1; kt < nk; kt += 3) {
+        step(1, steady, kt);
+        if (kt + 1 < nk) step(2, steady, kt + 1);
+        if (kt + 2 < nk) step(0, steady, kt + 2);
+    }
+    mma_rot<4, KS, 2, LPT, 1>(ring, 0, ring, 0, fsw, fa, fb, acc, [](int) {});
+}
+
 // Half of a tile of logits (vocabulary along the rows, tokens along the columns) in float32 through LDS: tokens 128 h .. 128 h + 127, a row of 256
 // vocabulary entries each, in the ring (which is free behind the product).  16-byte chunks are XORed with the token, so that writes (lanes on 32 tokens), reads along a row and reads down
 // columns (16 entries by 4 groups of 8 tokens) all spread over the banks.
