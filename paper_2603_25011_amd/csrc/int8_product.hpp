@@ -21,13 +21,16 @@ struct Int8Params {
     int na, nb, ga;            // tiles of rows and of vocabulary entries, row tiles per group
 };
 
-// 16 bytes of a row of logits, of which `left` elements exist; the row may begin at any element.
-template <typename OT>
+// 16 bytes of a row of logits, of which `left` elements exist; the row may begin at any element.  PAST: past the caches.
+template <typename OT, bool PAST>
 __device__ __forceinline__ void store16(OT* o, const uint4& w, int left) {
     constexpr int N = 16 / sizeof(OT);
-    struct __attribute__((packed, aligned(sizeof(OT)))) Piece { uint32_t v[4]; };
     if (left >= N) {
-        *reinterpret_cast<Piece*>(o) = Piece{{w.x, w.y, w.z, w.w}};
+        typedef uint32_t V4 __attribute__((ext_vector_type(4)));
+        typedef V4 U4 __attribute__((aligned(2)));
+        const V4 x = {w.x, w.y, w.z, w.w};
+        if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<U4*>(o));
+        else *reinterpret_cast<U4*>(o) = x;
     } else {
         const uint32_t q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -41,8 +44,10 @@ __device__ __forceinline__ void store16(OT* o, const uint4& w, int left) {
 
 // Many rows: one tile of 256 vocabulary entries x 128 rows per workgroup, two workgroups per CU.  The logits go through LDS, so that a row of the result leaves in
 // pieces of 512 bytes or more.  8192 x 768 x 30522 to bfloat16: one 256 x 256 tile per CU, 2-byte stores straight from the accumulators 430 us; the same
-// through LDS 350 us; two narrow tiles per CU, stores and products beside each other, MEASURED us.
-template <typename OT>
+// through LDS 350 us; two narrow tiles per CU 345 us; with stores past the caches 272 us (the products alone take 220).  PAST: the host takes it where the result
+// is larger than the memory-side cache; written through it, it pushes the operands out (2048 x 1024 x 250002 787 -> 662 us), below that size plain
+// stores are as fast or faster (59 MB 27 / 30 us, 119 MB 47 / 56, 238 MB 145 / 143).
+template <typename OT, bool PAST>
 __global__ __launch_bounds__(NT_THREADS, 2) void int8_tile_kernel(Int8Params p) {
     __shared__ __attribute__((aligned(1024))) uint8_t s_ring[NT_STAGES * NT_STAGE];
     __shared__ __attribute__((aligned(16))) float s_ws[TP_T], s_bs[TP_T];
@@ -99,7 +104,7 @@ __global__ __launch_bounds__(NT_THREADS, 2) void int8_tile_kernel(Int8Params p) 
             const int n = (k * 4 + t.wave) * RPW + t.lane / LPR, ch = t.lane % LPR;
             const uint4 w = *reinterpret_cast<const uint4*>(s_ring + n * ROW_BYTES + ((ch ^ (n & 15)) << 4));
             const int row = n0 + h * ROWS + n;
-            if (row < p.N) store16<OT>(out + (int64_t)row * p.ldo + v0 + ch * EPL, w, p.V - v0 - ch * EPL);
+            if (row < p.N) store16<OT, PAST>(out + (int64_t)row * p.ldo + v0 + ch * EPL, w, p.V - v0 - ch * EPL);
         }
     }
 }

@@ -270,7 +270,7 @@ LogitsParams logits_params(const DShape& s, const DWs& w, char* ws, const Begun&
     p.hits = reinterpret_cast<const int2*>(ws + w.hits);
     p.first = reinterpret_cast<const int*>(ws + w.first);
     p.n_vt = s.n_vt; p.vt0 = 0; p.nvt = s.n_vt;
-    p.V = s.V; p.K = s.K; p.ga = 8; p.inv_t = s.inv_t;
+    p.V = s.V; p.K = s.K; p.ga = 4; p.inv_t = s.inv_t;
     return p;
 }
 
@@ -326,7 +326,7 @@ int run_backward(const DShape& s, const void* H, const void* W, const float* bia
     g.dh_first = w.grads.dh_first;
     g.D = s.D;
     g.nd = (s.D + TP_T - 1) / TP_T;
-    g.ga = 8;
+    g.ga = 4;
     for (int k = 0; k < pc.n; ++k) {
         const int v0 = k * pv;
         const int nv = s.V - v0 < pv ? s.V - v0 : pv;
@@ -419,8 +419,14 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
         return launch_status();
     }
     const unsigned grid = xcd_grid((long long)na * nb);
-    if (out_dtype == LSR_F32) int8_tile_kernel<float><<<grid, NT_THREADS, 0, stream>>>(p);
-    else int8_tile_kernel<uint16_t><<<grid, NT_THREADS, 0, stream>>>(p);
+    const bool past = (size_t)N * V * type_bytes(out_dtype) >= (size_t(1) << 28);      // the memory-side cache
+    if (out_dtype == LSR_F32) {
+        if (past) int8_tile_kernel<float, true><<<grid, NT_THREADS, 0, stream>>>(p);
+        else int8_tile_kernel<float, false><<<grid, NT_THREADS, 0, stream>>>(p);
+    } else {
+        if (past) int8_tile_kernel<uint16_t, true><<<grid, NT_THREADS, 0, stream>>>(p);
+        else int8_tile_kernel<uint16_t, false><<<grid, NT_THREADS, 0, stream>>>(p);
+    }
     return launch_status();
 }
 
