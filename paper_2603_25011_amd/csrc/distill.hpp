@@ -36,22 +36,40 @@ __global__ __launch_bounds__(COMPACT_THREADS) void distill_compact_kernel(const 
     __shared__ int s_wave[COMPACT_THREADS / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int base = 0;
-    for (int r0 = 0; r0 < N; r0 += COMPACT_THREADS) {
-        const int r = r0 + tid;
-        const bool on = r < N && mask[r] != 0;
-        const unsigned long long b = __ballot(on);
-        if (lane == 0) s_wave[wave] = __popcll(b);
+    for (int r0 = 0; r0 < N; r0 += COMPACT_THREADS * 16) {       // 16 mask bytes per thread
+        const int r = r0 + tid * 16;
+        uint8_t m[16] = {0};
+        if (r + 16 <= N) {
+            *reinterpret_cast<uint4*>(m) = *reinterpret_cast<const uint4*>(mask + r);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) m[e] = r + e < N ? mask[r + e] : 0;
+        }
+        int mine = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mine += m[e] != 0 ? 1 : 0;
+        int s = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(s, o);
+            if (lane >= o) s += y;
+        }
+        if (lane == 63) s_wave[wave] = s;
         __syncthreads();
-        int at = base + __popcll(b & ((1ull << lane) - 1ull));
-        int all = 0;
+        int at = base + s - mine, all = 0;
 #pragma unroll
         for (int w = 0; w < COMPACT_THREADS / 64; ++w) {
             at += w < wave ? s_wave[w] : 0;
             all += s_wave[w];
         }
-        if (on) rows[at] = r;
-        if (place && r < N) place[r] = on ? at : -1;
-        if (loss && r < N && !on) { loss[r] = 0.f; lse[r] = 0.f; }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const bool on = m[e] != 0;
+            if (on) rows[at] = r + e;
+            if (place && r + e < N) place[r + e] = on ? at : -1;
+            if (loss && r + e < N && !on) { loss[r + e] = 0.f; lse[r + e] = 0.f; }
+            at += on ? 1 : 0;
+        }
         base += all;
         __syncthreads();
     }
@@ -637,14 +655,20 @@ __global__ __launch_bounds__(256) void distill_dh_kernel(const float* __restrict
     }
 }
 
-// db from the token tiles' sums.
+// db from the token tiles' sums: 64 entries per workgroup, its four waves a quarter of the tiles each.
 __global__ __launch_bounds__(256) void distill_db_kernel(const float* __restrict__ part, int pitch, RowList list, int V, float* __restrict__ db) {
-    const int v = blockIdx.x * 256 + threadIdx.x;
-    if (v >= V) return;
+    __shared__ float s_sum[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int v = blockIdx.x * 64 + lane;
     const int ntt = (list.n() + TP_T - 1) / TP_T;
     float s = 0.f;
-    for (int k = 0; k < ntt; ++k) s += part[(size_t)k * pitch + v];
-    db[v] = s;
+    if (v < V) {
+#pragma unroll 4
+        for (int k = wave; k < ntt; k += 4) s += part[(size_t)k * pitch + v];
+    }
+    s_sum[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && v < V) db[v] = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
 }
 
 }  // namespace lsr

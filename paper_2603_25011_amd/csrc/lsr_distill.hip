@@ -81,9 +81,9 @@ void int8_few_of_type(const Int8Params& p, int32_t a_type, int n_cus, hipStream_
 
 // ---- top logits ----
 
-// Segments per row: enough workgroups to fill the chip where there are few rows, no segment shorter than TOP_MIN_SEG, no
-// more keys in all than the joining launch holds.
-constexpr int64_t TOP_WANTED = 2048;
+// Segments per row: enough workgroups to fill the chip where there are few rows (256 rows of 250002: 512 workgroups 106 us, 1024 90, 2048 102), no segment
+// shorter than TOP_MIN_SEG (one row of 30522: 2048 logits 15 us, 4096 13.5, 8192 16), no more keys in all than the joining launch holds.
+constexpr int64_t TOP_WANTED = 1024;
 constexpr int64_t TOP_MIN_SEG = 4096;
 struct TopPlan { int splits, seg; };
 TopPlan top_plan(int64_t rows, int64_t V, int64_t K) {
@@ -270,7 +270,7 @@ LogitsParams logits_params(const DShape& s, const DWs& w, char* ws, const Begun&
     p.hits = reinterpret_cast<const int2*>(ws + w.hits);
     p.first = reinterpret_cast<const int*>(ws + w.first);
     p.n_vt = s.n_vt; p.vt0 = 0; p.nvt = s.n_vt;
-    p.V = s.V; p.K = s.K; p.ga = 4; p.inv_t = s.inv_t;
+    p.V = s.V; p.K = s.K; p.ga = 8; p.inv_t = s.inv_t;
     return p;
 }
 
@@ -348,7 +348,7 @@ int run_backward(const DShape& s, const void* H, const void* W, const float* bia
     if (dH)
         distill_dh_kernel<T><<<(unsigned)(((int64_t)s.N * (s.D / 4) + 255) / 256), 256, 0, st>>>(g.dh_part, g.dh_plane, g.splits, b.place, s.N, s.D,
                                                                                                 static_cast<T*>(dH));
-    if (db) distill_db_kernel<<<(s.V + 255) / 256, 256, 0, st>>>(p.db_part, p.db_pitch, b.list, s.V, db);
+    if (db) distill_db_kernel<<<(s.V + 63) / 64, 256, 0, st>>>(p.db_part, p.db_pitch, b.list, s.V, db);
     return launch_status();
 }
 
