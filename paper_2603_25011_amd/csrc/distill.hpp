@@ -642,6 +642,7 @@ __global__ __launch_bounds__(256) void distill_dh_kernel(const float* __restrict
     const int i = place ? place[r] : r;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i >= 0) {
+#pragma unroll 4
         for (int k = 0; k < splits; ++k) {
             const float4 x = *reinterpret_cast<const float4*>(part + k * plane + (size_t)i * D + d);
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;

@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include "distill.hpp"
+#include "distill_few.hpp"
 #include "host_checks.hpp"
 #include "int8_product.hpp"
 #include "quantize.hpp"
@@ -189,10 +190,29 @@ struct DWs {
     size_t total;
     GradsPlan grads;
 };
+// Few rows (distill_few.hpp): their hidden states fit LDS.
+bool few_rows(const DShape& s) {
+    return s.N <= FEWD_ROWS && (int)up(s.N, 32) * fewd_stride(s.D * (s.dtype == LSR_F32 ? 4 : 2)) <= FEWD_H_LDS;
+}
+int few_tiles(const DShape& s) { return (s.V + 31) / 32; }
+// Workgroups of the pass over the vocabulary, four tiles of 32 entries each at a time; and parts of the vocabulary of the dH pass, with their 128-column workgroups about two
+// per CU, at least four tiles each.
+int few_blocks(const DShape& s) {
+    const int b = (few_tiles(s) + 3) / 4;
+    return b < GRADS_CUS ? b : GRADS_CUS;
+}
+int few_parts(const DShape& s) {
+    const int per = (s.D + 127) / 128, most = (few_tiles(s) + 3) / 4;
+    int k = (2 * GRADS_CUS + per - 1) / per;
+    k = k < most ? k : most;
+    return k < 1 ? 1 : k;
+}
+
 DWs distill_ws(const DShape& s, bool backward) {
     DWs w = {};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes); return o; };
+    const bool few = few_rows(s);
     w.rows = take((size_t)s.N * 4);
     w.count = take(4);
     w.place = take((size_t)s.N * 4);
@@ -200,11 +220,16 @@ DWs distill_ws(const DShape& s, bool backward) {
     w.mass = take((size_t)s.N * 4);
     w.hits = take((size_t)s.n_up * s.K * 8);
     w.first = take((size_t)s.n_tt * (TP_T / GROUP) * (s.n_vt + 1) * 4);
-    w.Hc = take((size_t)s.planes * s.N * s.width * 2);
-    w.Wc = in_place(s) ? 0 : take((size_t)s.planes * s.V * s.width * 2);
+    if (!few) {
+        w.Hc = take((size_t)s.planes * s.N * s.width * 2);
+        w.Wc = in_place(s) ? 0 : take((size_t)s.planes * s.V * s.width * 2);
+    }
     if (!backward) {
-        w.part = take((size_t)s.n_vt * s.N * 8);
+        w.part = take((size_t)(few ? few_blocks(s) : s.n_vt) * s.N * 8);
         w.picked = take((size_t)s.N * s.K * 4);
+    } else if (few) {
+        w.G = take((size_t)few_tiles(s) * 32 * up(s.N, 32) * 4);
+        w.dh_part = take((size_t)few_parts(s) * s.N * s.D * 4);
     } else {
         const Pieces p = pieces(s);
         const size_t pv = (size_t)p.tiles * TP_T;
@@ -229,7 +254,7 @@ struct Begun {
     const int* place;
 };
 template <typename T, int PLANES>
-Begun begin(const DShape& s, const DWs& w, char* ws, const void* H, const void* W, const int32_t* ids, const float* logits, const float* given_lse,
+Begun begin(bool few, const DShape& s, const DWs& w, char* ws, const void* H, const void* W, const int32_t* ids, const float* logits, const float* given_lse,
             const uint8_t* mask, float* loss, float* lse, hipStream_t st) {
     Begun b;
     int* const rows = reinterpret_cast<int*>(ws + w.rows);
@@ -245,10 +270,10 @@ Begun begin(const DShape& s, const DWs& w, char* ws, const void* H, const void* 
     b.pitch = (size_t)s.width * 2;
     b.h_plane = (size_t)s.N * s.width * 2;
     b.w_plane = (size_t)s.V * s.width * 2;
-    if (!h_here)
+    if (!h_here && !few)
         distill_rows_kernel<T, PLANES><<<(s.N + 3) / 4, 256, 0, st>>>(static_cast<const T*>(H), s.D, b.list, reinterpret_cast<uint16_t*>(ws + w.Hc),
                                                                       s.width, b.h_plane / 2);
-    if (!in_place(s))
+    if (!in_place(s) && !few)
         distill_rows_kernel<T, PLANES><<<(s.V + 3) / 4, 256, 0, st>>>(static_cast<const T*>(W), s.D, RowList{nullptr, nullptr, s.V},
                                                                       reinterpret_cast<uint16_t*>(ws + w.Wc), s.width, b.w_plane / 2);
     int2* const hits = reinterpret_cast<int2*>(ws + w.hits);
@@ -274,11 +299,33 @@ LogitsParams logits_params(const DShape& s, const DWs& w, char* ws, const Begun&
     return p;
 }
 
+template <typename T>
+FewDistillParams few_params(const DShape& s, const DWs& w, char* ws, const Begun& b, const void* H, const void* W, const float* bias) {
+    FewDistillParams p = {};
+    p.H = H; p.W = W; p.bias = bias; p.list = b.list;
+    p.hits = reinterpret_cast<const int2*>(ws + w.hits);
+    p.first = reinterpret_cast<const int*>(ws + w.first);
+    p.D = s.D; p.V = s.V; p.K = s.K; p.n_vt = s.n_vt; p.n_tiles = few_tiles(s);
+    p.stride = fewd_stride(s.D * (int)sizeof(T));
+    p.inv_t = s.inv_t;
+    p.places = s.N;
+    return p;
+}
+
 template <typename T, int PLANES>
 int run_forward(const DShape& s, const void* H, const void* W, const float* bias, const int32_t* ids, const float* logits, const float* given_lse,
                 const uint8_t* mask, float* loss, float* lse, char* ws, hipStream_t st) {
     const DWs w = distill_ws(s, false);
-    const Begun b = begin<T, PLANES>(s, w, ws, H, W, ids, logits, given_lse, mask, loss, lse, st);
+    const Begun b = begin<T, PLANES>(few_rows(s), s, w, ws, H, W, ids, logits, given_lse, mask, loss, lse, st);
+    if (few_rows(s)) {
+        FewDistillParams p = few_params<T>(s, w, ws, b, H, W, bias);
+        p.part = reinterpret_cast<float2*>(ws + w.part);
+        p.picked = reinterpret_cast<float*>(ws + w.picked);
+        if (s.N <= 32) distill_few_kernel<T, 1, false><<<few_blocks(s), FEWD_THREADS, 0, st>>>(p);
+        else distill_few_kernel<T, 2, false><<<few_blocks(s), FEWD_THREADS, 0, st>>>(p);
+        distill_loss_kernel<<<(s.N + LOSS_TOKENS - 1) / LOSS_TOKENS, LOSS_THREADS, 0, st>>>(b.teacher, b.list, p.part, few_blocks(s), s.N, p.picked, loss, lse);
+        return launch_status();
+    }
     LogitsParams p = logits_params(s, w, ws, b, bias);
     p.part = reinterpret_cast<float2*>(ws + w.part);
     p.places = s.N;
@@ -293,7 +340,28 @@ int run_backward(const DShape& s, const void* H, const void* W, const float* bia
                  const uint8_t* mask, const float* lse, const float* dloss, void* dH, void* dW, float* db, char* ws, hipStream_t st) {
     if (!dH && !dW && !db) return LSR_OK;
     const DWs w = distill_ws(s, true);
-    const Begun b = begin<T, PLANES>(s, w, ws, H, W, ids, logits, given_lse, mask, nullptr, nullptr, st);
+    const Begun b = begin<T, PLANES>(few_rows(s), s, w, ws, H, W, ids, logits, given_lse, mask, nullptr, nullptr, st);
+    if (few_rows(s)) {
+        FewDistillParams p = few_params<T>(s, w, ws, b, H, W, bias);
+        p.lse = lse;
+        p.dloss = dloss;
+        p.mass = b.teacher.mass;
+        p.G = dH ? ws + w.G : nullptr;
+        p.dW = dW;
+        p.db = db;
+        p.dh_part = reinterpret_cast<float*>(ws + w.dh_part);
+        p.parts = few_parts(s);
+        const dim3 grid(p.parts, (s.D + 127) / 128);
+        if (s.N <= 32) distill_few_kernel<T, 1, true><<<few_blocks(s), FEWD_THREADS, 0, st>>>(p);
+        else distill_few_kernel<T, 2, true><<<few_blocks(s), FEWD_THREADS, 0, st>>>(p);
+        if (dH) {
+            if (s.N <= 32) distill_few_dh_kernel<T, 1><<<grid, FEWD_THREADS, 0, st>>>(p);
+            else distill_few_dh_kernel<T, 2><<<grid, FEWD_THREADS, 0, st>>>(p);
+            distill_dh_kernel<T><<<(unsigned)(((int64_t)s.N * (s.D / 4) + 255) / 256), 256, 0, st>>>(p.dh_part, (size_t)s.N * s.D, p.parts, b.place, s.N, s.D,
+                                                                                                    static_cast<T*>(dH));
+        }
+        return launch_status();
+    }
     const Pieces pc = pieces(s);
     const int pv = pc.tiles * TP_T;
     uint16_t* const Ht = reinterpret_cast<uint16_t*>(ws + w.Ht);

@@ -7,8 +7,8 @@ namespace lsr {
 
 // Q = rne(127 x / m), scale = m / 127, m the largest magnitude of the row.  One wave per row, the row read once:
 // up to QUANT_REGS chunks of 8 elements per lane stay in registers between the maximum and the quotient (rows of up to 512 QUANT_REGS
-// elements; longer ones are read a second time, from the caches).  The quotient is a product with 1 / m, off by one level at most where it lies
-// near half-way, put right by its remainder 127 x - q m, which is exact: what is half-way between two levels goes to the even one.
+// elements; longer ones are read a second time, from the caches).  The level is the correctly rounded float32 quotient 127 x / m rounded to a whole number: by a
+// product with 1 / m, and by the division itself where the remainder 127 x - q m, which is exact, is near half a level.
 // Rows with a very large or very small maximum are scaled by a power of two first, so that neither 127 x nor 1 / m leaves the range of float32.
 // Bound by memory traffic (read e, write 1 byte per element).
 constexpr int QUANT_THREADS = 256;
@@ -31,8 +31,8 @@ __device__ __forceinline__ RowScale row_scale(uint32_t most) {
     s.scale = m / 127.f;
     return s;
 }
-// Eight levels as bytes.  A sum with 1.5 2^23 rounds to a whole number and leaves it in the low bits.  The remainder a - q m is exact; where one of the wave's is half
-// a level or more, the level next to it is taken, or of two equally near the even one.
+// Eight levels as bytes.  A sum with 1.5 2^23 rounds to a whole number and leaves it in the low bits.  The product with 1 / m and the rounded quotient are both within
+// 127 2^-24 of the quotient; where one of the wave's remainders is within 2^-16 of half a level, the eight are divided.
 __device__ __forceinline__ uint2 quantize8(const float (&x)[8], const RowScale& s) {
     if (s.m == 0.f) return make_uint2(0, 0);     // (the same for the whole wave; infinities and NaN of such a row are not looked at)
     constexpr float MAGIC = 0x1.8p23f;
@@ -43,14 +43,9 @@ __device__ __forceinline__ uint2 quantize8(const float (&x)[8], const RowScale& 
         t[i] = fmaf(a, s.inv, MAGIC);
         far = fmaxf(far, fabsf(fmaf(-(t[i] - MAGIC), s.m, a)));
     }
-    const float half = 0.5f * s.m;
-    if (__any(far >= half)) {
+    if (__any(far >= (0.5f - 0x1p-16f) * s.m)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float q = t[i] - MAGIC, r = fmaf(-q, s.m, s.k * x[i]);
-            const bool past = fabsf(r) > half || (fabsf(r) == half && (__float_as_uint(t[i]) & 1u));
-            t[i] += past ? copysignf(1.f, r) : 0.f;
-        }
+        for (int i = 0; i < 8; ++i) t[i] = (s.k * x[i]) / s.m + MAGIC;
     }
     uint32_t w[2];
 #pragma unroll

@@ -9,6 +9,9 @@ Argument checks and marshalling only: all arithmetic runs in the HIP library, on
 """
 from __future__ import annotations
 
+import contextlib
+import functools
+
 import torch
 
 from . import binding as lsr
@@ -23,12 +26,29 @@ def _kind(t: torch.Tensor, who: str, what: str) -> int:
 
 
 def _on_gpu(who: str, *tensors) -> None:
-    """All on the current device, whose stream the work goes to."""
+    """All on one GPU."""
+    dev = -1
     for t in tensors:
-        if t is not None and not t.is_cuda:
-            raise RuntimeError(f"{who}: all tensors must live on the GPU; there is no CPU path")
-    if len({t.device for t in tensors if t is not None}) > 1:
-        raise RuntimeError(f"{who}: all tensors must live on one GPU")
+        if t is not None:
+            at = t.get_device()
+            if at < 0:
+                raise RuntimeError(f"{who}: all tensors must live on the GPU; there is no CPU path")
+            if dev not in (-1, at):
+                raise RuntimeError(f"{who}: all tensors must live on one GPU")
+            dev = at
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _on(device):
+    """With the tensors' device current, whose stream the work goes to."""
+    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+@functools.lru_cache(maxsize=256)
+def _distill_bytes(shape: tuple, backward: bool) -> int:
+    return lsr.lsr_distill_workspace_bytes(*shape, backward)
 
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
@@ -59,7 +79,7 @@ def quantize_rows(X: torch.Tensor):
     scale = torch.empty((rows,), dtype=torch.float32, device=X.device)
     if rows:
         X = _rows(X.detach())
-        with torch.cuda.device(X.device):
+        with _on(X.device):
             lsr.lsr_quantize_rows(rows, cols, kind, X, _ld(X), Q, pitch, scale)
     return Q, scale
 
@@ -78,7 +98,7 @@ def top_logits(X: torch.Tensor, K: int, temperature: float = 1.0):
     lse = torch.empty((rows,), dtype=torch.float32, device=X.device)
     if rows:
         X = _rows(X.detach())
-        with torch.cuda.device(X.device):
+        with _on(X.device):
             ws = _scratch(lsr.lsr_top_logits_workspace_bytes(rows, V, K), X.device)
             lsr.lsr_top_logits(rows, V, K, kind, temperature, X, _ld(X), values, ids, lse, ws)
     return values, ids, lse
@@ -111,7 +131,7 @@ class Int8Head:
         out = torch.empty((N, self.V), dtype=dtype, device=H.device)
         if N:
             A = _rows(A)
-            with torch.cuda.device(H.device):
+            with _on(H.device):
                 ws = _scratch(lsr.lsr_int8_matmul_workspace_bytes(N, self.V, self.D, kind), H.device)
                 lsr.lsr_int8_matmul(N, self.V, self.D, kind, _KIND[dtype], A, _ld(A), None, self.W8, self.W8.stride(0), self.w_scale, self.bias,
                                     out, self.V, ws)
@@ -143,30 +163,29 @@ class _LsrDistill(torch.autograd.Function):
         if (teacher_lse is not None and teacher_lse.shape != lead) or (mask is not None and mask.shape != lead):
             raise ValueError("lsr_distill: teacher_lse and mask must have one value for each row of H")
         dt = _KIND[H.dtype]
-        H2, W = _aligned(H.reshape(-1, D)), _aligned(W)
-        b32 = _aligned(bias.float())
+        H2, W, b32 = _aligned(_as(H, (-1, D))), _aligned(W), _aligned(bias.float())
         if ids.dtype == torch.int64:
             # an id that 32 bits do not hold is padding like any other outside the vocabulary
             ids = torch.where((ids >= 0) & (ids < V), ids, -1).to(torch.int32)
-        ids, logits = _aligned(ids.reshape(-1, K)), _aligned(logits.float().reshape(-1, K))
+        ids, logits = _aligned(_as(ids, (-1, K))), _aligned(_as(logits.float(), (-1, K)))
         if teacher_lse is not None:
-            teacher_lse = _aligned(teacher_lse.float().reshape(-1))
+            teacher_lse = _aligned(_as(teacher_lse.float(), (-1,)))
         if mask is not None:
             # the library takes any non-zero byte for a row that counts
             if mask.dtype not in (torch.bool, torch.uint8):
                 mask = mask != 0
-            mask = _aligned(mask.reshape(-1)).view(torch.uint8)
+            mask = _aligned(_as(mask, (-1,))).view(torch.uint8)
         N = H2.shape[0]
         loss = torch.empty((N,), dtype=torch.float32, device=H.device)
         lse = torch.empty((N,), dtype=torch.float32, device=H.device)
         ctx.shape = (N, D, V, K, dt, float(temperature))
         if N:
-            with torch.cuda.device(H.device):
-                ws = _scratch(lsr.lsr_distill_workspace_bytes(*ctx.shape, False), H.device)
+            with _on(H.device):
+                ws = _scratch(_distill_bytes(ctx.shape, False), H.device)
                 lsr.lsr_distill_forward(*ctx.shape, H2, W, b32, ids, logits, teacher_lse, mask, loss, lse, ws)
         ctx.save_for_backward(H2, W, b32, ids, logits, teacher_lse, mask, lse)
         ctx.lead, ctx.bias_dtype = lead, bias.dtype
-        loss, lse_out = loss.reshape(lead), lse.reshape(lead)
+        loss, lse_out = _as(loss, lead), _as(lse, lead)
         ctx.mark_non_differentiable(lse_out)
         ctx.set_materialize_grads(False)
         return loss, lse_out
@@ -185,13 +204,17 @@ class _LsrDistill(torch.autograd.Function):
                 if g is not None:
                     g.zero_()
         elif need_h or need_w or need_b:
-            dloss = _aligned(dloss.float().reshape(-1))
-            with torch.cuda.device(dev):
-                ws = _scratch(lsr.lsr_distill_workspace_bytes(*ctx.shape, True), dev)
+            dloss = _aligned(_as(dloss.float(), (-1,)))
+            with _on(dev):
+                ws = _scratch(_distill_bytes(ctx.shape, True), dev)
                 lsr.lsr_distill_backward(*ctx.shape, H, W, bias, ids, logits, teacher_lse, mask, lse, dloss, dH, dW, db, ws)
         if dH is not None:
-            dH = dH.reshape(*ctx.lead, D)
-        return dH, dW, None if db is None else db.to(ctx.bias_dtype), None, None, None, None, None
+            dH = _as(dH, (*ctx.lead, D))
+        return dH, dW, db if db is None or ctx.bias_dtype == torch.float32 else db.to(ctx.bias_dtype), None, None, None, None, None
+
+
+def _as(t: torch.Tensor, shape: tuple) -> torch.Tensor:
+    return t if t.dim() == len(shape) else t.reshape(shape)
 
 
 def _aligned(t: torch.Tensor) -> torch.Tensor:
