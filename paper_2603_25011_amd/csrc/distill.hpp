@@ -325,8 +325,8 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsPar
     if (t.tid < TP_T) s_bias[t.tid] = v0 + t.tid < p.V ? p.bias[v0 + t.tid] : -INFINITY;
 
     floatx16 acc[4][2];
-    tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, row_operand(p.W, p.w_pitch, p.w_plane, v0, p.V),
-                                row_operand(p.Hc, p.h_pitch, p.h_plane, i0, n), p.slabs, acc);
+    tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, row_operand(p.W, p.w_pitch, p.w_plane, v0, p.V), p.V - v0,
+                                row_operand(p.Hc, p.h_pitch, p.h_plane, i0, n), n - i0, p.slabs, acc);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -567,29 +567,39 @@ struct GradsParams {
     int ga;
 };
 
-// (what is added to is read 16 values at a time: a load behind each store would wait for it)
+// Stores a tile whose rows run along D and whose columns are rows of the result (of which `rows` exist, `cols` of D): a lane holds four neighbouring elements of a row,
+// in bfloat16 the half-waves trade groups of four first, so every store is 16 bytes.  (With the result's rows along the tile's rows, 2- and 4-byte stores
+// and 128 of them, a unit of 2 slabs took 20 us.)  D is a multiple of 8.
 template <typename OT>
 __device__ __forceinline__ void store_tile(const TileLane& t, const floatx16 (&acc)[4][2], OT* out, size_t pitch, int rows, int cols, bool add) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-        const int col = t.col(c);
-        if (col < cols) {
+        if (t.col(c) >= rows) continue;
+        OT* const o = out + (size_t)t.col(c) * pitch;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                OT* o[16];
+        for (int i = 0; i < 4; ++i) {
+            const int d0 = (2 * i + t.wm) * 32;
+            if constexpr (sizeof(OT) == 4) {
+                float4 x[4];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[r] = out + (size_t)min(t.row(i, r), rows - 1) * pitch + col;
-                float x[16];
-                if (sizeof(OT) == 4 && add) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) x[r] = acc[i][c][r] + *reinterpret_cast<const float*>(o[r]);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) x[r] = acc[i][c][r];
+                for (int g = 0; g < 4; ++g) {
+                    x[g] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (add && d0 + 8 * g < cols) x[g] = *reinterpret_cast<const float4*>(o + d0 + 8 * g + 4 * t.half);
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (t.row(i, r) < rows) *o[r] = as_type<OT>(x[r]);
+                for (int g = 0; g < 4; ++g)
+                    if (d0 + 8 * g < cols)
+                        *reinterpret_cast<float4*>(o + d0 + 8 * g + 4 * t.half) = make_float4(x[g].x + acc[i][c][4 * g], x[g].y + acc[i][c][4 * g + 1],
+                                                                                              x[g].z + acc[i][c][4 * g + 2], x[g].w + acc[i][c][4 * g + 3]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const float* const a = reinterpret_cast<const float*>(&acc[i][c]) + 8 * q;
+                    const auto lo = __builtin_amdgcn_permlane32_swap(bf16_bits(a[0]) | (uint32_t)bf16_bits(a[1]) << 16, bf16_bits(a[4]) | (uint32_t)bf16_bits(a[5]) << 16, false, false);
+                    const auto hi = __builtin_amdgcn_permlane32_swap(bf16_bits(a[2]) | (uint32_t)bf16_bits(a[3]) << 16, bf16_bits(a[6]) | (uint32_t)bf16_bits(a[7]) << 16, false, false);
+                    const int d = d0 + 8 * (2 * q + t.half);
+                    if (d < cols) *reinterpret_cast<uint4*>(o + d) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+                }
             }
         }
     }
@@ -616,8 +626,8 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_grads_kernel(GradsParam
     int at, bt;
     if (u < w_units) {
         tile_of_unit(u, nvt, p.nd, p.ga, at, bt);
-        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, block_operand(p.Gt, p.gt_plane, at, p.t_slabs, 0), block_operand(p.Ht, p.ht_plane, bt, p.t_slabs, 0),
-                                    (n + 63) / 64, acc);
+        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, block_operand(p.Ht, p.ht_plane, bt, p.t_slabs, 0), p.D - bt * TP_T,
+                                    block_operand(p.Gt, p.gt_plane, at, p.t_slabs, 0), p.nv - at * TP_T, (n + 63) / 64, acc);
         store_tile(t, acc, reinterpret_cast<OT*>(p.dW) + (size_t)at * TP_T * p.D + bt * TP_T, p.D, p.nv - at * TP_T, p.D - bt * TP_T, false);
     } else {
         u -= w_units;
@@ -625,8 +635,8 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_grads_kernel(GradsParam
         tile_of_unit(u - s * h_units, ntt, p.nd, p.ga, at, bt);
         const int slabs = (p.nv + 63) / 64;
         const int k0 = (int)((long long)slabs * s / p.splits), k1 = (int)((long long)slabs * (s + 1) / p.splits);
-        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, block_operand(p.G, p.g_plane, at, p.v_slabs, k0), block_operand(p.Wt, p.wt_plane, bt, p.v_slabs, k0),
-                                    k1 - k0, acc);
+        tile_product<bf16x8, SPLIT>(s_ring0, s_ring1, block_operand(p.Wt, p.wt_plane, bt, p.v_slabs, k0), p.D - bt * TP_T,
+                                    block_operand(p.G, p.g_plane, at, p.v_slabs, k0), n - at * TP_T, k1 - k0, acc);
         store_tile(t, acc, p.dh_part + s * p.dh_plane + (size_t)at * TP_T * p.D + bt * TP_T, p.D, n - at * TP_T, p.D - bt * TP_T, p.accumulate != 0);
     }
 }

@@ -321,7 +321,6 @@ __global__ __launch_bounds__(FEWD_THREADS) void distill_few_dh_kernel(FewDistill
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
     const T* const W = reinterpret_cast<const T*>(p.W) + d;
-#pragma unroll 2
     for (int tile = t0; tile < t1; ++tile) {
         const int v0 = tile * 32 + 4 * half;
         if constexpr (sizeof(T) == 2) {

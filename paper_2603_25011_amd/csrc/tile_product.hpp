@@ -62,7 +62,7 @@ struct TileLane {
     int tid, lane, wave, wm, wn, half, l32;
     __device__ __forceinline__ TileLane() {
         tid = threadIdx.x; lane = tid & 63; wave = tid >> 6;
-        wm = wave >> 2; wn = wave & 3; half = lane >> 5; l32 = lane & 31;
+        wm = wave & 1; wn = wave >> 1; half = lane >> 5; l32 = lane & 31;      // (waves w and w + 4 share a SIMD: one of either half of the columns)
     }
     __device__ __forceinline__ int row(int i, int r) const { return acc_row(2 * i + wm, r, half); }
     __device__ __forceinline__ int col(int c) const { return wn * 64 + c * 32 + l32; }
@@ -75,9 +75,10 @@ __device__ __forceinline__ const char* uniform(const char* p) {
     return reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
 }
 
-// acc = A B^T over nkp slabs (per plane).  Pitches below 2^23.  On return every wave is past its LDS reads only after the caller's next barrier.
+// acc = A B^T over nkp slabs (per plane).  Of the tile, `rows` rows and `cols` columns exist: 32-row blocks and 64-column parts that do not are not multiplied (their
+// accumulators are 0).  Pitches below 2^23.  On return every wave is past its LDS reads only after the caller's next barrier.
 template <typename Frag, bool SPLIT>
-__device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, const TileOperand& A, const TileOperand& B, int nkp,
+__device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, const TileOperand& A, int rows, const TileOperand& B, int cols, int nkp,
                                              typename TileAcc<Frag>::type (&acc)[4][2]) {
     constexpr int KS = TP_RB / 32, LPT = 8, SPREAD = 2, CPR = TP_RB / 16, RPI = 64 / CPR, NW = 8;
     const TileLane t;
@@ -120,31 +121,48 @@ __device__ __forceinline__ void tile_product(uint8_t* ring0, uint8_t* ring1, con
 #pragma unroll
         for (int n = 0; n < LPT; ++n) issue_one(ring0, Ab + ka, Bb + kb, n);
     }
-    Frag fa[2][4], fb[2][2];
-    auto step = [&](uint8_t* st, uint8_t* other, auto mode_c, int kt) {
-        // every fragment read of the slab before has returned, and slab kt has landed
-        __builtin_amdgcn_s_waitcnt(0xC07F);     // lgkmcnt(0)
-        wait_vmcnt<0>();
-        __syncthreads();
-        const int more = __builtin_amdgcn_readfirstlane(kt + 1 < nk ? 1 : 0);
-        size_t ka, kb;
-        slab_at(SPLIT, kt + 1, nkp, A, B, ka, kb);
-        const char* ab = Ab + ka;
-        const char* bb = Bb + kb;
-        auto dma = [&](int n) {
-            if (more != 0) issue_one(other, ab, bb, n);
+    // The whole walk is instantiated once per count of live row blocks, so that each instance is straight-line MFMA code.
+    auto walk = [&](auto na_c) {
+        constexpr int NA = decltype(na_c)::value;
+        Frag fa[2][4], fb[2][2];
+        auto step = [&](uint8_t* st, uint8_t* other, auto mode_c, int kt) {
+            // every fragment read of the slab before has returned, and slab kt has landed
+            __builtin_amdgcn_s_waitcnt(0xC07F);     // lgkmcnt(0)
+            wait_vmcnt<0>();
+            __syncthreads();
+            const int more = __builtin_amdgcn_readfirstlane(kt + 1 < nk ? 1 : 0);
+            size_t ka, kb;
+            slab_at(SPLIT, kt + 1, nkp, A, B, ka, kb);
+            const char* ab = Ab + ka;
+            const char* bb = Bb + kb;
+            auto dma = [&](int n) {
+                if (more != 0) issue_one(other, ab, bb, n);
+            };
+            if constexpr (NA == 0) {                // nothing to multiply: only the loads
+#pragma unroll
+                for (int n = 0; n < LPT; ++n) dma(n);
+            } else {
+                mma_rot<NA, KS, decltype(mode_c)::value, LPT, SPREAD>(st + fa_row * TP_RB, 64 * TP_RB, st + TP_SLAB + fb_row * TP_RB, 32 * TP_RB, fsw, fa, fb,
+                                                                      acc, dma);
+            }
         };
-        mma_rot<4, KS, decltype(mode_c)::value, LPT, SPREAD>(st + fa_row * TP_RB, 64 * TP_RB, st + TP_SLAB + fb_row * TP_RB, 32 * TP_RB,
-                                                             fsw, fa, fb, acc, dma);
+        constexpr std::integral_constant<int, 0> first{};
+        constexpr std::integral_constant<int, 1> steady{};
+        step(ring0, ring1, first, 0);
+        for (int kt = 1; kt < nk; kt += 2) {
+            step(ring1, ring0, steady, kt);
+            if (kt + 1 < nk) step(ring0, ring1, steady, kt + 1);
+        }
+        if constexpr (NA > 0) mma_rot<NA, KS, 2, LPT, SPREAD>(ring0, 0, ring0, 0, fsw, fa, fb, acc, [](int) {});
     };
-    constexpr std::integral_constant<int, 0> first{};
-    constexpr std::integral_constant<int, 1> steady{};
-    step(ring0, ring1, first, 0);
-    for (int kt = 1; kt < nk; kt += 2) {
-        step(ring1, ring0, steady, kt);
-        if (kt + 1 < nk) step(ring0, ring1, steady, kt + 1);
+    const int na = __builtin_amdgcn_readfirstlane(t.wn * 64 < cols ? ((min(rows, TP_T) + 31) / 32 + 1 - t.wm) >> 1 : 0);
+    switch (na) {
+        case 4: walk(std::integral_constant<int, 4>{}); break;
+        case 3: walk(std::integral_constant<int, 3>{}); break;
+        case 2: walk(std::integral_constant<int, 2>{}); break;
+        case 1: walk(std::integral_constant<int, 1>{}); break;
+        default: walk(std::integral_constant<int, 0>{}); break;
     }
-    mma_rot<4, KS, 2, LPT, SPREAD>(ring0, 0, ring0, 0, fsw, fa, fb, acc, [](int) {});
 }
 
 // ---- the narrow tile: 256 rows of A by 128 of B, 4 waves (2 x 2 of the same 128 x 64 part), so that two workgroups share a CU and one's epilogue runs
@@ -206,6 +224,8 @@ __device__ __forceinline__ void narrow_product(uint8_t* ring, const TileOperand&
     int fsw[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) fsw[ks] = ((ks * 2 + t.half) ^ lds_swz<NT_RB>(t.l32)) << 4;
+    // From here to the last slab only direct-to-LDS loads are in flight: they retire in the order of issue, which the partial waits below count on.
+    wait_vmcnt<0>();
     issue(0, 0);
     issue(1, 1);
     Frag fa[2][4], fb[2][2];

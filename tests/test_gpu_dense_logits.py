@@ -371,6 +371,48 @@ def test_distill_large_logits(dtype):
     run_and_check(distill_case(60, 64, 900, 8, dtype, 11, spread=3.0))
 
 
+# up to 64 rows whose hidden states fit LDS take a path of their own; 64 x 1024 in bfloat16 and 40 x 1024 in float32 do not fit it
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,D,V,K", [(2, 1024, 31, 3), (31, 40, 33, 9), (32, 264, 1025, 64), (33, 24, 640, 200), (40, 1024, 515, 8), (63, 520, 129, 2), (64, 1024, 700, 17),
+                                     (65, 64, 300, 5), (7, 8192, 300, 4)])
+def test_distill_few_rows(N, D, V, K, dtype):
+    run_and_check(distill_case(N, D, V, K, dtype, N + D + V, keep=0.7, given=N % 2 == 0, T=[1.0, 2.0][N % 2]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [20, 50])
+def test_distill_few_rows_masks_padding_and_excluded_entries(N, dtype):
+    H, W, bias, ids, logits, L, mask, T, dloss = distill_case(N, 96, 600, 9, dtype, 21, keep=0.8)
+    gone = np.zeros(600, bool)
+    gone[[0, 255, 256, 599]] = True
+    gone[300:360] = True
+    bias = torch.where(torch.from_numpy(gone), -math.inf, bias.double()).float()
+    ids = np.where(gone[ids], -1, ids).astype(np.int32)
+    mask[:3], mask[-2:] = 0, 0
+    ids[4, 2:] = -1
+    ids[5], logits[6], ids[7, 1] = -1, -np.inf, 600
+    ids[8, 1] = ids[8, 0]
+    mask[4:9] = 9
+    for given in (L, None):
+        got = run_and_check((H, W, bias, ids, logits, given, mask, T, dloss))
+        assert not got["dH"][dev(mask == 0)].any() and not got["dH"][5:7].any()
+        assert not got["dW"][dev(gone)].any() and not got["db"][dev(gone)].any()
+    got = run_and_check((H, W, bias, ids, logits, L, np.zeros(N, np.uint8), T, dloss))
+    assert not any(got[k].any() for k in got)
+
+
+@pytest.mark.parametrize("need", [(True, False, False), (False, True, False), (False, False, True), (False, False, False)])
+def test_distill_few_rows_gradients_that_are_wanted_only(need):
+    run_and_check(distill_case(33, 72, 520, 5, "bf16", 22, keep=0.7), need)
+
+
+def test_distill_few_rows_crowded_tile():
+    case = list(distill_case(48, 64, 2000, 200, "bf16", 23))
+    rng = np.random.default_rng(24)
+    case[3] = np.stack([512 + rng.permutation(256)[:200] for _ in range(48)]).astype(np.int32)
+    run_and_check(tuple(case))
+
+
 def test_distill_in_pieces_of_the_vocabulary():
     # so many rows that the backward walks the vocabulary in pieces
     N, D, V, K = 262144, 64, 3000, 2
