@@ -15,7 +15,7 @@ namespace lsr {
 //   distill_few_dh_kernel      dH = g W, W read by columns: a wave owns 32 columns of D and a part of the vocabulary
 // Float32 is multiplied in float32 (the time is that of the reads).  bfloat16 gradients take g as two bfloat16 whose sum has 16 bits: with few rows, single entries
 // make up whole sums, and the one rounding that many rows average out would show.
-// N = 20, 768 x 30522: step 264 us in plain operations, 203 in tiles, MEASURED here.
+// 20 x 1024 x 250002: forward 114 us and step 620 us in bfloat16 (4.5 and 3.3 TB/s), 300 and 1170 us in float32.
 constexpr int FEWD_THREADS = 256;
 constexpr int FEWD_ROWS = 64;
 constexpr int FEWD_U = 8;

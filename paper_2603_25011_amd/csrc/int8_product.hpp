@@ -115,18 +115,17 @@ __global__ __launch_bounds__(NT_THREADS, 2) void int8_tile_kernel(Int8Params p) 
 // workgroup from the values (the first loads of W are in flight meanwhile), so the call is one launch.
 constexpr int FEW8_THREADS = 256;
 constexpr int FEW8_COLS = 32 * FEW8_THREADS / 64;
-constexpr int FEW8_ROWS = 64;
-constexpr int FEW8_OWN = 16;
+constexpr int FEW8_ROWS = 32;                     // one block of the MFMA
+constexpr int FEW8_OWN = 8;
 constexpr int FEW8_U = 12;
-constexpr int FEW8_LDS = 156 * 1024;              // of the rows of A at most; up to FEW8_LDS_TWO two workgroups share a CU
-constexpr int FEW8_LDS_TWO = 76 * 1024;
+constexpr int FEW8_LDS = 76 * 1024;               // of the rows of A: two workgroups share a CU
 // LDS bytes of a row: padded so that the 32 rows of a fragment read lie on different banks
 inline int few8_stride(int row_bytes) { return row_bytes + 16; }
 
-template <typename T, typename OT, bool VEC, int NB, bool TWO>
-__global__ __launch_bounds__(FEW8_THREADS, TWO ? 2 : 1) void int8_few_kernel(Int8Params p, int stride, int n_tiles) {
-    __shared__ __attribute__((aligned(16))) uint8_t s_a[TWO ? FEW8_LDS_TWO : FEW8_LDS];       // [N][stride]
-    __shared__ float s_scale[32 * NB];
+template <typename T, typename OT, bool VEC>
+__global__ __launch_bounds__(FEW8_THREADS, 2) void int8_few_kernel(Int8Params p, int stride, int n_tiles) {
+    __shared__ __attribute__((aligned(16))) uint8_t s_a[FEW8_LDS];       // [N][stride]
+    __shared__ float s_scale[FEW8_ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
     const int nks = p.row_bytes / 32;
     int tile = blockIdx.x;
@@ -180,49 +179,36 @@ __global__ __launch_bounds__(FEW8_THREADS, TWO ? 2 : 1) void int8_few_kernel(Int
     }
     __syncthreads();
     OT* const out = reinterpret_cast<OT*>(p.out);
-    {
-        const uint8_t* sa[NB];
+    const uint8_t* const sa = s_a + min(l32, p.N - 1) * stride + half * 16;
+    for (; tile < n_tiles; tile += gridDim.x) {
+        const int vc = min(v, p.V - 1);
+        const float ws = p.w_scale[vc];
+        const float bs = p.bias ? p.bias[vc] : 0.f;
+        intx16 acc;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) sa[i] = s_a + min(i * 32 + l32, p.N - 1) * stride + half * 16;
-        for (; tile < n_tiles; tile += gridDim.x) {
-            const int vc = min(v, p.V - 1);
-            const float ws = p.w_scale[vc];
-            const float bs = p.bias ? p.bias[vc] : 0.f;
-            intx16 acc[NB];
+        for (int r = 0; r < 16; ++r) acc[r] = 0;
+        auto multiply = [&](const intx4 (&w)[FEW8_U], int k0) {
 #pragma unroll
-            for (int i = 0; i < NB; ++i)
+            for (int u = 0; u < FEW8_U; ++u)
+                if (k0 + u < nks) acc = mma_chunk(*reinterpret_cast<const intx4*>(sa + (k0 + u) * 32), w[u], acc);
+        };
+        for (int k0 = 0; k0 < nks; k0 += 2 * FEW8_U) {
+            if (k0 + FEW8_U < nks) load_w(w1, k0 + FEW8_U);
+            multiply(w0, k0);
+            if (k0 + 2 * FEW8_U < nks) load_w(w0, k0 + 2 * FEW8_U);
+            if (k0 + FEW8_U < nks) multiply(w1, k0 + FEW8_U);
+        }
+        const int v_here = v;
+        if (tile + (int)gridDim.x < n_tiles) {           // the next tile's first fragments fly while this one is stored
+            v += (int)gridDim.x * FEW8_COLS;
+            wrow = p.W + (int64_t)min(v, p.V - 1) * p.ldw + half * 16;
+            load_w(w0, 0);
+        }
+        if (v_here < p.V) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][r] = 0;
-            auto multiply = [&](const intx4 (&w)[FEW8_U], int k0) {
-#pragma unroll
-                for (int u = 0; u < FEW8_U; ++u) {
-                    if (k0 + u < nks) {
-#pragma unroll
-                        for (int i = 0; i < NB; ++i)
-                            acc[i] = mma_chunk(*reinterpret_cast<const intx4*>(sa[i] + (k0 + u) * 32), w[u], acc[i]);
-                    }
-                }
-            };
-            for (int k0 = 0; k0 < nks; k0 += 2 * FEW8_U) {
-                if (k0 + FEW8_U < nks) load_w(w1, k0 + FEW8_U);
-                multiply(w0, k0);
-                if (k0 + 2 * FEW8_U < nks) load_w(w0, k0 + 2 * FEW8_U);
-                if (k0 + FEW8_U < nks) multiply(w1, k0 + FEW8_U);
-            }
-            const int v_here = v;
-            if (tile + (int)gridDim.x < n_tiles) {       // the next tile's first fragments fly while this one is stored
-                v += (int)gridDim.x * FEW8_COLS;
-                wrow = p.W + (int64_t)min(v, p.V - 1) * p.ldw + half * 16;
-                load_w(w0, 0);
-            }
-            if (v_here < p.V) {
-#pragma unroll
-                for (int i = 0; i < NB; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int n = acc_row(i, r, half);
-                        if (n < p.N) out[(int64_t)n * p.ldo + v_here] = as_type<OT>(fmaf((float)acc[i][r], s_scale[n] * ws, bs));
-                    }
+            for (int r = 0; r < 16; ++r) {
+                const int n = acc_row(0, r, half);
+                if (n < p.N) out[(int64_t)n * p.ldo + v_here] = as_type<OT>(fmaf((float)acc[r], s_scale[n] * ws, bs));
             }
         }
     }

@@ -39,11 +39,11 @@ void quantize(int32_t type, const void* X, int64_t ldx, int64_t rows, int cols, 
     else launch_quantize<uint16_t>(X, ldx, rows, cols, Q, ldq, scale, st);
 }
 
-// Few rows: their quantised form fits the LDS of the kernel that reads W straight into registers.  Against tiles of 256 x 256 (us): 64 rows, 384 x 30522
-// 10.6 / 16, 1024 x 250002 82 / 100.  (With 96 or 128 rows its accumulators leave one workgroup per CU: 384 x 30522 15.3 / 16.5 and 18.2 / 17,
-// 1024 x 250002 142 / 105 and 168 / 114; not kept.)
-bool int8_few(int64_t N, int64_t K) {
-    return N <= FEW8_ROWS && N * few8_stride((int)up(K, 128)) <= (N <= 32 ? FEW8_LDS_TWO : FEW8_LDS);
+// Few rows, whose quantised form fits the LDS of the kernel that reads W straight into registers.  Against narrow tiles (us, 8-bit rows): 768 x 30522 1 row
+// 6.6 / 10.1, 32 rows 9.0 / 10.3, 64 rows (two blocks) 14 / 11; 768 x 100000 16 rows 19.4 / 19.8, 32 rows 21.8 / 20.4; 1024 x 250002 1 row 40.6 / 43.0, 16 rows 47 / 45.6,
+// 32 rows 55 / 48.
+bool int8_few(int64_t N, int64_t V, int64_t K) {
+    return N <= (V <= 65536 ? FEW8_ROWS : FEW8_ROWS / 2) && N * few8_stride((int)up(K, 128)) <= FEW8_LDS;
 }
 
 struct Int8Ws { size_t q, scale, total; };
@@ -57,16 +57,9 @@ Int8Ws int8_ws(int64_t N, int64_t K) {
 
 template <typename T, typename OT, bool VEC>
 void launch_int8_few(const Int8Params& p, int n_cus, hipStream_t st) {
-    const int stride = few8_stride(p.row_bytes);
     const int n_tiles = (p.V + FEW8_COLS - 1) / FEW8_COLS;
-    const bool two = p.N * stride <= FEW8_LDS_TWO;
-    const int resident = two ? 2 * n_cus : n_cus;
-    const unsigned grid = (unsigned)(n_tiles < resident ? n_tiles : resident);
-    if (p.N <= 32) int8_few_kernel<T, OT, VEC, 1, true><<<grid, FEW8_THREADS, 0, st>>>(p, stride, n_tiles);
-    else if constexpr (sizeof(T) == 1) {
-        if (two) int8_few_kernel<T, OT, VEC, 2, true><<<grid, FEW8_THREADS, 0, st>>>(p, stride, n_tiles);
-        else int8_few_kernel<T, OT, VEC, 2, false><<<grid, FEW8_THREADS, 0, st>>>(p, stride, n_tiles);
-    }
+    const unsigned grid = (unsigned)(n_tiles < 2 * n_cus ? n_tiles : 2 * n_cus);
+    int8_few_kernel<T, OT, VEC><<<grid, FEW8_THREADS, 0, st>>>(p, few8_stride(p.row_bytes), n_tiles);
 }
 template <typename OT>
 void int8_few_of_type(const Int8Params& p, int32_t a_type, int n_cus, hipStream_t st) {
@@ -473,7 +466,7 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
     p.lda = lda; p.ldw = ldw; p.ldo = ldo;
     p.N = (int)N; p.V = (int)V; p.K = (int)K; p.row_bytes = (int)row_bytes;
     p.na = (int)na; p.nb = (int)nb; p.ga = 8;
-    const bool few = int8_few(N, K);
+    const bool few = int8_few(N, V, K);
     if (a_dtype != LSR_I8 && !(few && N <= FEW8_OWN)) {
         int8_t* const q = static_cast<int8_t*>(workspace) + w.q;
         float* const scale = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.scale);
