@@ -38,7 +38,7 @@ int64_t lsr_int8_row_bytes(int64_t cols);
  *   Q     [rows, ldq] int8, ldq a multiple of 16 and at least lsr_int8_row_bytes(cols); the bytes behind cols are
  *         set to zero up to lsr_int8_row_bytes(cols), and not touched behind that
  *   scale [rows] f32 (4-byte aligned)
- * Limits: 1 <= rows < 2^31, 1 <= cols <= 65536.
+ * Limits: 1 <= rows < 2^26, 1 <= cols <= 65536.
  */
 int lsr_quantize_rows(int64_t rows, int64_t cols, int32_t x_dtype, const void* X, int64_t ldx,
                       int8_t* Q, int64_t ldq, float* scale, lsr_stream_t stream);
@@ -54,7 +54,8 @@ int lsr_quantize_rows(int64_t rows, int64_t cols, int32_t x_dtype, const void* X
  *   bias      [V] f32, or NULL for none
  *   out       [N, ldo] out_dtype (LSR_F32 or LSR_BF16), any alignment of its elements, ldo >= V
  *   workspace lsr_int8_matmul_workspace_bytes (0 for LSR_I8: then it may be NULL; 0 also for an invalid shape)
- * Scales and bias are 4-byte aligned.  Limits: 1 <= N, V < 2^31 - 4096, 1 <= K <= 65536, ldw and the lda of int8 rows at most 2^23.
+ * Scales and bias are 4-byte aligned.  Limits: 1 <= N < 2^26, 1 <= V < 2^31 - 4096, N V < 2^38, 1 <= K <= 65536,
+ * ldw and the lda of int8 rows at most 2^23.
  */
 size_t lsr_int8_matmul_workspace_bytes(int64_t N, int64_t V, int64_t K, int32_t a_dtype);
 
@@ -71,7 +72,7 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
  *   values  [rows, K] f32, ids [rows, K] int32, lse [rows] f32 or NULL (all 4-byte aligned)
  * Logits of -inf are ordinary values (they come last, and add nothing to lse; a row of them has lse = -inf).
  * -0 and +0 are equal.  NaN comes before +inf and makes lse NaN.
- * Limits: 1 <= rows < 2^31, 1 <= K <= min(V, 256), V < 2^31 - 4096, temperature > 0 and finite.
+ * Limits: 1 <= rows < 2^23, 1 <= K <= min(V, 256), V < 2^31 - 4096, temperature > 0 and finite.
  */
 size_t lsr_top_logits_workspace_bytes(int64_t rows, int64_t V, int64_t K);
 
@@ -93,7 +94,8 @@ int lsr_top_logits(int64_t rows, int64_t V, int64_t K, int32_t x_dtype, float te
  * bias[v] = -inf excludes an entry (a teacher's probability on it makes the loss infinite); everything else is finite.
  *
  * N counts tokens (B * S of the head), D is the hidden size, V the vocabulary, K the teacher's entries per token.
- * Limits: 1 <= N <= 2^22; D a multiple of 8, 8 <= D <= 8192; 1 <= V <= 2^21; 1 <= K <= 256; temperature > 0, finite.
+ * Limits: 1 <= N <= 2^22; D a multiple of 8, 8 <= D <= 8192; 1 <= V <= 2^21; N V < 2^38; N D < 2^33;
+ * 1 <= K <= 256; temperature > 0, finite.
  *   H [N,D], W [V,D] hw_dtype;  bias [V] f32;  teacher_ids [N,K] int32;  teacher_logits [N,K] f32;
  *   teacher_lse [N] f32 or NULL;  mask [N] uint8 or NULL (no row left out);  loss [N], lse [N] f32.
  * LSR_BF16 multiplies in bfloat16 with float32 sums; LSR_F32 to the precision of float32.

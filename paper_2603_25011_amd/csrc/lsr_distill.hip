@@ -18,6 +18,11 @@ using namespace lsr;
 
 constexpr int64_t INT8_MAX_K = 65536;
 constexpr int64_t MAX_INDEX = (int64_t(1) << 31) - 4096;
+// A launch stays below 2^32 threads: 64 per row quantised; 256 per segment of a row of logits; 512 per 256 x 256 tile (or two of 256 x 128); one per four elements of dH.
+constexpr int64_t MAX_QUANT_ROWS = int64_t(1) << 26;
+constexpr int64_t MAX_TOP_ROWS = int64_t(1) << 23;
+constexpr int64_t MAX_LOGITS = int64_t(1) << 38;
+constexpr int64_t MAX_STATES = int64_t(1) << 33;
 
 inline bool float_type(int32_t t) { return t == LSR_F32 || t == LSR_BF16; }
 inline size_t type_bytes(int32_t t) { return t == LSR_F32 ? 4 : t == LSR_BF16 ? 2 : 1; }
@@ -102,8 +107,7 @@ TopWs top_ws(int64_t rows, const TopPlan& p, int64_t K) {
     return w;
 }
 bool top_shape(int64_t rows, int64_t V, int64_t K) {
-    return rows >= 1 && rows < (int64_t(1) << 31) && V >= 1 && V < MAX_INDEX && K >= 1 && K <= V && K <= TOP_MAX_K &&
-           rows * top_plan(rows, V, K).splits < (int64_t(1) << 31);
+    return rows >= 1 && rows < MAX_TOP_ROWS && V >= 1 && V < MAX_INDEX && K >= 1 && K <= V && K <= TOP_MAX_K;
 }
 
 // ---- distillation ----
@@ -122,6 +126,7 @@ int check_distill(const lsr_distill_desc* d, DShape* s) {
     if (!float_type(d->hw_dtype)) return LSR_ERR_DTYPE;
     if (d->N < 1 || d->N > (int64_t(1) << 22) || d->D < 8 || d->D > 8192 || d->D % 8 != 0) return LSR_ERR_SHAPE;
     if (d->V < 1 || d->V > (int64_t(1) << 21) || d->K < 1 || d->K > TOP_MAX_K) return LSR_ERR_SHAPE;
+    if (d->N * d->V >= MAX_LOGITS || d->N * d->D >= MAX_STATES) return LSR_ERR_SHAPE;
     if (!(d->temperature > 0.f) || !isfinite(d->temperature) || !isfinite(1.f / d->temperature)) return LSR_ERR_SHAPE;
     s->N = (int)d->N; s->D = (int)d->D; s->V = (int)d->V; s->K = (int)d->K; s->dtype = d->hw_dtype;
     s->planes = s->dtype == LSR_F32 ? 3 : 1;
@@ -422,7 +427,7 @@ int64_t lsr_int8_row_bytes(int64_t cols) { return cols < 1 || cols > INT8_MAX_K 
 int lsr_quantize_rows(int64_t rows, int64_t cols, int32_t x_dtype, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, float* scale,
                       lsr_stream_t stream) {
     if (!float_type(x_dtype)) return LSR_ERR_DTYPE;
-    if (rows < 1 || rows >= (int64_t(1) << 31) || cols < 1 || cols > INT8_MAX_K) return LSR_ERR_SHAPE;
+    if (rows < 1 || rows >= MAX_QUANT_ROWS || cols < 1 || cols > INT8_MAX_K) return LSR_ERR_SHAPE;
     if (ldx < cols || ldq < lsr_int8_row_bytes(cols)) return LSR_ERR_SHAPE;
     if (!X || !Q || !scale) return LSR_ERR_NULL;
     if (off_type(X, type_bytes(x_dtype)) || misaligned(Q) || ldq % 16 != 0 || off_type(scale, 4)) return LSR_ERR_ALIGN;
@@ -434,7 +439,7 @@ int lsr_quantize_rows(int64_t rows, int64_t cols, int32_t x_dtype, const void* X
 }
 
 size_t lsr_int8_matmul_workspace_bytes(int64_t N, int64_t V, int64_t K, int32_t a_dtype) {
-    if (!float_type(a_dtype) || N < 1 || N >= MAX_INDEX || V < 1 || V >= MAX_INDEX || K < 1 || K > INT8_MAX_K) return 0;
+    if (!float_type(a_dtype) || N < 1 || N >= MAX_QUANT_ROWS || V < 1 || V >= MAX_INDEX || K < 1 || K > INT8_MAX_K) return 0;
     return int8_ws(N, K).total;
 }
 
@@ -442,12 +447,11 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
                     const int8_t* W, int64_t ldw, const float* w_scale, const float* bias, void* out, int64_t ldo, void* workspace,
                     size_t workspace_bytes, lsr_stream_t stream) {
     if ((!float_type(a_dtype) && a_dtype != LSR_I8) || !float_type(out_dtype)) return LSR_ERR_DTYPE;
-    if (N < 1 || N >= MAX_INDEX || V < 1 || V >= MAX_INDEX || K < 1 || K > INT8_MAX_K) return LSR_ERR_SHAPE;
+    if (N < 1 || N >= MAX_QUANT_ROWS || V < 1 || V >= MAX_INDEX || N * V >= MAX_LOGITS || K < 1 || K > INT8_MAX_K) return LSR_ERR_SHAPE;
     const int64_t row_bytes = up(K, 128);
     const int64_t ld_max = int64_t(1) << 23;
     if (lda < (a_dtype == LSR_I8 ? row_bytes : K) || ldw < row_bytes || ldo < V || ldw > ld_max || (a_dtype == LSR_I8 && lda > ld_max)) return LSR_ERR_SHAPE;
     const int64_t na = (N + NT_COLS - 1) / NT_COLS, nb = (V + TP_T - 1) / TP_T;
-    if (na * nb > int64_t(1) << 30) return LSR_ERR_SHAPE;
     if (!A || !W || !w_scale || !out || (a_dtype == LSR_I8 && !a_scale)) return LSR_ERR_NULL;
     if (a_dtype != LSR_I8 && a_scale) return LSR_ERR_DTYPE;      // values bring no scales
     if (misaligned(W) || ldw % 16 != 0 || off_type(w_scale, 4) || off_type(bias, 4) || off_type(a_scale, 4) || off_type(out, type_bytes(out_dtype)))

@@ -196,9 +196,9 @@ class _LsrDistill(torch.autograd.Function):
         N, D, V, K, dt, temperature = ctx.shape
         need_h, need_w, need_b = ctx.needs_input_grad[:3]
         dev = H.device
-        dH = torch.empty((N, D), dtype=H.dtype, device=dev) if need_h else None
-        dW = torch.empty((V, D), dtype=W.dtype, device=dev) if need_w else None
-        db = torch.empty((V,), dtype=torch.float32, device=dev) if need_b else None
+        dH = torch.empty_like(H) if need_h else None
+        dW = torch.empty_like(W) if need_w else None
+        db = torch.empty_like(bias) if need_b else None
         if dloss is None or not N:
             for g in (dH, dW, db):
                 if g is not None:

@@ -117,6 +117,16 @@ def test_distill_workspace_is_bounded():
     assert f(N, 1024, 250002, K, lsr.LSR_BF16, 1.0, True) < 4 * ((1 << 28) + 256 * N) + 16 * N * (1024 + K + 250002 // 32) + 8 * 250002 * 1024
 
 
+def test_launches_stay_below_their_limits():
+    assert status(lsr.lsr_quantize_rows, 1 << 26, 100, lsr.LSR_BF16, P, 100, P, 128, P) == SHAPE
+    assert status(lsr.lsr_int8_matmul, 1 << 20, 1 << 18, 100, lsr.LSR_BF16, lsr.LSR_F32, P, 100, None, P, 128, P, P, P, 1 << 18, WS) == SHAPE
+    assert lsr.lsr_top_logits_workspace_bytes(1 << 23, 50000, 8) == 0
+    assert status(lsr.lsr_top_logits, 1 << 23, 50000, 8, lsr.LSR_F32, 1.0, P, 50000, P, P, P, WS) == SHAPE
+    for n, d, v in ((1 << 20, 768, 1 << 18), (1 << 21, 4096, 1000)):
+        assert lsr.lsr_distill_workspace_bytes(n, d, v, 8, lsr.LSR_BF16, 1.0, False) == 0
+    assert lsr.lsr_distill_workspace_bytes((1 << 20) - 1, 768, 1 << 18, 8, lsr.LSR_BF16, 1.0, False) > 0
+
+
 def test_no_cpu_path_and_wrong_types():
     x = torch.zeros(4, 64)
     with pytest.raises(RuntimeError):
