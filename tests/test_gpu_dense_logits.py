@@ -406,6 +406,27 @@ def test_distill_few_rows_gradients_that_are_wanted_only(need):
     run_and_check(distill_case(33, 72, 520, 5, "bf16", 22, keep=0.7), need)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [30, 300])
+def test_distill_reads_nothing_of_rows_and_entries_that_are_left_out(N, dtype):
+    H, W, bias, ids, logits, L, mask, T, dloss = distill_case(N, 96, 600, 9, dtype, 25, keep=0.7)
+    ids[::3, 4] = -1
+    rest = lambda i, l, t: (dev(i), dev(l), dev(t), dev(mask), T)                # noqa: E731
+    args = [t.to(DEV).requires_grad_(True) for t in (H, W, bias)]
+    loss, lse = distill.lsr_distill(*args, *rest(ids, logits, L))
+    want = [loss.detach(), lse, *torch.autograd.grad(loss, args, dev(dloss))]
+    off = mask == 0
+    H2, ids2, logits2, L2, dloss2 = H.clone(), ids.copy(), logits.copy(), L.copy(), dloss.copy()
+    H2[torch.from_numpy(off)] = math.nan
+    H2[int(np.flatnonzero(off)[0])] = math.inf
+    ids2[off], logits2[off], L2[off], dloss2[off] = 2 ** 30, np.nan, np.inf, np.nan
+    logits2[::3, 4] = np.nan                            # of an entry that is padding by its id
+    args = [t.to(DEV).requires_grad_(True) for t in (H2, W, bias)]
+    loss, lse = distill.lsr_distill(*args, *rest(ids2, logits2, L2))
+    got = [loss.detach(), lse, *torch.autograd.grad(loss, args, dev(dloss2))]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_distill_few_rows_crowded_tile():
     case = list(distill_case(48, 64, 2000, 200, "bf16", 23))
     rng = np.random.default_rng(24)
