@@ -18,8 +18,10 @@ using namespace lsr;
 
 constexpr int64_t INT8_MAX_K = 65536;
 constexpr int64_t MAX_INDEX = (int64_t(1) << 31) - 4096;
-// A launch stays below 2^32 threads: 64 per row quantised; 256 per segment of a row of logits; 512 per 256 x 256 tile (or two of 256 x 128); one per four elements of dH.
+// A launch stays below 2^32 threads: 64 per row quantised (QUANT_LAUNCH_ROWS at a time: whole workgroups of 2^26 - 1 rows would be 2^32); 256 per segment of a row of
+// logits; 512 per 256 x 256 tile (or two of 256 x 128); one per four elements of dH.
 constexpr int64_t MAX_QUANT_ROWS = int64_t(1) << 26;
+constexpr int64_t QUANT_LAUNCH_ROWS = int64_t(1) << 25;
 constexpr int64_t MAX_TOP_ROWS = int64_t(1) << 23;
 constexpr int64_t MAX_LOGITS = int64_t(1) << 38;
 constexpr int64_t MAX_STATES = int64_t(1) << 33;
@@ -32,16 +34,22 @@ inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 inline bool rows_on_16(const void* p, int64_t ld, size_t esize) { return !misaligned(p) && (ld * (int64_t)esize) % 16 == 0; }
 
 template <typename T>
-void launch_quantize(const void* X, int64_t ldx, int64_t rows, int cols, int8_t* Q, int64_t ldq, float* scale, hipStream_t st) {
-    const unsigned grid = (unsigned)((rows + QUANT_THREADS / 64 - 1) / (QUANT_THREADS / 64));
-    if (rows_on_16(X, ldx, sizeof(T)))
-        quantize_kernel<T, true><<<grid, QUANT_THREADS, 0, st>>>(static_cast<const T*>(X), ldx, rows, cols, Q, ldq, scale);
-    else
-        quantize_kernel<T, false><<<grid, QUANT_THREADS, 0, st>>>(static_cast<const T*>(X), ldx, rows, cols, Q, ldq, scale);
+int launch_quantize(const void* X, int64_t ldx, int64_t rows, int cols, int8_t* Q, int64_t ldq, float* scale, hipStream_t st) {
+    const bool vec = rows_on_16(X, ldx, sizeof(T));
+    for (int64_t r = 0; r < rows; r += QUANT_LAUNCH_ROWS) {
+        const int64_t n = rows - r < QUANT_LAUNCH_ROWS ? rows - r : QUANT_LAUNCH_ROWS;
+        const unsigned grid = (unsigned)((n + QUANT_THREADS / 64 - 1) / (QUANT_THREADS / 64));
+        const T* const x = static_cast<const T*>(X) + r * ldx;
+        if (vec) quantize_kernel<T, true><<<grid, QUANT_THREADS, 0, st>>>(x, ldx, n, cols, Q + r * ldq, ldq, scale + r);
+        else quantize_kernel<T, false><<<grid, QUANT_THREADS, 0, st>>>(x, ldx, n, cols, Q + r * ldq, ldq, scale + r);
+        const int rc = launch_status();
+        if (rc != LSR_OK) return rc;
+    }
+    return LSR_OK;
 }
-void quantize(int32_t type, const void* X, int64_t ldx, int64_t rows, int cols, int8_t* Q, int64_t ldq, float* scale, hipStream_t st) {
-    if (type == LSR_F32) launch_quantize<float>(X, ldx, rows, cols, Q, ldq, scale, st);
-    else launch_quantize<uint16_t>(X, ldx, rows, cols, Q, ldq, scale, st);
+int quantize(int32_t type, const void* X, int64_t ldx, int64_t rows, int cols, int8_t* Q, int64_t ldq, float* scale, hipStream_t st) {
+    if (type == LSR_F32) return launch_quantize<float>(X, ldx, rows, cols, Q, ldq, scale, st);
+    return launch_quantize<uint16_t>(X, ldx, rows, cols, Q, ldq, scale, st);
 }
 
 // Few rows, whose quantised form fits the LDS of the kernel that reads W straight into registers.  Against narrow tiles (us, 8-bit rows): 768 x 30522 1 row
@@ -434,8 +442,7 @@ int lsr_quantize_rows(int64_t rows, int64_t cols, int32_t x_dtype, const void* X
     int n_cus = 0;
     const int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
-    quantize(x_dtype, X, ldx, rows, (int)cols, Q, ldq, scale, stream);
-    return launch_status();
+    return quantize(x_dtype, X, ldx, rows, (int)cols, Q, ldq, scale, stream);
 }
 
 size_t lsr_int8_matmul_workspace_bytes(int64_t N, int64_t V, int64_t K, int32_t a_dtype) {
@@ -463,7 +470,7 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
         if (misaligned(workspace)) return LSR_ERR_ALIGN;
     }
     int n_cus = 0;
-    const int rc = check_device(&n_cus);
+    int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
     Int8Params p = {};
     p.A = A; p.a_scale = a_scale; p.W = W; p.w_scale = w_scale; p.bias = bias; p.out = out;
@@ -474,7 +481,8 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
     if (a_dtype != LSR_I8 && !(few && N <= FEW8_OWN)) {
         int8_t* const q = static_cast<int8_t*>(workspace) + w.q;
         float* const scale = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.scale);
-        quantize(a_dtype, A, lda, N, (int)K, q, row_bytes, scale, stream);
+        rc = quantize(a_dtype, A, lda, N, (int)K, q, row_bytes, scale, stream);
+        if (rc != LSR_OK) return rc;
         p.A = q; p.lda = row_bytes; p.a_scale = scale;
         a_dtype = LSR_I8;
     }

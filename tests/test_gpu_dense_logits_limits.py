@@ -1,0 +1,38 @@
+"""The operators around the dense logits at the ends of what they accept."""
+import math
+
+import pytest
+import torch
+
+import paper_2603_25011_amd as lsr
+from paper_2603_25011_amd import distill
+from tests import test_gpu_dense_logits as base
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def test_quantize_the_most_rows_that_are_accepted():
+    # 2^26 - 1 rows: as many workgroups as would be 2^32 threads in one launch
+    n = (1 << 26) - 1
+    x = torch.ones((n, 1), dtype=torch.bfloat16, device=DEV)
+    x[::3] = -2.0
+    q, s = distill.quantize_rows(x)
+    assert torch.equal(q[:, 0], torch.where(x[:, 0] < 0, -127, 127).to(torch.int8))
+    assert not q.view(torch.int32)[:, 1:].any() and not q[:, 1:4].any()
+    assert torch.equal(s, x[:, 0].float().abs() / 127)
+
+
+def test_int8_matmul_the_most_rows_that_are_accepted():
+    # the product reads the levels that the same call has quantised
+    n = (1 << 26) - 1
+    x = torch.ones((n, 1), dtype=torch.bfloat16, device=DEV)
+    x[::3] = -2.0
+    w = torch.zeros((1, 128), dtype=torch.int8, device=DEV)
+    w[0, 0] = 127
+    out = torch.full((n, 1), math.nan, dtype=torch.float32, device=DEV)
+    ws = torch.empty(lsr.lsr_int8_matmul_workspace_bytes(n, 1, 1, lsr.LSR_BF16), dtype=torch.uint8, device=DEV)
+    ws.fill_(255)                                       # scales that are not written are NaN
+    lsr.lsr_int8_matmul(n, 1, 1, lsr.LSR_BF16, lsr.LSR_F32, x, 1, None, w, 128, torch.full((1,), 1 / 127, device=DEV), None, out, 1, ws)
+    # two scales of a rounding each, their product, and the sum's product with it (and the squares of those)
+    assert ((out - x.float()).abs() <= 4.001 * base.U * x.float().abs()).all()
