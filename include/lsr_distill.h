@@ -92,6 +92,7 @@ int lsr_top_logits(int64_t rows, int64_t V, int64_t K, int32_t x_dtype, float te
  * one that comes twice counts with both probabilities.
  * Rows whose mask byte is 0 are left out: loss 0, lse 0, no gradient.  A row without any entry has loss 0 and no gradient.
  * bias[v] = -inf excludes an entry (a teacher's probability on it makes the loss infinite); everything else is finite.
+ * (A row whose logits hold a NaN and no +inf has lse NaN, and loss NaN where it has an entry; other rows do not see it.)
  *
  * N counts tokens (B * S of the head), D is the hidden size, V the vocabulary, K the teacher's entries per token.
  * Limits: 1 <= N <= 2^22; D a multiple of 8, 8 <= D <= 8192; 1 <= V <= 2^21; N V < 2^38; N D < 2^33;

@@ -46,8 +46,10 @@ __device__ __forceinline__ ExpSum join(ExpSum a, ExpSum b, float c) {
     r.s = a.s * __builtin_amdgcn_exp2f((a.m - z) * c) + b.s * __builtin_amdgcn_exp2f((b.m - z) * c);
     return r;
 }
+// (A maximum does not see a NaN: where there is no number beside it, m is -inf and the sum is NaN.)
 __device__ __forceinline__ float log_sum(ExpSum e, float inv_t) {
-    return fabsf(e.m) == INFINITY ? e.m : fmaf(e.m, inv_t, logf(e.s));
+    if (e.m == INFINITY || (e.m == -INFINITY && e.s == e.s)) return e.m;
+    return fmaf(finite_or_zero(e.m), inv_t, logf(e.s));
 }
 
 struct TopShared {

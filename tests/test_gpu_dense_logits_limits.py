@@ -36,3 +36,23 @@ def test_int8_matmul_the_most_rows_that_are_accepted():
     lsr.lsr_int8_matmul(n, 1, 1, lsr.LSR_BF16, lsr.LSR_F32, x, 1, None, w, 128, torch.full((1,), 1 / 127, device=DEV), None, out, 1, ws)
     # two scales of a rounding each, their product, and the sum's product with it (and the squares of those)
     assert ((out - x.float()).abs() <= 4.001 * base.U * x.float().abs()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [20, 300])
+def test_distill_a_row_that_is_not_a_number_says_so(N, dtype):
+    # every logit of the row is NaN: so are its normaliser and its loss; the other rows do not see it
+    H, W, bias, ids, logits, L, _, T, _ = base.distill_case(N, 64, 600, 5, dtype, 31)
+    rest = (W.to(DEV), bias.to(DEV), base.dev(ids), base.dev(logits), base.dev(L), None, T)
+    want = distill.lsr_distill(H.to(DEV), *rest)
+    H[3, 7] = math.nan
+    loss, lse = distill.lsr_distill(H.to(DEV), *rest)
+    others = torch.arange(N, device=DEV) != 3
+    assert lse[3].isnan() and loss[3].isnan()
+    assert torch.equal(loss[others], want[0][others]) and torch.equal(lse[others], want[1][others])
+    # entries that the bias excludes change nothing about it; a NaN in the matrix is in every row's logits
+    out = torch.where(torch.arange(600, device=DEV) < 590, -math.inf, rest[1])
+    assert distill.lsr_distill(H.to(DEV), rest[0], out, *rest[2:])[1][3].isnan()
+    W2 = rest[0].clone()
+    W2[599, 1] = math.nan
+    assert distill.lsr_distill(H.to(DEV), W2, *rest[1:])[1].isnan().all()
