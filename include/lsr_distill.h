@@ -72,7 +72,7 @@ int lsr_int8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t ou
  *   values  [rows, K] f32, ids [rows, K] int32, lse [rows] f32 or NULL (all 4-byte aligned)
  * Logits of -inf are ordinary values (they come last, and add nothing to lse; a row of them has lse = -inf).
  * -0 and +0 are equal.  NaN comes before +inf and makes lse NaN.
- * Limits: 1 <= rows < 2^23, 1 <= K <= min(V, 256), V < 2^31 - 4096, temperature > 0 and finite.
+ * Limits: 1 <= rows < 2^23, 1 <= K <= min(V, 256), V < 2^31 - 4096, temperature finite and at least 5e-39.
  */
 size_t lsr_top_logits_workspace_bytes(int64_t rows, int64_t V, int64_t K);
 
@@ -96,7 +96,7 @@ int lsr_top_logits(int64_t rows, int64_t V, int64_t K, int32_t x_dtype, float te
  *
  * N counts tokens (B * S of the head), D is the hidden size, V the vocabulary, K the teacher's entries per token.
  * Limits: 1 <= N <= 2^22; D a multiple of 8, 8 <= D <= 8192; 1 <= V <= 2^21; N V < 2^38; N D < 2^33;
- * 1 <= K <= 256; temperature > 0, finite.
+ * 1 <= K <= 256; temperature finite and at least 5e-39 (log2(e) / temperature is a float32).
  *   H [N,D], W [V,D] hw_dtype;  bias [V] f32;  teacher_ids [N,K] int32;  teacher_logits [N,K] f32;
  *   teacher_lse [N] f32 or NULL;  mask [N] uint8 or NULL (no row left out);  loss [N], lse [N] f32.
  * LSR_BF16 multiplies in bfloat16 with float32 sums; LSR_F32 to the precision of float32.

@@ -29,6 +29,8 @@ constexpr int64_t MAX_STATES = int64_t(1) << 33;
 inline bool float_type(int32_t t) { return t == LSR_F32 || t == LSR_BF16; }
 inline size_t type_bytes(int32_t t) { return t == LSR_F32 ? 4 : t == LSR_BF16 ? 2 : 1; }
 inline bool off_type(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+// the kernels multiply by log2(e) / T, formed as here
+inline bool temperature_ok(float t) { return t > 0.f && isfinite(t) && isfinite(1.f / t * LOG2E); }
 inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 // rows of values begin on 16-byte boundaries
 inline bool rows_on_16(const void* p, int64_t ld, size_t esize) { return !misaligned(p) && (ld * (int64_t)esize) % 16 == 0; }
@@ -135,7 +137,7 @@ int check_distill(const lsr_distill_desc* d, DShape* s) {
     if (d->N < 1 || d->N > (int64_t(1) << 22) || d->D < 8 || d->D > 8192 || d->D % 8 != 0) return LSR_ERR_SHAPE;
     if (d->V < 1 || d->V > (int64_t(1) << 21) || d->K < 1 || d->K > TOP_MAX_K) return LSR_ERR_SHAPE;
     if (d->N * d->V >= MAX_LOGITS || d->N * d->D >= MAX_STATES) return LSR_ERR_SHAPE;
-    if (!(d->temperature > 0.f) || !isfinite(d->temperature) || !isfinite(1.f / d->temperature)) return LSR_ERR_SHAPE;
+    if (!temperature_ok(d->temperature)) return LSR_ERR_SHAPE;
     s->N = (int)d->N; s->D = (int)d->D; s->V = (int)d->V; s->K = (int)d->K; s->dtype = d->hw_dtype;
     s->planes = s->dtype == LSR_F32 ? 3 : 1;
     s->width = (int)up(d->D, 64);
@@ -512,7 +514,7 @@ int lsr_top_logits(int64_t rows, int64_t V, int64_t K, int32_t x_dtype, float te
                    float* lse, void* workspace, size_t workspace_bytes, lsr_stream_t stream) {
     if (!float_type(x_dtype)) return LSR_ERR_DTYPE;
     if (!top_shape(rows, V, K) || ldx < V) return LSR_ERR_SHAPE;
-    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return LSR_ERR_SHAPE;
+    if (!temperature_ok(temperature)) return LSR_ERR_SHAPE;
     if (!X || !values || !ids) return LSR_ERR_NULL;
     if (off_type(X, type_bytes(x_dtype)) || off_type(values, 4) || off_type(ids, 4) || off_type(lse, 4)) return LSR_ERR_ALIGN;
     const TopPlan plan = top_plan(rows, V, K);
