@@ -409,7 +409,7 @@ __global__ __launch_bounds__(TP_THREADS, 2) void distill_logits_kernel(LogitsPar
                 const int r = p.list.row(i);
                 gs = p.dloss[r] * p.inv_t;
                 ga = gs * p.mass[i];
-                lse = p.lse[r];
+                if (ga != 0.f) lse = p.lse[r];                 // (a row without a gradient: whatever its normaliser is)
             }
             if (t.wm == 0 && t.half == 0) s_gs[t.col(c)] = gs;
 #pragma unroll

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(FEWD_THREADS, 1) void distill_few_kernel(FewDistill
             const int r = p.list.row(i);
             gs[b] = p.dloss[r] * p.inv_t;
             ga[b] = gs[b] * p.mass[i];
-            lse[b] = p.lse[r];
+            if (ga[b] != 0.f) lse[b] = p.lse[r];               // (a row without a gradient: whatever its normaliser is)
         }
         if (BWD && wave == 0 && half == 0) s_gs[i] = gs[b];
     }

@@ -56,3 +56,14 @@ def test_distill_a_row_that_is_not_a_number_says_so(N, dtype):
     W2 = rest[0].clone()
     W2[599, 1] = math.nan
     assert distill.lsr_distill(H.to(DEV), W2, *rest[1:])[1].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [20, 300])
+def test_distill_a_row_without_entries_has_no_gradient_where_nothing_is_allowed_either(N, dtype):
+    # the bias excludes the whole vocabulary (lse = -inf), and the teacher has no entry: no loss, and zeros as gradients
+    H, W, bias, ids, logits, _, _, T, dloss = base.distill_case(N, 64, 600, 5, dtype, 32)
+    args = [t.to(DEV).requires_grad_(True) for t in (H, W, torch.full_like(bias, -math.inf))]
+    loss, lse = distill.lsr_distill(*args, torch.full_like(base.dev(ids), -1), base.dev(logits), None, None, T)
+    assert not loss.any() and (lse == -math.inf).all()
+    assert not any(g.any() for g in torch.autograd.grad(loss, args, base.dev(dloss)))
