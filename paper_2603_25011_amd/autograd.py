@@ -8,6 +8,29 @@ import torch
 from . import binding as lsr
 
 
+class _FirstOrderOnly(torch.autograd.Function):
+    """The first n of the tensors as they are; differentiating through them raises."""
+
+    @staticmethod
+    def forward(ctx, who, n, *tensors):
+        ctx.who = who
+        return tensors[:n]
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{ctx.who}: gradients of its gradients are not implemented")
+
+
+def first_order_only(who: str, grads: tuple, of: tuple) -> tuple:
+    """What a backward returns.  The library fills gradients without a graph; where one is asked for (create_graph=True), they
+    are tied to the tensors that they depend on (`of`), so that a second derivative raises rather than being left out."""
+    some = [g for g in grads if g is not None]
+    if not torch.is_grad_enabled() or not some:
+        return grads
+    tied = iter(_FirstOrderOnly.apply(who, len(some), *some, *of))
+    return tuple(None if g is None else next(tied) for g in grads)
+
+
 class _LsrHead(torch.autograd.Function):
     @staticmethod
     def forward(ctx, H, W, bias, mask):

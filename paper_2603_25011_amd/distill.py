@@ -15,6 +15,7 @@ import functools
 import torch
 
 from . import binding as lsr
+from .autograd import first_order_only
 
 _KIND = {torch.float32: lsr.LSR_F32, torch.bfloat16: lsr.LSR_BF16}
 
@@ -149,68 +150,41 @@ class Int8Head:
 
 
 class _LsrDistill(torch.autograd.Function):
+    """Tensors as the library takes them: what autograd saves are then the inputs themselves, with their graphs."""
+
     @staticmethod
     def forward(ctx, H, W, bias, ids, logits, teacher_lse, mask, temperature):
-        _on_gpu("lsr_distill", H, W, bias, ids, logits, teacher_lse, mask)
-        if H.dtype != W.dtype or H.dtype not in _KIND:
-            raise TypeError("lsr_distill: H and W must both be bfloat16 or both float32")
-        if ids.dtype not in (torch.int32, torch.int64):
-            raise TypeError("lsr_distill: teacher_ids must be whole numbers of 32 or 64 bits")
-        lead, D = H.shape[:-1], H.shape[-1]
-        V, K = W.shape[0], ids.shape[-1]
-        if W.shape != (V, D) or bias.shape != (V,) or ids.shape != (*lead, K) or logits.shape != ids.shape:
-            raise ValueError("lsr_distill: H [..., D], W [V, D], bias [V], teacher_ids and teacher_logits [..., K] do not fit together")
-        if (teacher_lse is not None and teacher_lse.shape != lead) or (mask is not None and mask.shape != lead):
-            raise ValueError("lsr_distill: teacher_lse and mask must have one value for each row of H")
-        dt = _KIND[H.dtype]
-        H2, W, b32 = _aligned(_as(H, (-1, D))), _aligned(W), _aligned(bias.float())
-        if ids.dtype == torch.int64:
-            # an id that 32 bits do not hold is padding like any other outside the vocabulary
-            ids = torch.where((ids >= 0) & (ids < V), ids, -1).to(torch.int32)
-        ids, logits = _aligned(_as(ids, (-1, K))), _aligned(_as(logits.float(), (-1, K)))
-        if teacher_lse is not None:
-            teacher_lse = _aligned(_as(teacher_lse.float(), (-1,)))
-        if mask is not None:
-            # the library takes any non-zero byte for a row that counts
-            if mask.dtype not in (torch.bool, torch.uint8):
-                mask = mask != 0
-            mask = _aligned(_as(mask, (-1,))).view(torch.uint8)
-        N = H2.shape[0]
+        N, D = H.shape
+        ctx.shape = (N, D, W.shape[0], ids.shape[1], _KIND[H.dtype], temperature)
         loss = torch.empty((N,), dtype=torch.float32, device=H.device)
         lse = torch.empty((N,), dtype=torch.float32, device=H.device)
-        ctx.shape = (N, D, V, K, dt, float(temperature))
         if N:
             with _on(H.device):
                 ws = _scratch(_distill_bytes(ctx.shape, False), H.device)
-                lsr.lsr_distill_forward(*ctx.shape, H2, W, b32, ids, logits, teacher_lse, mask, loss, lse, ws)
-        ctx.save_for_backward(H2, W, b32, ids, logits, teacher_lse, mask, lse)
-        ctx.lead, ctx.bias_dtype = lead, bias.dtype
-        loss, lse_out = _as(loss, lead), _as(lse, lead)
-        ctx.mark_non_differentiable(lse_out)
+                lsr.lsr_distill_forward(*ctx.shape, H, W, bias, ids, logits, teacher_lse, mask, loss, lse, ws)
+        ctx.save_for_backward(H, W, bias, ids, logits, teacher_lse, mask, lse)
+        ctx.mark_non_differentiable(lse)
         ctx.set_materialize_grads(False)
-        return loss, lse_out
+        return loss, lse
 
     @staticmethod
     def backward(ctx, dloss, _dlse):
         H, W, bias, ids, logits, teacher_lse, mask, lse = ctx.saved_tensors
-        N, D, V, K, dt, temperature = ctx.shape
         need_h, need_w, need_b = ctx.needs_input_grad[:3]
         dev = H.device
         dH = torch.empty_like(H) if need_h else None
         dW = torch.empty_like(W) if need_w else None
         db = torch.empty_like(bias) if need_b else None
-        if dloss is None or not N:
+        if dloss is None or not ctx.shape[0]:
             for g in (dH, dW, db):
                 if g is not None:
                     g.zero_()
         elif need_h or need_w or need_b:
-            dloss = _aligned(_as(dloss.float(), (-1,)))
             with _on(dev):
                 ws = _scratch(_distill_bytes(ctx.shape, True), dev)
-                lsr.lsr_distill_backward(*ctx.shape, H, W, bias, ids, logits, teacher_lse, mask, lse, dloss, dH, dW, db, ws)
-        if dH is not None:
-            dH = _as(dH, (*ctx.lead, D))
-        return dH, dW, db if db is None or ctx.bias_dtype == torch.float32 else db.to(ctx.bias_dtype), None, None, None, None, None
+                lsr.lsr_distill_backward(*ctx.shape, H, W, bias, ids, logits, teacher_lse, mask, lse, _aligned(dloss.detach()), dH, dW, db, ws)
+            dH, dW, db = first_order_only("lsr_distill", (dH, dW, db), (H, W, bias, dloss))
+        return dH, dW, db, None, None, None, None, None
 
 
 def _as(t: torch.Tensor, shape: tuple) -> torch.Tensor:
@@ -232,5 +206,29 @@ def lsr_distill(H: torch.Tensor, W: torch.Tensor, bias: torch.Tensor, teacher_id
     L is teacher_lse [...] (log sum exp(logits / temperature) over the teacher's whole vocabulary, as top_logits returns it) or, without it, the same
     over the K entries.  Rows whose mask [...] is zero count nothing; an id outside the vocabulary or a logit of -inf is padding.
     Returns (loss float32 [...], lse float32 [...]): lse is the logarithm of the student's normaliser, not differentiable.
-    Differentiable in H, W and bias; gradients come in the parameters' own dtypes.  The N x V logits are never stored."""
-    return _LsrDistill.apply(H, W, bias, teacher_ids, teacher_logits, teacher_lse, mask, temperature)
+    Differentiable (once) in H, W and bias; gradients come in the parameters' own dtypes.  The N x V logits are never stored."""
+    _on_gpu("lsr_distill", H, W, bias, teacher_ids, teacher_logits, teacher_lse, mask)
+    if H.dtype != W.dtype or H.dtype not in _KIND:
+        raise TypeError("lsr_distill: H and W must both be bfloat16 or both float32")
+    if teacher_ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError("lsr_distill: teacher_ids must be whole numbers of 32 or 64 bits")
+    lead, D = H.shape[:-1], H.shape[-1]
+    V, K = W.shape[0], teacher_ids.shape[-1]
+    if W.shape != (V, D) or bias.shape != (V,) or teacher_ids.shape != (*lead, K) or teacher_logits.shape != teacher_ids.shape:
+        raise ValueError("lsr_distill: H [..., D], W [V, D], bias [V], teacher_ids and teacher_logits [..., K] do not fit together")
+    if (teacher_lse is not None and teacher_lse.shape != lead) or (mask is not None and mask.shape != lead):
+        raise ValueError("lsr_distill: teacher_lse and mask must have one value for each row of H")
+    ids = teacher_ids
+    if ids.dtype == torch.int64:
+        # an id that 32 bits do not hold is padding like any other outside the vocabulary
+        ids = torch.where((ids >= 0) & (ids < V), ids, -1).to(torch.int32)
+    ids, logits = _aligned(_as(ids, (-1, K))), _aligned(_as(teacher_logits.float(), (-1, K)))
+    if teacher_lse is not None:
+        teacher_lse = _aligned(_as(teacher_lse.float(), (-1,)))
+    if mask is not None:
+        # the library takes any non-zero byte for a row that counts
+        if mask.dtype not in (torch.bool, torch.uint8):
+            mask = mask != 0
+        mask = _aligned(_as(mask, (-1,))).view(torch.uint8)
+    loss, lse = _LsrDistill.apply(_aligned(_as(H, (-1, D))), _aligned(W), _aligned(bias.float()), ids, logits, teacher_lse, mask, float(temperature))
+    return _as(loss, lead), _as(lse, lead)
