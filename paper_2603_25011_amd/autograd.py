@@ -73,12 +73,13 @@ class _LsrHead(torch.autograd.Function):
         db = torch.empty((V,), dtype=torch.float32, device=dev) if need_b else None
         if need_h or need_w or need_b:
             ws = torch.empty(lsr.lsr_head_backward_ex_workspace_bytes(B, S, D, V, dt, dt), dtype=torch.uint8, device=dev)
-            lsr.lsr_head_backward_ex(B, S, D, V, dt, H, W, dY, Y, I, dH, dW, db, dt, False, ws)
-        return dH, dW, db, None
+            lsr.lsr_head_backward_ex(B, S, D, V, dt, H, W, dY.detach(), Y, I, dH, dW, db, dt, False, ws)
+        # (Y leads to H, W and bias, of which copies may have been saved)
+        return (*first_order_only("lsr_head", (dH, dW, db), (Y, dY)), None)
 
 
 def lsr_head(H: torch.Tensor, W: torch.Tensor, bias: torch.Tensor, mask: torch.Tensor):
     """Y[b,v] = max over valid s of log(1 + ReLU(H[b,s,:] . W[v,:] + bias[v]))  (Eq. 1), differentiable
-    in H, W and bias.  Returns (Y float32 [B,V], I int32 [B,V]); I is the arg-max position.
+    (once) in H, W and bias.  Returns (Y float32 [B,V], I int32 [B,V]); I is the arg-max position.
     Gradients are summed in float32 and stored by the library in the dtype of the parameter they belong to."""
     return _LsrHead.apply(H, W, bias, mask)

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2603_25011_amd import distill
+from paper_2603_25011_amd.autograd import lsr_head
 from tests import test_gpu_dense_logits as base
 
 pytestmark = pytest.mark.gpu
@@ -55,3 +56,23 @@ def test_distill_second_derivatives_raise_through_copies_and_weights():
         for to in (wide, Wt, b, weight):
             with pytest.raises(RuntimeError, match="lsr_distill"):
                 torch.autograd.grad(total, to, retain_graph=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_head_second_derivatives_raise(dtype):
+    gen = torch.Generator(device=DEV).manual_seed(43)
+    H = torch.randn(64, 70, 2, device=DEV, generator=gen).to(dtype).requires_grad_(True)       # (a transposed view goes in: a copy is saved)
+    W = torch.randn(300, 64, device=DEV, generator=gen).to(dtype).requires_grad_(True)
+    b = torch.randn(300, device=DEV, generator=gen).to(dtype).requires_grad_(True)
+    weight = torch.rand(2, 300, device=DEV, generator=gen).requires_grad_(True)
+    mask = torch.ones(2, 70, dtype=torch.bool, device=DEV)
+    for of in (H, W, b):
+        Y, I = lsr_head(H.permute(2, 1, 0), W, b, mask)
+        plain, = torch.autograd.grad(Y, of, weight.detach(), retain_graph=True)
+        g, total = penalised(Y, sum((x.float() ** 2).sum() for x in (H, W, b)), of, weight)
+        assert torch.equal(g, plain)
+        for to in (H, W, b, weight):
+            with pytest.raises(RuntimeError, match="lsr_head"):
+                torch.autograd.grad(total, to, retain_graph=True)
+        with pytest.raises(RuntimeError, match="lsr_head"):
+            total.backward(retain_graph=True)
