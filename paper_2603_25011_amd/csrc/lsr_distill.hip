@@ -54,11 +54,19 @@ int quantize(int32_t type, const void* X, int64_t ldx, int64_t rows, int cols, i
     return launch_quantize<uint16_t>(X, ldx, rows, cols, Q, ldq, scale, st);
 }
 
-// Few rows, whose quantised form fits the LDS of the kernel that reads W straight into registers.  Against narrow tiles (us, 8-bit rows): 768 x 30522 1 row
-// 6.6 / 10.1, 32 rows 9.0 / 10.3, 64 rows (two blocks) 14 / 11; 768 x 100000 16 rows 19.4 / 19.8, 32 rows 21.8 / 20.4; 1024 x 250002 1 row 40.6 / 43.0, 16 rows 47 / 45.6,
-// 32 rows 55 / 48.
+// Few rows, whose quantised form fits the LDS of the kernel that reads W straight into registers, as many as it is not slower for than narrow tiles.  Its rows of
+// logits leave in pieces of 32 entries, and its reads of W share the CU with them: the rows it is worth go down with the vocabulary, and again where W does not
+// stay in the memory-side cache.  Against narrow tiles (us, float32 / bfloat16 logits):
+//   768 x 30522, 8-bit rows    1 row 6.0 : 9.0 / 5.9 : 9.7    32 rows 9.3 : 9.8 / 9.0 : 10.1    64 rows (two blocks) 14 : 11
+//   768 x 65536, 8-bit rows    24 rows 13.8 : 13.7 / 13.4 : 14.2    32 rows 14.8 : 14.3 / 14.3 : 14.4
+//   768 x 100000, 8-bit rows   16 rows 19.4 : 19.0 / 19.3 : 19.5    24 rows 20.8 : 19.5 / 20.6 : 19.8
+//   1024 x 200000, 8-bit rows  16 rows 40.5 : 40.2 / 39.6 : 40.9
+//   1024 x 250002, 8-bit rows  12 rows 48.0 : 44.2 / 46.0 : 44.8    16 rows 49.8 : 45.8 / 48.1 : 45.7
+//   1024 x 250002, values      4 rows 45.5 : 46.9 / 45.3 : 48.0    8 rows 47.5 : 47.0 / 47.4 : 48.4    9 rows 49.9 : 47.2 / 48.3 : 48.6
+constexpr int64_t CACHED_W = int64_t(7) << 25;         // bytes: 7/8 of the memory-side cache
 bool int8_few(int64_t N, int64_t V, int64_t K) {
-    return N <= (V <= 65536 ? FEW8_ROWS : FEW8_ROWS / 2) && N * few8_stride((int)up(K, 128)) <= FEW8_LDS;
+    const int64_t most = V <= 65536 ? FEW8_ROWS : V * up(K, 128) <= CACHED_W ? FEW8_ROWS / 2 : FEW8_OWN;
+    return N <= most && N * few8_stride((int)up(K, 128)) <= FEW8_LDS;
 }
 
 struct Int8Ws { size_t q, scale, total; };

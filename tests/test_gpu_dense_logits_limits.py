@@ -67,3 +67,15 @@ def test_distill_a_row_without_entries_has_no_gradient_where_nothing_is_allowed_
     loss, lse = distill.lsr_distill(*args, torch.full_like(base.dev(ids), -1), base.dev(logits), None, None, T)
     assert not loss.any() and (lse == -math.inf).all()
     assert not any(g.any() for g in torch.autograd.grad(loss, args, base.dev(dloss)))
+
+
+@pytest.mark.parametrize("V,K", [(30522, 768), (70001, 384), (250002, 1024)])
+def test_int8_rows_do_not_depend_on_how_many_come_along(V, K):
+    # the kernels for few rows and for many give the same bits, wherever the one hands over to the other
+    gen = torch.Generator(device=DEV).manual_seed(V)
+    head = distill.Int8Head(torch.randn(V, K, device=DEV, generator=gen, dtype=torch.bfloat16), torch.randn(V, device=DEV, generator=gen))
+    H = torch.randn(40, K, device=DEV, generator=gen)
+    for dtype in (torch.float32, torch.bfloat16):
+        want = torch.cat([head.logits(h, dtype) for h in H.split(1)])
+        for n in (8, 9, 16, 17, 32, 33, 40):
+            assert torch.equal(head.logits(H[:n], dtype), want[:n]), (n, dtype)
