@@ -79,3 +79,30 @@ def test_int8_rows_do_not_depend_on_how_many_come_along(V, K):
         want = torch.cat([head.logits(h, dtype) for h in H.split(1)])
         for n in (8, 9, 16, 17, 32, 33, 40):
             assert torch.equal(head.logits(H[:n], dtype), want[:n]), (n, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [1, 40, 9000, 70000])
+def test_top_logits_infinite_normalisers_are_exactly_that(V, dtype):
+    # in one segment and in several (70000 entries of few rows), wherever the infinity lies
+    td = base.TYPES[dtype]
+    x = torch.zeros(6, V, dtype=td)
+    x[0] = -math.inf
+    x[1, V - 1] = math.inf
+    x[2, 0] = math.inf
+    x[3] = math.inf
+    x[4] = -math.inf
+    x[4, V // 2] = math.inf
+    x[5] = -math.inf
+    x[5, V // 2] = 1.5
+    v, i, lse = distill.top_logits(x.to(DEV), 1, 2.0)
+    assert lse.tolist() == [-math.inf, *[math.inf] * 4, 0.75]
+    assert v[:, 0].tolist() == [-math.inf, *[math.inf] * 4, 1.5] and i[:, 0].tolist() == [0, V - 1, 0, 0, V // 2, V // 2]
+
+
+def test_distill_infinite_normalisers_are_exactly_that():
+    for N in (20, 300):
+        H, W, bias, ids, logits, _, _, T, _ = base.distill_case(N, 64, 600, 5, "bf16", 33)
+        rest = (base.dev(ids), base.dev(logits))
+        loss, lse = distill.lsr_distill(H.to(DEV), W.to(DEV), torch.full((600,), -math.inf, device=DEV), torch.full_like(rest[0], 600), rest[1])
+        assert (lse == -math.inf).all() and not loss.any()
