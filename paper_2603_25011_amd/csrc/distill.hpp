@@ -11,8 +11,8 @@
 //   forward   distill_logits_kernel<false>: per tile and token one (maximum, sum of exp); distill_loss_kernel joins them
 //   backward  distill_logits_kernel<true>: logits again, g in bfloat16 in two layouts for a piece of the vocabulary at a time, db from
 //             the unrounded g; distill_grads_kernel: the two products of that piece in one launch
-// Measured (kernels): logits forward 4096 x 1024 x 250002 1.9 ms (1.1 PFLOP/s; a large library product reaches 1.18), 10800 x 768 x 30522 0.54 ms; backward the same
-// products and g, 4096 x 1024 x 62720 0.63 ms (0.83 PFLOP/s; 0.53 ms without writing g's two layouts); both gradient products of that piece 0.88 ms (1.2 PFLOP/s).
+// Measured (kernels): logits forward 4096 x 1024 x 250002 2.0 ms (1.05 PFLOP/s; a large library product reaches 1.18), 10800 x 768 x 30522 0.54 to 0.58 ms; backward the
+// same products and g, 4096 x 1024 x 62720 0.65 ms (0.81 PFLOP/s; 0.53 ms without writing g's two layouts); both gradient products of that piece 0.88 ms (1.2 PFLOP/s).
 // All are bound by the matrix cores and the clock they leave (1.8 to 1.9 GHz); the backward's logits by the exchange and the write of g besides.
 // The vocabulary runs along the rows of a logit tile, tokens along the columns: a lane then holds 64 logits of each of two tokens,
 // and the softmax statistics are in-lane sums with one exchange at the end.
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(256) void distill_transpose_kernel(const uint16_t* 
 //   hits[64 K grp + first[grp][vt] .. 64 K grp + first[grp][vt + 1]): .x = place in the token tile << 16 | place in the vocabulary tile << 8 | j, .y = p
 // Entries with p = 0 are left out.  One workgroup per group, four rows per wave, a row's entries across the lanes and kept in registers from the
 // statistics to the placement: a count in LDS, a prefix sum, the placement (the order within a bucket is free: every entry has its own result).
-// Bound by latency: 10 us for 4096 rows of 64 (one group of 256 rows per workgroup, entries read twice: 27 us).
+// Bound by latency: 9 to 12 us for 2048 or 4096 rows of 64 (one group of 256 rows per workgroup, entries read twice: 27 us).
 constexpr int GROUP = 64;
 constexpr int TEACHER_THREADS = 1024;
 template <int PER>                               // entries per lane and row: K <= 64 PER

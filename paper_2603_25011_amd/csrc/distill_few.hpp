@@ -1,4 +1,5 @@
-// Distillation of few rows: up to 64 tokens, whose hidden states stay in LDS while W is read straight into registers.
+// Distillation of few rows: up to 64 tokens whose hidden states fit LDS (64 of 1072 or 32 of 2160 elements in bfloat16, 64 of 536 or 32 of 1080 in float32) and
+// stay there while W is read straight into registers.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -13,9 +14,9 @@ namespace lsr {
 //                              sums of exp run along in registers
 //   distill_few_kernel<true>   the same products; g of the 32 entries, their rows of dW = g^T H and their db on the spot, g itself to memory
 //   distill_few_dh_kernel      dH = g W, W read by columns: a wave owns 32 columns of D and a part of the vocabulary
-// Float32 is multiplied in float32 (the time is that of the reads).  bfloat16 gradients take g as two bfloat16 whose sum has 16 bits: with few rows, single entries
-// make up whole sums, and the one rounding that many rows average out would show.
-// 20 x 1024 x 250002: forward 114 us and step 620 us in bfloat16 (4.5 and 3.3 TB/s), 300 and 1170 us in float32.
+// Float32 is multiplied in float32 (the time is that of the reads).  bfloat16 gradients take g as two bfloat16 whose sum has 16 bits, which the reads of W leave room
+// for: dH and dW are then as exact as their own rounding to bfloat16 (error 0.0017 of the norm; with g rounded once, as for more rows, 0.0024).
+// 20 x 1024 x 250002: forward 115 us and step 627 us in bfloat16 (4.5 and 3.3 TB/s), 299 and 1163 us in float32.
 constexpr int FEWD_THREADS = 256;
 constexpr int FEWD_ROWS = 64;
 constexpr int FEWD_U = 8;
@@ -47,10 +48,6 @@ struct FewDistillParams {
     int parts;
 };
 
-template <typename T> __device__ __forceinline__ float as_float(T b) {
-    if constexpr (sizeof(T) == 4) return b;
-    else return __uint_as_float((uint32_t)b << 16);
-}
 // eight values as bfloat16, and what is left of them as bfloat16
 __device__ __forceinline__ void two_bf16(const float (&g)[8], bf16x8& hi, bf16x8& lo) {
 #pragma unroll

@@ -44,7 +44,7 @@ __device__ __forceinline__ void store16(OT* o, const uint4& w, int left) {
 
 // Many rows: one tile of 256 vocabulary entries x 128 rows per workgroup, two workgroups per CU.  The logits go through LDS, so that a row of the result leaves in
 // pieces of 512 bytes or more.  8192 x 768 x 30522 to bfloat16: one 256 x 256 tile per CU, 2-byte stores straight from the accumulators 430 us; the same
-// through LDS 350 us; two narrow tiles per CU 345 us; with stores past the caches 272 us (the products alone take 220).  PAST: the host takes it where the result
+// through LDS 350 us; two narrow tiles per CU 345 us; with stores past the caches 264 us (the products alone take 220).  PAST: the host takes it where the result
 // is larger than the memory-side cache; written through it, it pushes the operands out (2048 x 1024 x 250002 787 -> 662 us), below that size plain
 // stores are as fast or faster (59 MB 27 / 30 us, 119 MB 47 / 56, 238 MB 145 / 143).
 template <typename OT, bool PAST>

@@ -12,8 +12,8 @@ namespace lsr {
 // logits are no smaller, and few more are.  When the list has grown it is cut to its K largest, whose last is the next threshold.
 // A key's place is the number of larger keys (counted, the list is short; no sort).  The maximum and sum of exp of the row
 // run along in registers.  Segments of one row are joined by a second launch.
-// Bound by the vector ALU, about 20 instructions per logit: 4096 x 30522 in bfloat16, K = 64, 84 us (3.0 TB/s; 64 us without the sums of exp), 256 x 250002 in
-// float32, K = 128, 92 us and 6 us for the joining launch; one row of 30522 8 + 5 us, latency.
+// Bound by the vector ALU, about 20 instructions per logit: 4096 x 30522 in bfloat16, K = 64, 84 to 89 us (2.8 to 3.0 TB/s; 64 us without the sums of
+// exp), 256 x 250002 in float32, K = 128, 89 us and 7 us for the joining launch; one row of 30522 8.5 + 5 us, latency.
 constexpr int TOP_THREADS = 256;
 constexpr int TOP_PER = 32;                            // logits per thread and batch
 constexpr int TOP_BATCH = TOP_THREADS * TOP_PER;
