@@ -1,7 +1,7 @@
 """ctypes binding of liblsr_head.so: argument marshalling only.
 
-Every function here has the name and argument order of its C entry point (include/lsr_head.h, include/lsr_distill.h) and
-does nothing but turn torch tensors into device pointers and pass the current HIP stream.  All of the
+Every function here has the name and argument order of its C entry point (include/lsr_head.h, include/lsr_distill.h,
+include/lsr_fp8.h, include/lsr_beam.h, include/lsr_dropout.h) and does nothing but turn torch tensors into device pointers and pass the current HIP stream.  All of the
 head's arithmetic runs in the HIP kernels; there is no fallback: if the library has not been built
 or cannot be loaded, importing succeeds but every call raises.
 """
@@ -14,6 +14,7 @@ from typing import Optional
 LSR_F32 = 0
 LSR_BF16 = 1
 LSR_I8 = 2                    # rows of 8-bit integers (include/lsr_distill.h)
+LSR_E4M3 = 3                  # 8-bit floating point in blocks (include/lsr_fp8.h)
 LSR_PROFILE_SLOTS = 8
 LSR_STATIC_SCRATCH_BYTES = 16 << 20
 LSR_DW_BEHIND_DH, LSR_DW_ON_AUX_STREAM, LSR_DW_IN_PLACEMENT_LAUNCH, LSR_DW_IN_DH_LAUNCH = range(4)
@@ -41,6 +42,12 @@ class _Desc(ctypes.Structure):
 class _DistillDesc(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int64), ("D", ctypes.c_int64), ("V", ctypes.c_int64), ("K", ctypes.c_int64),
                 ("hw_dtype", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+class _BeamState(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("src_batch", ctypes.c_int64), ("src_beam", ctypes.c_int64),
+                ("src_piece", ctypes.c_int64), ("dst_batch", ctypes.c_int64), ("dst_beam", ctypes.c_int64), ("dst_piece", ctypes.c_int64),
+                ("pieces", ctypes.c_int64), ("piece_bytes", ctypes.c_int64)]
 
 
 def library_path() -> str:
@@ -106,6 +113,28 @@ def load_library():
     lib.lsr_distill_forward.argtypes = [ddp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lsr_distill_backward.restype = ctypes.c_int
     lib.lsr_distill_backward.argtypes = [ddp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lsr_fp8_row_bytes.restype = i64
+    lib.lsr_fp8_row_bytes.argtypes = [i64]
+    lib.lsr_fp8_exp_bytes.restype = i64
+    lib.lsr_fp8_exp_bytes.argtypes = [i64, i64]
+    lib.lsr_fp8_quantize.restype = ctypes.c_int
+    lib.lsr_fp8_quantize.argtypes = [i64, i64, i32, vp, i64, i32, vp, i64, vp, vp, i64, vp, vp]
+    lib.lsr_fp8_matmul_workspace_bytes.restype = sz
+    lib.lsr_fp8_matmul_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.lsr_fp8_matmul.restype = ctypes.c_int
+    lib.lsr_fp8_matmul.argtypes = [i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+    lib.lsr_fp8_backward_workspace_bytes.restype = sz
+    lib.lsr_fp8_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32]
+    lib.lsr_fp8_backward.restype = ctypes.c_int
+    lib.lsr_fp8_backward.argtypes = [i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+    lib.lsr_beam_select_workspace_bytes.restype = sz
+    lib.lsr_beam_select_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.lsr_beam_select.restype = ctypes.c_int
+    lib.lsr_beam_select.argtypes = [i64, i64, i64, i64, i32, ctypes.c_double, vp, i64, vp, vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.lsr_beam_reorder.restype = ctypes.c_int
+    lib.lsr_beam_reorder.argtypes = [i64, i64, i64, vp, i64, ctypes.POINTER(_BeamState), vp]
+    lib.lsr_dropout.restype = ctypes.c_int
+    lib.lsr_dropout.argtypes = [i64, i32, vp, vp, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, vp, vp]
     lib.lsr_status_string.restype = ctypes.c_char_p
     lib.lsr_status_string.argtypes = [ctypes.c_int]
     _lib = lib
@@ -318,3 +347,66 @@ def lsr_distill_backward(N, D, V, K, hw_dtype, temperature, H, W, bias, teacher_
     _check(load_library().lsr_distill_backward(ctypes.byref(d), _ptr(H), _ptr(W), _ptr(bias), _ptr(teacher_ids), _ptr(teacher_logits),
                                                _ptr(teacher_lse), _ptr(mask), _ptr(lse), _ptr(dloss), _ptr(dH), _ptr(dW), _ptr(db), wp, wb,
                                                _stream(stream)))
+
+
+# ---- the head's dense logits in 8-bit floating point (include/lsr_fp8.h) ----
+
+def lsr_fp8_row_bytes(cols) -> int:
+    return int(load_library().lsr_fp8_row_bytes(int(cols)))
+
+
+def lsr_fp8_exp_bytes(rows, cols) -> int:
+    return int(load_library().lsr_fp8_exp_bytes(int(rows), int(cols)))
+
+
+def lsr_fp8_quantize(rows, cols, x_dtype, X, ldx, square, Q, ldq, exps, Qt, ldqt, exps_t, stream=None) -> None:
+    _check(load_library().lsr_fp8_quantize(int(rows), int(cols), int(x_dtype), _ptr(X), int(ldx), int(square), _ptr(Q), int(ldq), _ptr(exps),
+                                           _ptr(Qt), int(ldqt), _ptr(exps_t), _stream(stream)))
+
+
+def lsr_fp8_matmul_workspace_bytes(N, V, K, a_dtype) -> int:
+    return int(load_library().lsr_fp8_matmul_workspace_bytes(int(N), int(V), int(K), int(a_dtype)))
+
+
+def lsr_fp8_matmul(N, V, K, a_dtype, out_dtype, A, lda, a_exps, W, ldw, w_exps, bias, out, ldo, workspace, stream=None) -> None:
+    wp, wb = _ws(workspace)
+    _check(load_library().lsr_fp8_matmul(int(N), int(V), int(K), int(a_dtype), int(out_dtype), _ptr(A), int(lda), _ptr(a_exps),
+                                         _ptr(W), int(ldw), _ptr(w_exps), _ptr(bias), _ptr(out), int(ldo), wp, wb, _stream(stream)))
+
+
+def lsr_fp8_backward_workspace_bytes(N, V, D, need_dh=True, need_dw=True, need_db=True) -> int:
+    return int(load_library().lsr_fp8_backward_workspace_bytes(int(N), int(V), int(D), int(need_dh), int(need_dw), int(need_db)))
+
+
+def lsr_fp8_backward(N, V, D, y_dtype, h_dtype, dY, ldy, H, ldh, Wt, ldwt, wt_exps, dH, dW, db, workspace, stream=None) -> None:
+    wp, wb = _ws(workspace)
+    _check(load_library().lsr_fp8_backward(int(N), int(V), int(D), int(y_dtype), int(h_dtype), _ptr(dY), int(ldy), _ptr(H), int(ldh), _ptr(Wt),
+                                           int(ldwt), _ptr(wt_exps), _ptr(dH), _ptr(dW), _ptr(db), wp, wb, _stream(stream)))
+
+
+# ---- beam search over the dense logits (include/lsr_beam.h) ----
+
+def lsr_beam_select_workspace_bytes(B, beams, V, K) -> int:
+    return int(load_library().lsr_beam_select_workspace_bytes(int(B), int(beams), int(V), int(K)))
+
+
+def lsr_beam_select(B, beams, V, K, x_dtype, temperature, X, ldx, scores, finished, end_id, out_scores, out_beams, out_tokens, workspace,
+                    stream=None) -> None:
+    wp, wb = _ws(workspace)
+    _check(load_library().lsr_beam_select(int(B), int(beams), int(V), int(K), int(x_dtype), float(temperature), _ptr(X), int(ldx), _ptr(scores),
+                                          _ptr(finished), int(end_id), _ptr(out_scores), _ptr(out_beams), _ptr(out_tokens), wp, wb,
+                                          _stream(stream)))
+
+
+def lsr_beam_reorder(B, beams, K, parents, states, stream=None) -> None:
+    """`states`: sequence of tuples (src, dst, src_batch, src_beam, src_piece, dst_batch, dst_beam, dst_piece, pieces, piece_bytes), strides in bytes."""
+    n = len(states)
+    table = (_BeamState * max(n, 1))(*[_BeamState(_ptr(s[0]), _ptr(s[1]), *map(int, s[2:])) for s in states])
+    _check(load_library().lsr_beam_reorder(int(B), int(beams), int(K), _ptr(parents), n, table, _stream(stream)))
+
+
+# ---- dropout (include/lsr_dropout.h) ----
+
+def lsr_dropout(n, dtype, X, Y, p, seed, offset, state, stream=None) -> None:
+    _check(load_library().lsr_dropout(int(n), int(dtype), _ptr(X), _ptr(Y), float(p), int(seed) % (1 << 64), int(offset) % (1 << 64), _ptr(state),
+                                      _stream(stream)))

@@ -11,6 +11,8 @@ LIB = os.path.join(PKG, "liblsr_head.so")
 SRC = os.path.join(PKG, "csrc", "lsr_head.hip")
 # the operators around the head's dense logits, in the same library
 DISTILL_SRC = os.path.join(PKG, "csrc", "lsr_distill.hip")
+# ... in 8-bit floating point, a beam search over them, and dropout
+MORE_SRC = [os.path.join(PKG, "csrc", n) for n in ("lsr_fp8.hip", "lsr_beam.hip", "lsr_dropout.hip")]
 # benchmark comparator (the reduce step of the paper's hybrid forward); not part of the product library
 ALG2_LIB = os.path.join(PKG, "libalg2_reduce.so")
 ALG2_SRC = os.path.join(PKG, "csrc", "alg2_reduce.hip")
@@ -38,7 +40,7 @@ def _compile(src: list, lib: str, verbose: bool) -> None:
 
 
 def build(verbose: bool = False) -> str:
-    _compile([SRC, DISTILL_SRC], LIB, verbose)
+    _compile([SRC, DISTILL_SRC, *MORE_SRC], LIB, verbose)
     _compile([ALG2_SRC], ALG2_LIB, verbose)
     return LIB
 

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "top_rank.hpp"
+
 namespace lsr {
 
 // A workgroup takes a segment of a row (the whole row, where there are enough rows to fill the chip) in batches of TOP_BATCH
@@ -14,30 +16,12 @@ namespace lsr {
 // run along in registers.  Segments of one row are joined by a second launch.
 // Bound by the vector ALU, about 20 instructions per logit: 4096 x 30522 in bfloat16, K = 64, 84 to 89 us (2.8 to 3.0 TB/s; 64 us without the sums of
 // exp), 256 x 250002 in float32, K = 128, 89 us and 7 us for the joining launch; one row of 30522 8.5 + 5 us, latency.
-constexpr int TOP_THREADS = 256;
 constexpr int TOP_PER = 32;                            // logits per thread and batch
 constexpr int TOP_BATCH = TOP_THREADS * TOP_PER;
 constexpr int TOP_CAP = 1024;                          // keys in the list
-constexpr int TOP_WAVES = TOP_THREADS / 64;
-constexpr int TOP_MAX_K = 256;                         // (no more than threads: the first threshold)
-constexpr int TOP_MERGE_KEYS = 2048;                   // keys that the segments of one row hand over
-constexpr float LOG2E = 1.44269504088896340736f;
-
-// Ordered bits: NaN above +inf, -0 as +0; never 0.
-__device__ __forceinline__ uint32_t ordered(float x) {
-    const uint32_t b = __float_as_uint(x + 0.f);
-    if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
-    return (int)b < 0 ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float value_of(uint32_t o) {
-    if (o == 0xffffffffu) return __uint_as_float(0x7fc00000u);
-    return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o);
-}
-__device__ __forceinline__ uint64_t key_of(uint32_t o, uint32_t index) { return (uint64_t)o << 32 | (uint32_t)~index; }
 
 // Running maximum and sum of exp2((x - m) c), c = log2(e) / temperature.  m = -inf: no finite logit yet.  (The difference is formed first: with one
 // fused multiply-add x c - m c instead, the rounding of m c overflows the sum where a mask holds the type's lowest value.)
-struct ExpSum { float m, s; };
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ ExpSum join(ExpSum a, ExpSum b, float c) {
     ExpSum r;
@@ -50,33 +34,6 @@ __device__ __forceinline__ ExpSum join(ExpSum a, ExpSum b, float c) {
 __device__ __forceinline__ float log_sum(ExpSum e, float inv_t) {
     if (e.m == INFINITY || (e.m == -INFINITY && e.s == e.s)) return e.m;
     return fmaf(finite_or_zero(e.m), inv_t, logf(e.s));
-}
-
-struct TopShared {
-    __attribute__((aligned(16))) uint64_t list[TOP_MERGE_KEYS];
-    uint64_t best[TOP_MAX_K];
-    uint32_t most[TOP_WAVES];
-    ExpSum part[TOP_WAVES];
-    int count;
-};
-
-// best[0 .. min(K, n)) = the largest of list[0 .. n), in order.  Whole workgroup; the list is complete (a barrier behind its last write); a barrier at the end.
-__device__ __forceinline__ void top_rank(TopShared& sh, int n, int K) {
-    for (int i = threadIdx.x; i < n; i += TOP_THREADS) {
-        const uint64_t k = sh.list[i];
-        int rank = 0;
-        int j = 0;
-        for (; j + 8 <= n; j += 8) {             // 16-byte reads, the same address in every lane
-            ulonglong2 q[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) q[e] = *reinterpret_cast<const ulonglong2*>(&sh.list[j + 2 * e]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) rank += (q[e].x > k ? 1 : 0) + (q[e].y > k ? 1 : 0);
-        }
-        for (; j < n; ++j) rank += sh.list[j] > k ? 1 : 0;
-        if (rank < K) sh.best[rank] = k;
-    }
-    __syncthreads();
 }
 
 __device__ __forceinline__ ExpSum block_join(TopShared& sh, ExpSum e, float c) {
