@@ -31,16 +31,22 @@ extern "C" {
 /* An element type beside LSR_F32 and LSR_BF16: e4m3 values with exponents as above. */
 #define LSR_E4M3 3
 
-/* Bytes of a row of `cols` e4m3 values, a multiple of 128; and of the exponents of a matrix (both 0 where out of range). */
+/*
+ * Bytes of a row of `cols` e4m3 values, a multiple of 128; of the exponents of a matrix; and of a matrix laid out by slab (all 0 where out of range):
+ * 256 rows of 64 bytes behind each other, then the next 64 columns of the same rows, so that what a tile of a product reads at a time lies in one
+ * piece however long the rows are.  Byte c of row r is byte ((r / 256) (lsr_fp8_row_bytes(cols) / 64) + c / 64) 16384 + (r % 256) 64 + c % 64.
+ */
 int64_t lsr_fp8_row_bytes(int64_t cols);
 int64_t lsr_fp8_exp_bytes(int64_t rows, int64_t cols);
+int64_t lsr_fp8_slab_bytes(int64_t rows, int64_t cols);
 
 /*
  * X [rows, ldx] x_dtype (LSR_F32 or LSR_BF16), any alignment of its elements, ldx >= cols, to one or both of
  *   Q  [rows, ldq], exps    blocks of 1 x 128 along the rows: operands whose contracted axis is the columns
  *   Qt [cols, ldqt], exps_t X transposed, blocks along the rows of X: operands whose contracted axis is the rows
  * With `square` not 0 a block is 128 x 128 of X, and Qt is Q transposed.  ldq and ldqt are multiples of 16, at least lsr_fp8_row_bytes(cols)
- * and (rows); bytes behind the end of a row are set to zero up to there, and not touched behind that.  Either pair may be NULL.
+ * and (rows); bytes behind the end of a row are set to zero up to there, and not touched behind that.  ldqt = 0: Qt by slab (rows behind the last of the
+ * last 256 are not touched).  Either pair may be NULL.
  * The exponents are laid out as said above (for exps_t with `cols` rows), 4-byte aligned.
  * Limits: 1 <= rows, cols <= 2^22, rows cols < 2^36.
  */
@@ -75,7 +81,7 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
  *   dW[v,:] = sum_n qt(dY)[n,v] qt(H)[n,:]   both in blocks of 128 x 1 along their columns (the tokens)
  *   db[v]   = sum_n dY[n,v]                  of the values as given
  *   dY [N, ldy] y_dtype, H [N, ldh] h_dtype (each LSR_F32 or LSR_BF16), any alignment of their elements
- *   Wt [D, ldwt], wt_exps: W transposed as lsr_fp8_quantize leaves Qt and exps_t (square)
+ *   Wt [D, ldwt], wt_exps: W transposed as lsr_fp8_quantize leaves Qt and exps_t (square), with ldwt = 0 by slab, which is faster
  *   dH [N, D], dW [V, D] of h_dtype, contiguous; db [V] f32; each may be NULL to skip it.  H is needed for dW alone, Wt for dH alone.
  * Sums are formed as in lsr_fp8_matmul (exact products and float32 sums where h_dtype is LSR_F32), over cuts of the contracted axis where there are
  * few tiles, joined in float32 in a fixed order and rounded once.  Results are the same bits from call to call.

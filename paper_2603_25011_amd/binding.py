@@ -115,6 +115,8 @@ def load_library():
     lib.lsr_distill_backward.argtypes = [ddp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lsr_fp8_row_bytes.restype = i64
     lib.lsr_fp8_row_bytes.argtypes = [i64]
+    lib.lsr_fp8_slab_bytes.restype = i64
+    lib.lsr_fp8_slab_bytes.argtypes = [i64, i64]
     lib.lsr_fp8_exp_bytes.restype = i64
     lib.lsr_fp8_exp_bytes.argtypes = [i64, i64]
     lib.lsr_fp8_quantize.restype = ctypes.c_int
@@ -357,6 +359,10 @@ def lsr_fp8_row_bytes(cols) -> int:
 
 def lsr_fp8_exp_bytes(rows, cols) -> int:
     return int(load_library().lsr_fp8_exp_bytes(int(rows), int(cols)))
+
+
+def lsr_fp8_slab_bytes(rows, cols) -> int:
+    return int(load_library().lsr_fp8_slab_bytes(int(rows), int(cols)))
 
 
 def lsr_fp8_quantize(rows, cols, x_dtype, X, ldx, square, Q, ldq, exps, Qt, ldqt, exps_t, stream=None) -> None:

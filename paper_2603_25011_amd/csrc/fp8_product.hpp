@@ -10,7 +10,6 @@
 namespace lsr {
 
 typedef int intx8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // Two ways to multiply, chosen by the type of the result.
 //   fast   the matrix cores' scaled 8-bit instruction: 32 x 32 x 64 at twice the rate of bfloat16, the powers as operands.  It adds its products in small groups in which
@@ -18,12 +17,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 //          magnitudes spread over 2^8), far below a rounding to bfloat16 (1.7e-3), which is what results of that type get.
 //   exact  e4m3 times its power is a bfloat16 value (but for what lies below 2^-126), so the bfloat16 instruction multiplies the same numbers with float32 sums (4e-8 of the norm
 //          at 1024 products, as a chain of float32 multiply-adds).  Results in float32 get this one.
-template <int BYTE>
 __device__ __forceinline__ floatx16 mma_scaled(const intx8& a, const intx8& b, const floatx16& c, uint32_t ea, uint32_t eb) {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, BYTE, (int)ea, BYTE, (int)eb);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, (int)ea, 0, (int)eb);
 }
-// 2^(e - 127) as float32, for any e of 0 .. 254.
-__device__ __forceinline__ float exp_value(uint32_t e) { return __uint_as_float(e ? e << 23 : 0x00400000u); }
 // Eight e4m3 values times a power of two, as bfloat16.
 __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float scale) {
     const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
@@ -31,32 +27,57 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float scale) {
     return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
 
-// ---- many rows: one tile of 256 columns of the result (rows of W) x 128 of its rows (rows of A) per workgroup of four waves, two workgroups per CU ----
+// ---- many rows: tiles of 256 columns of the result (rows of W) by 64 WN of its rows (rows of A), 2 x WN waves of 128 x 64 each ----
 
-// A slab is 64 bytes of each of the 384 operand rows, a k-step of the scaled instruction; three stages, loaded directly to LDS.  Eight slabs share a word
-// of four powers per row (512 values), which come the same way into two small buffers.
-constexpr int FP_SLAB = 64;
-constexpr int FP_EXP_WORDS = TP_T + NT_COLS;
-constexpr int FP_RING = NT_STAGES * NT_STAGE;
+// A slab is 64 bytes of every operand row, a k-step of the scaled instruction, and two of them are a block of 128 values; they come directly to LDS, several requested ahead. Words of
+// four powers per row (512 values) come the same way into two small buffers.
+//   WN = 4: 256 x 256, one workgroup of eight waves per CU, four stages of 32 KB
+//   WN = 2: 256 x 128, two workgroups of four waves per CU, so that one's stores run beside the other's products; three stages of 24 KB.  It moves half as much again into LDS
+//           per product, which at full rate would be three quarters of what the caches hand a CU.
+template <int WN>
+struct Fp8Tile {
+    static constexpr int COLS = 64 * WN, THREADS = 128 * WN, WAVES = 2 * WN;
+    static constexpr int STAGES = WN == 4 ? 4 : 3, SLAB = 64, ROWS = TP_T + COLS, STAGE = ROWS * SLAB, RING = STAGES * STAGE;
+    static constexpr int LPT = STAGE / 16 / THREADS, LPW = TP_T * SLAB / 16 / THREADS;      // 16-byte loads per thread and slab; of them W's
+    static constexpr int EXP_WORDS = ROWS;
+};
+template <int WN>
+struct Fp8Lane {
+    int tid, lane, wave, wm, wn, half, l32;
+    __device__ __forceinline__ Fp8Lane() {
+        tid = threadIdx.x; lane = tid & 63; wave = tid >> 6;
+        wm = wave & 1; wn = wave >> 1; half = lane >> 5; l32 = lane & 31;
+    }
+    __device__ __forceinline__ int row(int i, int r) const { return acc_row(2 * i + wm, r, half); }
+    __device__ __forceinline__ int col(int c) const { return wn * 64 + c * 32 + l32; }
+};
 
+// One operand of a tile: 64-byte pieces of its rows `pitch` bytes apart, `step` from slab to slab: rows as a caller has them, or by slab (see Fp8Rows).
 struct Fp8Operand {
     const char* base;        // first row of the tile, first slab
-    uint32_t pitch;
+    uint32_t pitch, step;
     int last;                // rows behind it repeat it
     const uint32_t* exps;    // powers of the first row, first word
     int64_t exp_pitch;       // words from one word of a row to its next
 };
-__device__ __forceinline__ Fp8Operand fp8_operand(const uint8_t* p, int64_t ld, const uint32_t* exps, int64_t rows, int64_t row0, int slab0) {
-    return Fp8Operand{reinterpret_cast<const char*>(p) + row0 * ld + (int64_t)slab0 * FP_SLAB, (uint32_t)ld, (int)min((int64_t)TP_T, rows - row0) - 1,
-                      exps + (int64_t)(slab0 >> 3) * rows + row0, rows};
+__device__ __forceinline__ Fp8Operand fp8_operand(const Fp8Rows& q, int64_t rows, int64_t row0, int slab0) {
+    Fp8Operand o;
+    o.base = reinterpret_cast<const char*>(q.at(row0, (int64_t)slab0 * FP_SLAB));
+    o.pitch = q.ld ? (uint32_t)q.ld : FP_SLAB;
+    o.step = q.ld ? FP_SLAB : (uint32_t)FP_SLAB_BYTES;
+    o.last = (int)min((int64_t)TP_T, rows - row0) - 1;
+    o.exps = reinterpret_cast<const uint32_t*>(q.exps) + (int64_t)(slab0 >> 3) * rows + row0;
+    o.exp_pitch = rows;
+    return o;
 }
 
-// acc = tile rows (W) x tile columns (A) over nk > 0 slabs, the first of them at a whole word of powers.  On return every wave is past its LDS reads only after the
-// caller's next barrier.  Needs ring (FP_RING bytes) and exps (2 FP_EXP_WORDS words).
-template <bool EXACT>
+// acc = tile rows (W) x tile columns (A) over nk > 0 slabs, an even number, the first of them at a whole word of powers.  On return every wave is past its LDS reads only after the
+// caller's next barrier.  Needs ring (RING bytes) and exps (2 EXP_WORDS words).
+template <bool EXACT, int WN>
 __device__ __forceinline__ void fp8_product(uint8_t* ring, uint32_t* exps, const Fp8Operand& W, const Fp8Operand& A, int nk, floatx16 (&acc)[4][2]) {
-    constexpr int LPT = NT_STAGE / 16 / NT_THREADS, LPW = TP_T * FP_SLAB / 16 / NT_THREADS, CPR = FP_SLAB / 16, RPI = NT_THREADS / CPR;
-    const NarrowLane t;
+    typedef Fp8Tile<WN> G;
+    constexpr int LPT = G::LPT, LPW = G::LPW, NS = G::STAGES, CPR = FP_SLAB / 16, RPI = G::THREADS / CPR;
+    const Fp8Lane<WN> t;
     nk = __builtin_amdgcn_readfirstlane(nk);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -64,7 +85,7 @@ __device__ __forceinline__ void fp8_product(uint8_t* ring, uint32_t* exps, const
         for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][c][r] = 0;
-    // access j of the workgroup covers RPI rows, 4096 contiguous LDS bytes; thread -> (row, LDS chunk), which holds the global chunk XORed with the swizzle
+    // access j of the workgroup covers RPI rows, RPI * 64 contiguous LDS bytes; thread -> (row, LDS chunk), which holds the global chunk XORed with the swizzle
     const int lrow = t.tid / CPR;
     const uint32_t gch = (uint32_t)((t.tid % CPR) ^ lds_swz<FP_SLAB>(lrow));
     const char* const Wb = uniform(W.base);
@@ -77,15 +98,19 @@ __device__ __forceinline__ void fp8_product(uint8_t* ring, uint32_t* exps, const
         off[j] = (uint32_t)min(r, w ? W.last : A.last) * (w ? W.pitch : A.pitch) + gch * 16;
     }
     const uint32_t wave_lds = __builtin_amdgcn_readfirstlane(lds_addr(ring) + t.wave * 1024);
-    auto issue_one = [&](int st, size_t k, int n) { dma16_to_lds(n < LPW ? Wb + k : Ab + k, off[n], wave_lds + st * NT_STAGE + n * 4096); };
-    // powers: word q of the rows 64 w .. 64 w + 63 of W by wave w, of A's by waves 0 and 1
+    auto request = [&](int stage, int kt, int n) {
+        dma16_to_lds(n < LPW ? Wb + (size_t)kt * W.step : Ab + (size_t)kt * A.step, off[n], wave_lds + stage * G::STAGE + n * (RPI * FP_SLAB));
+    };
+    // words of powers, 64 rows per access: of W's rows, then of A's, dealt out to the waves
     const uint32_t exp_lds = __builtin_amdgcn_readfirstlane(lds_addr(exps) + t.wave * 256);
-    const uint32_t* const we = W.exps + min(t.tid, W.last);
-    const uint32_t* const ae = A.exps + min(t.tid, A.last);
-    auto issue_exps = [&](int q) {
-        const uint32_t dst = exp_lds + (q & 1) * (FP_EXP_WORDS * 4);
-        dma4_to_lds(we + (int64_t)q * W.exp_pitch, dst);
-        if (t.wave < 2) dma4_to_lds(ae + (int64_t)q * A.exp_pitch, dst + TP_T * 4);
+    auto request_exps = [&](int q) {
+        const uint32_t dst = exp_lds + (q & 1) * (G::EXP_WORDS * 4);
+#pragma unroll
+        for (int j = 0; j < (G::ROWS / 64 + G::WAVES - 1) / G::WAVES; ++j) {
+            const int r = (t.wave + j * G::WAVES) * 64 + t.lane;       // (the same side of W and A, and of the end, for a whole wave)
+            if (r < TP_T) dma4_to_lds(W.exps + (int64_t)q * W.exp_pitch + min(r, W.last), dst + j * G::WAVES * 256);
+            else if (r < G::ROWS) dma4_to_lds(A.exps + (int64_t)q * A.exp_pitch + min(r - TP_T, A.last), dst + j * G::WAVES * 256);
+        }
     };
     const int fw_row = t.wm * 32 + t.l32, fa_row = t.wn * 64 + t.l32;
     const int swz = lds_swz<FP_SLAB>(t.l32);
@@ -96,149 +121,227 @@ __device__ __forceinline__ void fp8_product(uint8_t* ring, uint32_t* exps, const
     };
     auto read_w = [&](const uint8_t* st, int i) { return read(st + (fw_row + 64 * i) * FP_SLAB); };
     auto read_a = [&](const uint8_t* st, int c) { return read(st + (TP_T + fa_row + 32 * c) * FP_SLAB); };
-    uint32_t ew[4], ea[2];
+    uint32_t ew[4], ea[2];                          // four powers of each of the lane's rows; and that of the block at hand
+    uint32_t bw[4], ba[2];
     auto read_exps = [&](int q) {
-        const uint32_t* const e = exps + (q & 1) * FP_EXP_WORDS;
+        const uint32_t* const e = exps + (q & 1) * G::EXP_WORDS;
 #pragma unroll
         for (int i = 0; i < 4; ++i) ew[i] = e[fw_row + 64 * i];
 #pragma unroll
         for (int c = 0; c < 2; ++c) ea[c] = e[TP_T + fa_row + 32 * c];
     };
-    // From here to the last slab only direct-to-LDS loads are in flight: they retire in the order of issue, which the partial waits below count on.
-    wait_vmcnt<0>();
-    issue_exps(0);
-    for (int kt = 0; kt < 2 && kt < nk; ++kt) {
+    auto block_exps = [&](int blk) {
+        const int shift = 8 * (blk & 3);
 #pragma unroll
-        for (int n = 0; n < LPT; ++n) issue_one(kt, (size_t)kt * FP_SLAB, n);
-    }
-    int st = 0;
-    for (int k8 = 0; k8 < nk; k8 += 8) {
-        auto step = [&](auto sub_c) {
-            constexpr int SUB = decltype(sub_c)::value, BYTE = SUB >> 1;
-            const int kt = k8 + SUB;
-            if (kt >= nk) return;
-            // every fragment read of the slab before has returned, and slab kt has landed (the one behind it may still fly)
-            __builtin_amdgcn_s_waitcnt(0xC07F);     // lgkmcnt(0)
-            if (kt + 1 < nk) wait_vmcnt<LPT>();
-            else wait_vmcnt<0>();
-            __syncthreads();
-            const uint8_t* const s = ring + st * NT_STAGE;
-            if constexpr (SUB == 0) read_exps(k8 >> 3);
-            if constexpr (SUB == 1) {
-                if (k8 + 8 < nk) issue_exps((k8 >> 3) + 1);      // (the buffer's last words were read a word ago)
+        for (int i = 0; i < 4; ++i) bw[i] = (ew[i] >> shift) & 255u;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) ba[c] = (ea[c] >> shift) & 255u;
+    };
+    const int nb = nk >> 1;
+    int st = 0;                                     // stage of the slab at hand
+    auto stage_after = [](int s, int n) { return s + n >= NS ? s + n - NS : s + n; };
+    // (issued a word ahead of its use; its buffer's words went into registers before)
+    auto next_word = [&](int blk) {
+        if ((blk & 3) == 0 && blk + 4 < nb) request_exps((blk >> 2) + 1);
+    };
+    // at most `flying` slabs requested last may still be on their way
+    auto fence = [&](auto flying_c) {
+        __builtin_amdgcn_s_waitcnt(0xC07F);         // lgkmcnt(0): every fragment read before has returned
+        wait_vmcnt<decltype(flying_c)::value * LPT>();
+        __syncthreads();
+    };
+    typedef std::integral_constant<int, 0> I0;
+    typedef std::integral_constant<int, 1> I1;
+    typedef std::integral_constant<int, NS - 2> Some;
+    // From here to the last slab only direct-to-LDS loads are in flight: they retire in the order of issue, which the partial waits count on.
+    wait_vmcnt<0>();
+    request_exps(0);
+    auto request_all = [&](int kt) {
+#pragma unroll
+        for (int n = 0; n < LPT; ++n) request(kt, kt, n);
+    };
+    request_all(0);
+    request_all(1);
+    if constexpr (!EXACT) {
+        // A slab's fragments are read while the slab before is multiplied: A's and W's last into registers of their own (by parity of the slab), W's others into
+        // those whose products have just been issued.  The slab NS ahead goes to the stage whose slab is in registers.
+        intx8 w0[3], w3[2], fa[2][2];
+        if (nb > 1) {
+#pragma unroll
+            for (int k = 2; k < NS; ++k) request_all(k);
+            fence(std::integral_constant<int, NS - 1>{});
+        } else {
+            fence(I1{});
+        }
+        read_exps(0);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) fa[0][c] = read_a(ring, c);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) w0[i] = read_w(ring, i);
+        w3[0] = read_w(ring, 3);
+        // one slab: NEXT: there is another, whose fragments are read; MORE: slab kt + NS is requested
+        auto step = [&](int blk, auto cur_c, auto next_c, auto more_c) {
+            constexpr int CUR = decltype(cur_c)::value, NXT = CUR ^ 1, NEXT = decltype(next_c)::value, MORE = decltype(more_c)::value;
+            const uint8_t* const s = ring + stage_after(st, 1) * G::STAGE;
+            const int ahead = 2 * blk + CUR + NS;
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                const int i = m >> 1, c = m & 1;
+                acc[i][c] = mma_scaled(i < 3 ? w0[i < 3 ? i : 0] : w3[CUR], fa[CUR][c], acc[i][c], bw[i], ba[c]);
+                if constexpr (NEXT) {
+                    if (m < 2) fa[NXT][m] = read_a(s, m);
+                    else if (m == 2) w3[NXT] = read_w(s, 3);
+                    else if (m < 6) w0[m - 3] = read_w(s, m - 3);
+                }
+                if constexpr (MORE) {
+                    if (m < LPT) request(st, ahead, m);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            const int st2 = st == 0 ? 2 : st - 1;
-            const int more = __builtin_amdgcn_readfirstlane(kt + 2 < nk ? 1 : 0);
-            const size_t k2 = (size_t)(kt + 2) * FP_SLAB;
-            auto dma = [&](int n) {
-                if (more != 0) issue_one(st2, k2, n);
-            };
+            // (the next block's word of powers, its own again or another: a branch here, and the compiler moves the products behind it)
+            if constexpr (CUR == 1 && NEXT) read_exps((blk + 1) >> 2);
+            st = stage_after(st, 1);
+        };
+        int blk = 0;
+        for (; blk + 2 < nb; ++blk) {
+            fence(Some{});
+            block_exps(blk);
+            next_word(blk);
+            step(blk, I0{}, I1{}, I1{});
+            fence(Some{});
+            step(blk, I1{}, I1{}, I1{});
+        }
+        if (blk + 1 < nb) {
+            fence(Some{});
+            block_exps(blk);
+            step(blk, I0{}, I1{}, std::integral_constant<int, NS == 3>{});
+            fence(I1{});
+            step(blk, I1{}, I1{}, I0{});
+            ++blk;
+        }
+        fence(I0{});
+        block_exps(blk);
+        step(blk, I0{}, I1{}, I0{});
+        step(blk, I1{}, I0{}, I0{});
+    } else {
+        // One slab after the other: widening takes the registers that fragments of the next would need.  The slab NS - 1 ahead goes to the stage of the slab before.
+        if (NS == 4 && nb > 1) request_all(2);
+        auto step = [&](int blk, auto cur_c, auto more_c) {
+            constexpr int CUR = decltype(cur_c)::value;
+            const uint8_t* const s = ring + st * G::STAGE;
+            const int to = stage_after(st, NS - 1), ahead = 2 * blk + CUR + NS - 1;
+            if constexpr (CUR == 0) {
+                if ((blk & 3) == 0) read_exps(blk >> 2);
+            }
             intx8 fa[2], fw[4];
 #pragma unroll
             for (int c = 0; c < 2; ++c) fa[c] = read_a(s, c);
 #pragma unroll
             for (int i = 0; i < 4; ++i) fw[i] = read_w(s, i);
-            if constexpr (!EXACT) {
+            if constexpr (CUR == 0) block_exps(blk);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bf16x8 a[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) a[c] = widen((uint32_t)fa[c][2 * j], (uint32_t)fa[c][2 * j + 1], exp_value(ba[c]));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    const bf16x8 w = widen((uint32_t)fw[i][2 * j], (uint32_t)fw[i][2 * j + 1], exp_value(bw[i]));
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) acc[i][c] = mma_scaled<BYTE>(fw[i], fa[c], acc[i][c], ew[i], ea[c]);
-                    dma(i);
+                    for (int c = 0; c < 2; ++c) acc[i][c] = mma_chunk(w, a[c], acc[i][c]);
                 }
-#pragma unroll
-                for (int n = 4; n < LPT; ++n) dma(n);
-            } else {
-                float sa[2], sw[4];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) sa[c] = exp_value((ea[c] >> (8 * BYTE)) & 255u);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sw[i] = exp_value((ew[i] >> (8 * BYTE)) & 255u);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    bf16x8 a[2];
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) a[c] = widen((uint32_t)fa[c][2 * j], (uint32_t)fa[c][2 * j + 1], sa[c]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const bf16x8 w = widen((uint32_t)fw[i][2 * j], (uint32_t)fw[i][2 * j + 1], sw[i]);
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) acc[i][c] = mma_chunk(w, a[c], acc[i][c]);
-                    }
-                    dma(j);
+                if constexpr (decltype(more_c)::value) {
+                    request(to, ahead, j);
+                    if (j < LPT - 4) request(to, ahead, 4 + j);
                 }
-#pragma unroll
-                for (int n = 4; n < LPT; ++n) dma(n);
             }
-            st = st == 2 ? 0 : st + 1;
+            st = stage_after(st, 1);
         };
-        step(std::integral_constant<int, 0>{});
-        step(std::integral_constant<int, 1>{});
-        step(std::integral_constant<int, 2>{});
-        step(std::integral_constant<int, 3>{});
-        step(std::integral_constant<int, 4>{});
-        step(std::integral_constant<int, 5>{});
-        step(std::integral_constant<int, 6>{});
-        step(std::integral_constant<int, 7>{});
+        int blk = 0;
+        for (; blk + 2 < nb; ++blk) {
+            fence(Some{});
+            next_word(blk);
+            step(blk, I0{}, I1{});
+            fence(Some{});
+            step(blk, I1{}, I1{});
+        }
+        if (blk + 1 < nb) {
+            fence(Some{});
+            step(blk, I0{}, I1{});
+            fence(Some{});
+            step(blk, I1{}, std::integral_constant<int, NS == 3>{});
+            ++blk;
+        }
+        fence(I1{});
+        step(blk, I0{}, I0{});
+        fence(I0{});
+        step(blk, I1{}, I0{});
     }
 }
 
-struct Fp8Params {
-    const uint8_t* A;          // e4m3 rows, or values that the call quantises (few rows only)
-    const uint32_t* a_exp;
-    const uint8_t* W;
-    const uint32_t* w_exp;
-    const float* bias;         // may be null
+// A product, cut along its contracted axis into `splits` parts that have a result each.
+struct Fp8Job {
+    Fp8Rows A, W;
     void* out;
-    int64_t lda, ldw, ldo;     // elements
-    int64_t split_pitch;       // elements from one part of the contracted axis to the next: each has a result of its own
-    int N, V, K;
+    int64_t ldo;               // elements
+    int64_t split_pitch;       // elements from one part's result to the next
+    int N, V;                  // rows and columns of the result
     int slabs, per_split;      // slabs in all, and of a part (a multiple of 8)
     int na, nb, ga;            // tiles of rows and of columns of the result, row tiles per group
     int splits;
 };
+template <int WN>
+inline void fp8_tiles(Fp8Job& j) {
+    j.na = (j.N + Fp8Tile<WN>::COLS - 1) / Fp8Tile<WN>::COLS;
+    j.nb = (j.V + TP_T - 1) / TP_T;
+    j.ga = 1024 / Fp8Tile<WN>::COLS;
+}
+inline long long fp8_units(const Fp8Job& j) { return (long long)j.na * j.nb * j.splits; }
 
-// The result leaves through LDS, in rows of 512 bytes or more, past the caches where it is larger than the memory-side cache.
-template <bool EXACT, typename OT, bool PAST>
-__global__ __launch_bounds__(NT_THREADS, 2) void fp8_tile_kernel(Fp8Params p) {
-    __shared__ __attribute__((aligned(1024))) uint8_t s_ring[FP_RING];
-    __shared__ __attribute__((aligned(16))) uint32_t s_exps[2 * FP_EXP_WORDS];
-    __shared__ __attribute__((aligned(16))) float s_bs[TP_T];
-    int u, at, bt;
-    if (!xcd_unit(p.na * p.nb * p.splits, u)) return;
-    const int split = u / (p.na * p.nb);
-    tile_of_unit(u - split * p.na * p.nb, p.na, p.nb, p.ga, at, bt);
-    const NarrowLane t;
-    const int n0 = at * NT_COLS, v0 = bt * TP_T;
-    s_bs[t.tid] = p.bias ? p.bias[min(v0 + t.tid, p.V - 1)] : 0.f;
-    floatx16 acc[4][2];
-    const int k0 = split * p.per_split;
-    fp8_product<EXACT>(s_ring, s_exps, fp8_operand(p.W, p.ldw, p.w_exp, p.V, v0, k0), fp8_operand(p.A, p.lda, p.a_exp, p.N, n0, k0),
-                       min(p.per_split, p.slabs - k0), acc);
-    // rows of 256 values through the ring: all 128 in bfloat16, 64 at a time in float32; 8-byte pieces (16-byte in float32) XORed with the row, so that the 32
+// Unit u of a job into acc; at, bt: its tile, split: its part.
+template <bool EXACT, int WN>
+__device__ __forceinline__ void fp8_unit(const Fp8Job& j, int u, uint8_t* ring, uint32_t* exps, floatx16 (&acc)[4][2], int& n0, int& v0, int& split) {
+    const int tiles = j.na * j.nb;
+    int at, bt;
+    split = u / tiles;
+    tile_of_unit(u - split * tiles, j.na, j.nb, j.ga, at, bt);
+    n0 = at * Fp8Tile<WN>::COLS;
+    v0 = bt * TP_T;
+    const int k0 = split * j.per_split;
+    fp8_product<EXACT, WN>(ring, exps, fp8_operand(j.W, j.V, v0, k0), fp8_operand(j.A, j.N, n0, k0),
+                           min(j.per_split, j.slabs - k0), acc);
+}
+
+// A tile's results to memory through LDS, in rows of 512 bytes or more; PAST: past the caches (where the result is larger than the memory-side cache).
+// bias: of the tile's 256 columns, in LDS, or null.
+template <int WN, typename OT, bool PAST>
+__device__ __forceinline__ void fp8_store(uint8_t* ring, const floatx16 (&acc)[4][2], const float* bias, OT* out, int64_t ldo, int n0, int v0, int N, int V) {
+    typedef Fp8Tile<WN> G;
+    const Fp8Lane<WN> t;
+    // rows of 256 values: all of the tile's in bfloat16, half of them at a time in float32; 8-byte pieces (16-byte in float32) XORed with the row, so that the 32
     // rows of a store lie on different banks
     constexpr int PASSES = sizeof(OT) == 4 ? 2 : 1;
-    constexpr int ROWS = NT_COLS / PASSES, ROW_BYTES = TP_T * sizeof(OT);
-    static_assert(ROWS * ROW_BYTES <= FP_RING, "the values fit the ring");
-    OT* const out = reinterpret_cast<OT*>(p.out) + split * p.split_pitch;
+    constexpr int ROWS = G::COLS / PASSES, ROW_BYTES = TP_T * sizeof(OT);
+    static_assert(ROWS * ROW_BYTES <= G::RING, "the values fit the ring");
 #pragma unroll 1
     for (int h = 0; h < PASSES; ++h) {
-        if (n0 + h * ROWS >= p.N) break;
+        if (n0 + h * ROWS >= N) break;
         __syncthreads();
-        if (PASSES == 1 || t.wn == h) {
+        if (t.wn * 64 / ROWS == h) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const int v = t.row(i, r);
-                    const float4 b = *reinterpret_cast<const float4*>(&s_bs[v]);
+                    const float4 b = bias ? *reinterpret_cast<const float4*>(&bias[v]) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const float4 y = make_float4(acc[i][c][r] + b.x, acc[i][c][r + 1] + b.y, acc[i][c][r + 2] + b.z, acc[i][c][r + 3] + b.w);
                         const int n = t.col(c) % ROWS;
                         if constexpr (sizeof(OT) == 4)
-                            *reinterpret_cast<float4*>(s_ring + n * ROW_BYTES + (((v >> 2) ^ (n & 15)) << 4)) = y;
+                            *reinterpret_cast<float4*>(ring + n * ROW_BYTES + (((v >> 2) ^ (n & 15)) << 4)) = y;
                         else
-                            *reinterpret_cast<uint2*>(s_ring + n * ROW_BYTES + (((v >> 2) ^ ((n & 15) << 1)) << 3)) =
+                            *reinterpret_cast<uint2*>(ring + n * ROW_BYTES + (((v >> 2) ^ ((n & 15) << 1)) << 3)) =
                                 make_uint2(bf16_bits(y.x) | (uint32_t)bf16_bits(y.y) << 16, bf16_bits(y.z) | (uint32_t)bf16_bits(y.w) << 16);
                     }
                 }
@@ -247,13 +350,48 @@ __global__ __launch_bounds__(NT_THREADS, 2) void fp8_tile_kernel(Fp8Params p) {
         // 16 bytes per lane, neighbouring lanes along a row
         constexpr int EPL = 16 / sizeof(OT), LPR = TP_T / EPL, RPW = 64 / LPR;      // elements per lane, lanes per row, rows per wave access
 #pragma unroll 4
-        for (int k = 0; k < ROWS / (4 * RPW); ++k) {
-            const int n = (k * 4 + t.wave) * RPW + t.lane / LPR, ch = t.lane % LPR;
-            const uint4 w = *reinterpret_cast<const uint4*>(s_ring + n * ROW_BYTES + ((ch ^ (n & 15)) << 4));
+        for (int k = 0; k < ROWS / (G::WAVES * RPW); ++k) {
+            const int n = (k * G::WAVES + t.wave) * RPW + t.lane / LPR, ch = t.lane % LPR;
+            const uint4 w = *reinterpret_cast<const uint4*>(ring + n * ROW_BYTES + ((ch ^ (n & 15)) << 4));
             const int row = n0 + h * ROWS + n;
-            if (row < p.N && v0 + ch * EPL < p.V) store16<OT, PAST>(out + (int64_t)row * p.ldo + v0 + ch * EPL, w, p.V - v0 - ch * EPL);
+            if (row < N && v0 + ch * EPL < V) store16<OT, PAST>(out + (int64_t)row * ldo + v0 + ch * EPL, w, V - v0 - ch * EPL);
         }
     }
+}
+
+// Logits.
+template <bool EXACT, int WN, typename OT, bool PAST>
+__global__ __launch_bounds__(Fp8Tile<WN>::THREADS, 2) void fp8_tile_kernel(Fp8Job j, const float* bias) {
+    typedef Fp8Tile<WN> G;
+    __shared__ __attribute__((aligned(1024))) uint8_t s_ring[G::RING];
+    __shared__ __attribute__((aligned(16))) uint32_t s_exps[2 * G::EXP_WORDS];
+    __shared__ __attribute__((aligned(16))) float s_bs[TP_T];
+    int u, n0, v0, split;
+    if (!xcd_unit(j.na * j.nb, u)) return;
+    floatx16 acc[4][2];
+    fp8_unit<EXACT, WN>(j, u, s_ring, s_exps, acc, n0, v0, split);
+    const int tid = threadIdx.x;
+    if (tid < TP_T) s_bs[tid] = bias ? bias[min(v0 + tid, j.V - 1)] : 0.f;      // (published by the store's first barrier)
+    fp8_store<WN, OT, PAST>(s_ring, acc, s_bs, reinterpret_cast<OT*>(j.out), j.ldo, n0, v0, j.N, j.V);
+}
+
+// The two products of a backward in one launch, so that one's last units run beside the other's first: every XCD takes an eighth of either job, `first`'s units before
+// `second`'s (either may have none).  Uncut results are of type OT, parts float32.
+template <bool EXACT, typename OT>
+__global__ __launch_bounds__(Fp8Tile<4>::THREADS, 2) void fp8_grads_kernel(Fp8Job first, Fp8Job second, int n_first, int n_second) {
+    typedef Fp8Tile<4> G;
+    __shared__ __attribute__((aligned(1024))) uint8_t s_ring[G::RING];
+    __shared__ __attribute__((aligned(16))) uint32_t s_exps[2 * G::EXP_WORDS];
+    int u, n0, v0, split;
+    if (!xcd_unit(n_first, n_second, u)) return;
+    const bool other = u >= n_first;
+    const Fp8Job& j = other ? second : first;
+    floatx16 acc[4][2];
+    fp8_unit<EXACT, 4>(j, other ? u - n_first : u, s_ring, s_exps, acc, n0, v0, split);
+    if (j.splits > 1)
+        fp8_store<4, float, false>(s_ring, acc, nullptr, reinterpret_cast<float*>(j.out) + split * j.split_pitch, j.ldo, n0, v0, j.N, j.V);
+    else
+        fp8_store<4, OT, false>(s_ring, acc, nullptr, reinterpret_cast<OT*>(j.out), j.ldo, n0, v0, j.N, j.V);
 }
 
 // Sum of the parts of a product whose contracted axis was cut, in order, rounded once.
@@ -290,11 +428,22 @@ constexpr int FEWF_LDS = 76 * 1024;               // of the rows of A: two workg
 // LDS bytes of a row: padded so that the 32 rows of a fragment read lie on different banks
 inline int fewf_stride(int64_t K) { return (int)((K + 127) / 128 * 256 + 16); }
 
+struct Fp8FewParams {
+    const uint8_t* A;          // e4m3 rows, or values that the call quantises
+    const uint32_t* a_exp;
+    const uint8_t* W;
+    const uint32_t* w_exp;
+    const float* bias;         // may be null
+    void* out;
+    int64_t lda, ldw, ldo;     // elements
+    int N, V, K;
+    int blocks;                // of 128 along K
+};
 template <typename T, typename OT>
-__global__ __launch_bounds__(FEWF_THREADS, 2) void fp8_few_kernel(Fp8Params p, int stride, int n_tiles) {
+__global__ __launch_bounds__(FEWF_THREADS, 2) void fp8_few_kernel(Fp8FewParams p, int stride, int n_tiles) {
     __shared__ __attribute__((aligned(16))) uint8_t s_a[FEWF_LDS];       // [N][stride]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
-    const int nks = p.slabs * 2;                  // chunks of 32 values
+    const int nks = p.blocks * 4;                 // chunks of 32 values
     int tile = blockIdx.x;
     int v = tile * FEWF_COLS + wave * 32 + l32;
     int vc = min(v, p.V - 1);
@@ -310,7 +459,7 @@ __global__ __launch_bounds__(FEWF_THREADS, 2) void fp8_few_kernel(Fp8Params p, i
     load_w(w0, e0, 0);
     // chunk of 8 values of row r at byte 16 (c / 8) of the row
     if constexpr (sizeof(T) == 1) {
-        const int cpr = p.slabs * 8;
+        const int cpr = p.blocks * 16;
         for (int i = tid; i < p.N * cpr; i += FEWF_THREADS) {
             const int r = i / cpr, c = i - r * cpr;
             const uint2 q = *reinterpret_cast<const uint2*>(p.A + (int64_t)r * p.lda + c * 8);
@@ -318,19 +467,16 @@ __global__ __launch_bounds__(FEWF_THREADS, 2) void fp8_few_kernel(Fp8Params p, i
             *reinterpret_cast<bf16x8*>(s_a + r * stride + c * 16) = widen(q.x, q.y, exp_value(e));
         }
     } else {
-        const int cols = p.slabs * 64;
+        const int cols = p.blocks * 128;
 #pragma unroll 1
         for (int r = wave; r < p.N; r += FEWF_THREADS / 64) {
             const T* const row = reinterpret_cast<const T*>(p.A) + (int64_t)r * p.lda;
 #pragma unroll 1
             for (int c = lane * 8; c - lane * 8 < cols; c += 512) {
-                float x[8];
-                load8_any(row, c, p.K, x);
-                const uint32_t e = block_exp(max16(finite_max8(x)));
-                const float f = block_factor(e);
-                if (c < cols)
-                    *reinterpret_cast<bf16x8*>(s_a + r * stride + c * 2) =
-                        widen(e4m3x4(x[0], x[1], x[2], x[3], f), e4m3x4(x[4], x[5], x[6], x[7], f), exp_value(e));
+                Eight<T> x;
+                x.load(row, c, p.K);
+                const float e = exp_value(block_exp(row_most(x)));
+                if (c < cols) *reinterpret_cast<bf16x8*>(s_a + r * stride + c * 2) = widen(x.four(0, e), x.four(4, e), e);
             }
         }
     }

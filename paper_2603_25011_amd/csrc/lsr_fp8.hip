@@ -17,6 +17,8 @@ constexpr int64_t MAX_AXIS = int64_t(1) << 22;
 constexpr int64_t MAX_VALUES = int64_t(1) << 36;
 constexpr int64_t MAX_HIDDEN = 65536;
 constexpr int64_t MAX_LD = int64_t(1) << 23;
+// Logits in tiles of 256 x 256 from that many slabs of 64 values on.
+constexpr int WIDE_SLABS = 64;
 constexpr size_t CACHE_BYTES = size_t(1) << 28;       // the memory-side cache
 
 inline bool float_type(int32_t t) { return t == LSR_F32 || t == LSR_BF16; }
@@ -28,22 +30,21 @@ inline bool matrix(int64_t rows, int64_t cols) {
 }
 inline int64_t exp_bytes(int64_t rows, int64_t cols) { return 4 * rows * ((cols + 511) / 512); }
 
-struct Rows {                 // e4m3 rows and their powers
-    uint8_t* q;
-    int64_t ld;
-    uint32_t* exps;
-};
+// e4m3 rows of `cols` values, ld apart or (ld = 0) by slab.
+Fp8Rows fp8_rows(const void* q, int64_t ld, const void* exps, int64_t cols) {
+    return Fp8Rows{static_cast<uint8_t*>(const_cast<void*>(q)), ld, up(cols, 128) / FP_SLAB, static_cast<uint8_t*>(const_cast<void*>(exps))};
+}
+inline int64_t slab_bytes(int64_t rows, int64_t cols) { return up(rows, 256) * up(cols, 128); }
 
 template <typename T>
-int quantize_as(int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Rows& q, const Rows& qt, float* sums, hipStream_t st) {
+int quantize_as(int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Fp8Rows& q, const Fp8Rows& qt, float* sums, hipStream_t st) {
     if (!square && q.q && !qt.q && !sums) {
-        fp8_rows_kernel<T><<<(unsigned)((rows + 3) / 4), FQ_THREADS, 0, st>>>(static_cast<const T*>(X), ldx, rows, (int)cols, q.q, q.ld, q.exps);
+        fp8_rows_kernel<T><<<(unsigned)((rows + 3) / 4), FQ_THREADS, 0, st>>>(static_cast<const T*>(X), ldx, rows, (int)cols, q);
         return launch_status();
     }
     Fp8TileParams p = {};
     p.X = X; p.ldx = ldx; p.rows = rows; p.cols = cols;
-    p.Q = q.q; p.ldq = q.ld; p.E = reinterpret_cast<uint8_t*>(q.exps);
-    p.Qt = qt.q; p.ldqt = qt.ld; p.Et = reinterpret_cast<uint8_t*>(qt.exps);
+    p.Q = q; p.Qt = qt;
     p.sums = sums;
     p.row_tiles = (int)((rows + 127) / 128); p.col_tiles = (int)((cols + 127) / 128);
     const unsigned grid = (unsigned)((int64_t)p.row_tiles * p.col_tiles);
@@ -52,75 +53,118 @@ int quantize_as(int64_t rows, int64_t cols, const void* X, int64_t ldx, bool squ
     else fp8_tile_quantize_kernel<T, false, false><<<grid, FQ_THREADS, 0, st>>>(p);
     return launch_status();
 }
-int quantize(int32_t type, int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Rows& q, const Rows& qt, float* sums, hipStream_t st) {
+int quantize(int32_t type, int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Fp8Rows& q, const Fp8Rows& qt, float* sums, hipStream_t st) {
     return type == LSR_F32 ? quantize_as<float>(rows, cols, X, ldx, square, q, qt, sums, st)
                            : quantize_as<uint16_t>(rows, cols, X, ldx, square, q, qt, sums, st);
 }
 
 // ---- products ----
 
-// Parts of the contracted axis: enough tiles to fill the chip where there are few, no part shorter than 16 slabs, whole words of powers each.  A part's tiles write their
-// sums in float32 and a second launch joins them, which costs about PART_COST slabs' time per tile.
-struct Parts { int splits, per; };
-constexpr int64_t SLOTS = 512;       // workgroups that are resident at once on the 256 CUs it is made for: the size of a workspace does not depend on the device
-constexpr int64_t PART_COST = 24;
-constexpr int MAX_PARTS = 64;
-Parts parts_of(int64_t N, int64_t V, int64_t slabs) {
-    const int64_t tiles = ((N + NT_COLS - 1) / NT_COLS) * ((V + TP_T - 1) / TP_T);
-    Parts best = {1, (int)up(slabs, 8)};
+Fp8Job job(int64_t N, int64_t V, int64_t K, const Fp8Rows& A, const Fp8Rows& W, void* out, int64_t ldo) {
+    Fp8Job j = {};
+    j.A = A; j.W = W;
+    j.out = out; j.ldo = ldo;
+    j.N = (int)N; j.V = (int)V;
+    j.slabs = j.per_split = (int)(up(K, 128) / FP_SLAB);
+    j.splits = 1;
+    return j;
+}
+
+template <bool EXACT, int WN, typename OT>
+int launch_logits(Fp8Job& j, const float* bias, hipStream_t st) {
+    fp8_tiles<WN>(j);
+    const unsigned grid = xcd_grid(fp8_units(j));
+    if ((size_t)j.N * j.V * sizeof(OT) >= CACHE_BYTES) fp8_tile_kernel<EXACT, WN, OT, true><<<grid, Fp8Tile<WN>::THREADS, 0, st>>>(j, bias);
+    else fp8_tile_kernel<EXACT, WN, OT, false><<<grid, Fp8Tile<WN>::THREADS, 0, st>>>(j, bias);
+    return launch_status();
+}
+int logits(Fp8Job& j, const float* bias, int32_t out_type, hipStream_t st) {
+    const bool wide = j.slabs >= WIDE_SLABS;
+    if (out_type == LSR_F32) return wide ? launch_logits<true, 4, float>(j, bias, st) : launch_logits<true, 2, float>(j, bias, st);
+    return wide ? launch_logits<false, 4, uint16_t>(j, bias, st) : launch_logits<false, 2, uint16_t>(j, bias, st);
+}
+
+// The launch of a backward's two products: dH (contracted over the vocabulary) and dW (over the tokens), tiles of 256 x 256, one workgroup per CU at a time.  Either may be
+// cut along its contracted axis, into whole words of powers; a part then writes float32 sums, which a second launch joins.  Chosen is what ends first when units are handed
+// out in order, the longer kind first: a unit costs its slabs, START slabs' time for its beginning and end, and a part PART more for its
+// sums, which are written and read again.
+struct Cut { int splits, per; };
+struct GradsPlan { Cut h, w; bool h_first; };
+constexpr int CUS = 256;             // CUs that it is made for: the size of a workspace does not depend on the device
+constexpr int START = 12, PART = 10;
+constexpr int64_t PART_VALUES = int64_t(1) << 29;
+Cut cut(int64_t slabs, int k) {
+    const int per = (int)up((slabs + k - 1) / k, 8);
+    return Cut{(int)((slabs + per - 1) / per), per};
+}
+// When n1 units of length l1 and then n2 of l2 are done on CUS CUs.
+int64_t end_of(int64_t n1, int64_t l1, int64_t n2, int64_t l2) {
+    const int64_t q = n1 / CUS, r = n1 % CUS;      // r CUs have q + 1 of the first kind, the others q
+    const int64_t t1 = (q + (r ? 1 : 0)) * l1;
+    if (!n2) return t1;
+    // rounds k of the second kind: behind q units of the first on CUS - r CUs, and on the r others as many as end by then
+    for (int64_t k = (n2 + CUS - 1) / CUS;; ++k) {
+        const int64_t ta = q * l1 + k * l2;
+        const int64_t others = r && ta > (q + 1) * l1 ? (ta - (q + 1) * l1) / l2 : 0;
+        if (k * (CUS - r) + others * r >= n2) return ta > t1 ? ta : t1;
+        const int64_t tb = (q + 1) * l1 + k * l2;      // (when the r others end their k-th)
+        if (r && (tb - q * l1) / l2 * (CUS - r) + k * r >= n2) return tb;
+    }
+}
+GradsPlan grads_plan(int64_t N, int64_t V, int64_t D, bool dh, bool dw) {
+    const int64_t sh = up(V, 128) / FP_SLAB, sw = up(N, 128) / FP_SLAB;
+    const int64_t nd = (D + TP_T - 1) / TP_T;
+    const int64_t th = dh ? (N + 255) / 256 * nd : 0, tw = dw ? (V + 255) / 256 * nd : 0;
+    static const int tries[] = {1, 2, 3, 4, 5, 6, 8, 12, 16, 24, 32};
+    GradsPlan best = {Cut{1, (int)up(sh, 8)}, Cut{1, (int)up(sw, 8)}, true};
     int64_t least = -1;
-    for (int64_t k = 1; k <= MAX_PARTS; ++k) {
-        const int64_t per = up((slabs + k - 1) / k, 8);
-        if (k > 1 && (per < 16 || k * N * V > (int64_t(1) << 29))) break;
-        const int64_t n = (slabs + per - 1) / per;
-        const int64_t rounds = (tiles * n + SLOTS - 1) / SLOTS;
-        const int64_t t = rounds * (per + 12 + (n > 1 ? PART_COST : 0));
-        if (least < 0 || t < least) { least = t; best = {(int)n, (int)per}; }
+    for (int kh : tries) {
+        const Cut h = cut(sh, kh);
+        if (kh > 1 && (!dh || h.splits < 2 || h.per < 16 || h.splits * N * D > PART_VALUES)) break;
+        for (int kw : tries) {
+            const Cut w = cut(sw, kw);
+            if (kw > 1 && (!dw || tw >= CUS || w.splits < 2 || w.per < 16 || w.splits * V * D > PART_VALUES)) break;
+            const int64_t lh = h.per + START + (h.splits > 1 ? PART : 0), lw = w.per + START + (w.splits > 1 ? PART : 0);
+            const bool first = lh >= lw;
+            const int64_t t = first ? end_of(th * h.splits, lh, tw * w.splits, lw) : end_of(tw * w.splits, lw, th * h.splits, lh);
+            if (least < 0 || t < least) { least = t; best = {h, w, first}; }
+        }
     }
     return best;
 }
-size_t parts_bytes(int64_t N, int64_t V, int64_t slabs) {
-    const Parts p = parts_of(N, V, slabs);
-    return p.splits > 1 ? align_up((size_t)p.splits * up(N * V, 4) * 4) : 0;
-}
+size_t part_bytes(const Cut& c, int64_t n) { return c.splits > 1 ? align_up((size_t)c.splits * up(n, 4) * 4) : 0; }
 
-// out [N, ldo] = A W^T + bias over `slabs` slabs; parts: where they are joined (then out is contiguous and there is no bias), or NULL.
-int product(int64_t N, int64_t V, int64_t slabs, const Rows& A, const Rows& W, const float* bias, int32_t out_type, void* out, int64_t ldo, float* parts,
-            hipStream_t st) {
-    Fp8Params p = {};
-    p.A = A.q; p.lda = A.ld; p.a_exp = A.exps;
-    p.W = W.q; p.ldw = W.ld; p.w_exp = W.exps;
-    p.bias = bias; p.out = out; p.ldo = ldo;
-    p.N = (int)N; p.V = (int)V; p.slabs = (int)slabs;
-    p.na = (int)((N + NT_COLS - 1) / NT_COLS); p.nb = (int)((V + TP_T - 1) / TP_T); p.ga = 8;
-    const Parts cut = parts ? parts_of(N, V, slabs) : Parts{1, (int)slabs};
-    p.splits = cut.splits; p.per_split = cut.per;
-    const unsigned grid = xcd_grid((long long)p.na * p.nb * p.splits);
-    if (p.splits > 1) {
-        const int64_t n = N * V;
-        p.out = parts; p.ldo = V; p.split_pitch = up(n, 4);
-        if (out_type == LSR_F32) fp8_tile_kernel<true, float, false><<<grid, NT_THREADS, 0, st>>>(p);
-        else fp8_tile_kernel<false, float, false><<<grid, NT_THREADS, 0, st>>>(p);
-        const unsigned joins = (unsigned)((n + 1023) / 1024);
-        if (out_type == LSR_F32) fp8_join_kernel<float><<<joins, 256, 0, st>>>(parts, p.split_pitch, p.splits, n, static_cast<float*>(out));
-        else fp8_join_kernel<uint16_t><<<joins, 256, 0, st>>>(parts, p.split_pitch, p.splits, n, static_cast<uint16_t*>(out));
-        return launch_status();
-    }
-    const bool past = (size_t)N * V * type_bytes(out_type) >= CACHE_BYTES;
-    if (out_type == LSR_F32) {
-        if (past) fp8_tile_kernel<true, float, true><<<grid, NT_THREADS, 0, st>>>(p);
-        else fp8_tile_kernel<true, float, false><<<grid, NT_THREADS, 0, st>>>(p);
-    } else {
-        if (past) fp8_tile_kernel<false, uint16_t, true><<<grid, NT_THREADS, 0, st>>>(p);
-        else fp8_tile_kernel<false, uint16_t, false><<<grid, NT_THREADS, 0, st>>>(p);
-    }
+// Both products of a backward, dh and dw without cuts or parts as yet; a job without units (N = 0) is none.
+template <bool EXACT, typename OT>
+int launch_grads(Fp8Job h, Fp8Job w, const GradsPlan& plan, float* h_parts, float* w_parts, hipStream_t st) {
+    auto prepare = [](Fp8Job& j, const Cut& c, float* parts) -> int {
+        if (!j.N) return 0;
+        j.splits = c.splits;
+        j.per_split = c.per;
+        if (c.splits > 1) { j.out = parts; j.split_pitch = up((int64_t)j.N * j.V, 4); }
+        fp8_tiles<4>(j);
+        return (int)fp8_units(j);
+    };
+    void* const dH = h.out;
+    void* const dW = w.out;
+    const int nh = prepare(h, plan.h, h_parts), nw = prepare(w, plan.w, w_parts);
+    const unsigned grid = xcd_grid(nh) + xcd_grid(nw);
+    if (plan.h_first) fp8_grads_kernel<EXACT, OT><<<grid, Fp8Tile<4>::THREADS, 0, st>>>(h, w, nh, nw);
+    else fp8_grads_kernel<EXACT, OT><<<grid, Fp8Tile<4>::THREADS, 0, st>>>(w, h, nw, nh);
+    auto join = [&](const Fp8Job& j, const float* parts, void* out) {
+        if (!j.N || j.splits < 2) return;
+        const int64_t n = (int64_t)j.N * j.V;
+        fp8_join_kernel<OT><<<(unsigned)((n + 1023) / 1024), 256, 0, st>>>(parts, j.split_pitch, j.splits, n, static_cast<OT*>(out));
+    };
+    join(h, h_parts, dH);
+    join(w, w_parts, dW);
     return launch_status();
 }
 
 bool few(int64_t N, int64_t K) { return N <= FEWF_ROWS && N * fewf_stride(K) <= FEWF_LDS; }
 
 template <typename T>
-void launch_few(const Fp8Params& p, int32_t out_type, int n_cus, hipStream_t st) {
+void launch_few(const Fp8FewParams& p, int32_t out_type, int n_cus, hipStream_t st) {
     const int n_tiles = (p.V + FEWF_COLS - 1) / FEWF_COLS;
     const unsigned grid = (unsigned)(n_tiles < 2 * n_cus ? n_tiles : 2 * n_cus);
     if (out_type == LSR_F32) fp8_few_kernel<T, float><<<grid, FEWF_THREADS, 0, st>>>(p, fewf_stride(p.K), n_tiles);
@@ -136,24 +180,24 @@ MatmulWs matmul_ws(int64_t N, int64_t K) {
     return w;
 }
 
-struct BackwardWs { size_t g, g_exp, gt, gt_exp, ht, ht_exp, sums, parts, total; };
-BackwardWs backward_ws(int64_t N, int64_t V, int64_t D, bool dh, bool dw, bool db) {
+struct BackwardWs { size_t g, g_exp, gt, gt_exp, ht, ht_exp, sums, h_parts, w_parts, total; };
+BackwardWs backward_ws(int64_t N, int64_t V, int64_t D, bool dh, bool dw, bool db, const GradsPlan& plan) {
     BackwardWs w = {};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes); return o; };
     if (dh) {
-        w.g = take((size_t)N * up(V, 128));
+        w.g = take((size_t)slab_bytes(N, V));
         w.g_exp = take((size_t)exp_bytes(N, V));
     }
     if (dw) {
-        w.gt = take((size_t)V * up(N, 128));
+        w.gt = take((size_t)slab_bytes(V, N));
         w.gt_exp = take((size_t)exp_bytes(V, N));
-        w.ht = take((size_t)D * up(N, 128));
+        w.ht = take((size_t)slab_bytes(D, N));
         w.ht_exp = take((size_t)exp_bytes(D, N));
     }
     if (db) w.sums = take((size_t)((N + 127) / 128) * V * 4);
-    const size_t a = dh ? parts_bytes(N, D, up(V, 128) / FP_SLAB) : 0, b = dw ? parts_bytes(V, D, up(N, 128) / FP_SLAB) : 0;
-    w.parts = take(a > b ? a : b);
+    w.h_parts = take(dh ? part_bytes(plan.h, N * D) : 0);
+    w.w_parts = take(dw ? part_bytes(plan.w, V * D) : 0);
     w.total = at;
     return w;
 }
@@ -164,6 +208,8 @@ extern "C" {
 
 int64_t lsr_fp8_row_bytes(int64_t cols) { return cols < 1 || cols > MAX_AXIS ? 0 : up(cols, 128); }
 
+int64_t lsr_fp8_slab_bytes(int64_t rows, int64_t cols) { return matrix(rows, cols) ? slab_bytes(rows, cols) : 0; }
+
 int64_t lsr_fp8_exp_bytes(int64_t rows, int64_t cols) { return matrix(rows, cols) ? exp_bytes(rows, cols) : 0; }
 
 int lsr_fp8_quantize(int64_t rows, int64_t cols, int32_t x_dtype, const void* X, int64_t ldx, int32_t square, uint8_t* Q, int64_t ldq, uint8_t* exps,
@@ -171,15 +217,14 @@ int lsr_fp8_quantize(int64_t rows, int64_t cols, int32_t x_dtype, const void* X,
     if (!float_type(x_dtype)) return LSR_ERR_DTYPE;
     if (!matrix(rows, cols) || ldx < cols) return LSR_ERR_SHAPE;
     if (!X || (!Q && !Qt) || (Q && !exps) || (Qt && !exps_t)) return LSR_ERR_NULL;
-    if ((Q && ldq < up(cols, 128)) || (Qt && ldqt < up(rows, 128))) return LSR_ERR_SHAPE;
+    if ((Q && ldq < up(cols, 128)) || (Qt && ldqt != 0 && ldqt < up(rows, 128))) return LSR_ERR_SHAPE;
     if (off_type(X, type_bytes(x_dtype)) || (Q && (misaligned(Q) || ldq % 16 != 0 || off_type(exps, 4))) ||
         (Qt && (misaligned(Qt) || ldqt % 16 != 0 || off_type(exps_t, 4))))
         return LSR_ERR_ALIGN;
     int n_cus = 0;
     const int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
-    return quantize(x_dtype, rows, cols, X, ldx, square != 0, Rows{Q, ldq, reinterpret_cast<uint32_t*>(exps)},
-                    Rows{Qt, ldqt, reinterpret_cast<uint32_t*>(exps_t)}, nullptr, stream);
+    return quantize(x_dtype, rows, cols, X, ldx, square != 0, fp8_rows(Q, ldq, exps, cols), fp8_rows(Qt, ldqt, exps_t, rows), nullptr, stream);
 }
 
 size_t lsr_fp8_matmul_workspace_bytes(int64_t N, int64_t V, int64_t K, int32_t a_dtype) {
@@ -208,31 +253,32 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
     int n_cus = 0;
     int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
-    const Rows weights = {const_cast<uint8_t*>(W), ldw, reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(w_exps))};
+    const Fp8Rows weights = fp8_rows(W, ldw, w_exps, K);
     if (few(N, K)) {
-        Fp8Params p = {};
+        Fp8FewParams p = {};
         p.A = static_cast<const uint8_t*>(A); p.lda = lda; p.a_exp = reinterpret_cast<const uint32_t*>(a_exps);
-        p.W = W; p.ldw = ldw; p.w_exp = weights.exps;
+        p.W = W; p.ldw = ldw; p.w_exp = reinterpret_cast<const uint32_t*>(w_exps);
         p.bias = bias; p.out = out; p.ldo = ldo;
-        p.N = (int)N; p.V = (int)V; p.K = (int)K; p.slabs = (int)(row / FP_SLAB);
+        p.N = (int)N; p.V = (int)V; p.K = (int)K; p.blocks = (int)(row / 128);
         if (bytes) launch_few<uint8_t>(p, out_dtype, n_cus, stream);
         else if (a_dtype == LSR_F32) launch_few<float>(p, out_dtype, n_cus, stream);
         else launch_few<uint16_t>(p, out_dtype, n_cus, stream);
         return launch_status();
     }
-    Rows states = {static_cast<uint8_t*>(const_cast<void*>(A)), lda, reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(a_exps))};
+    Fp8Rows states = fp8_rows(A, lda, a_exps, K);
     if (!bytes) {
         char* const ws = static_cast<char*>(workspace);
-        states = Rows{reinterpret_cast<uint8_t*>(ws + w.q), row, reinterpret_cast<uint32_t*>(ws + w.exps)};
-        rc = quantize(a_dtype, N, K, A, lda, false, states, Rows{}, nullptr, stream);
+        states = fp8_rows(ws + w.q, row, ws + w.exps, K);
+        rc = quantize(a_dtype, N, K, A, lda, false, states, Fp8Rows{}, nullptr, stream);
         if (rc != LSR_OK) return rc;
     }
-    return product(N, V, row / FP_SLAB, states, weights, bias, out_dtype, out, ldo, nullptr, stream);
+    Fp8Job j = job(N, V, K, states, weights, out, ldo);
+    return logits(j, bias, out_dtype, stream);
 }
 
 size_t lsr_fp8_backward_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t need_dh, int32_t need_dw, int32_t need_db) {
     if (!matrix(N, V) || D < 1 || D > MAX_HIDDEN) return 0;
-    return backward_ws(N, V, D, need_dh != 0, need_dw != 0, need_db != 0).total;
+    return backward_ws(N, V, D, need_dh != 0, need_dw != 0, need_db != 0, grads_plan(N, V, D, need_dh != 0, need_dw != 0)).total;
 }
 
 int lsr_fp8_backward(int64_t N, int64_t V, int64_t D, int32_t y_dtype, int32_t h_dtype, const void* dY, int64_t ldy, const void* H, int64_t ldh,
@@ -240,36 +286,35 @@ int lsr_fp8_backward(int64_t N, int64_t V, int64_t D, int32_t y_dtype, int32_t h
                      lsr_stream_t stream) {
     if (!float_type(y_dtype) || !float_type(h_dtype)) return LSR_ERR_DTYPE;
     if (!matrix(N, V) || D < 1 || D > MAX_HIDDEN || ldy < V) return LSR_ERR_SHAPE;
-    if ((dW && ldh < D) || (dH && (ldwt < up(V, 128) || ldwt > MAX_LD))) return LSR_ERR_SHAPE;
+    if ((dW && ldh < D) || (dH && ((ldwt != 0 && ldwt < up(V, 128)) || ldwt > MAX_LD))) return LSR_ERR_SHAPE;
     if (!dY || (!dH && !dW && !db) || (dW && !H) || (dH && (!Wt || !wt_exps))) return LSR_ERR_NULL;
     if (off_type(dY, type_bytes(y_dtype)) || (dW && off_type(H, type_bytes(h_dtype))) || (dH && (misaligned(Wt) || ldwt % 16 != 0 || off_type(wt_exps, 4))) ||
         misaligned(dH) || misaligned(dW) || off_type(db, 4))
         return LSR_ERR_ALIGN;
-    const BackwardWs w = backward_ws(N, V, D, dH, dW, db);
+    const GradsPlan plan = grads_plan(N, V, D, dH, dW);
+    const BackwardWs w = backward_ws(N, V, D, dH, dW, db, plan);
     if (!workspace || workspace_bytes < w.total) return LSR_ERR_WORKSPACE;
     if (misaligned(workspace)) return LSR_ERR_ALIGN;
     int n_cus = 0;
     int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
     char* const ws = static_cast<char*>(workspace);
-    auto rows_at = [&](bool on, size_t q, size_t exps, int64_t cols) {
-        return on ? Rows{reinterpret_cast<uint8_t*>(ws + q), up(cols, 128), reinterpret_cast<uint32_t*>(ws + exps)} : Rows{};
-    };
-    const Rows g = rows_at(dH, w.g, w.g_exp, V), gt = rows_at(dW, w.gt, w.gt_exp, N), ht = rows_at(dW, w.ht, w.ht_exp, N);
+    const Fp8Rows g = dH ? fp8_rows(ws + w.g, 0, ws + w.g_exp, V) : Fp8Rows{};
+    const Fp8Rows gt = dW ? fp8_rows(ws + w.gt, 0, ws + w.gt_exp, N) : Fp8Rows{}, ht = dW ? fp8_rows(ws + w.ht, 0, ws + w.ht_exp, N) : Fp8Rows{};
     float* const sums = db ? reinterpret_cast<float*>(ws + w.sums) : nullptr;
-    float* const parts = reinterpret_cast<float*>(ws + w.parts);
     rc = quantize(y_dtype, N, V, dY, ldy, false, g, gt, sums, stream);
-    if (rc == LSR_OK && dW) rc = quantize(h_dtype, N, D, H, ldh, false, Rows{}, ht, nullptr, stream);
+    if (rc == LSR_OK && dW) rc = quantize(h_dtype, N, D, H, ldh, false, Fp8Rows{}, ht, nullptr, stream);
     if (rc == LSR_OK && db) {
         fp8_sums_kernel<<<(unsigned)((V + 63) / 64), 256, 0, stream>>>(sums, (int)((N + 127) / 128), V, db);
         rc = launch_status();
     }
-    if (rc == LSR_OK && dH) {
-        const Rows wt = {const_cast<uint8_t*>(Wt), ldwt, reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(wt_exps))};
-        rc = product(N, D, up(V, 128) / FP_SLAB, g, wt, nullptr, h_dtype, dH, D, parts, stream);
-    }
-    if (rc == LSR_OK && dW) rc = product(V, D, up(N, 128) / FP_SLAB, gt, ht, nullptr, h_dtype, dW, D, parts, stream);
-    return rc;
+    if (rc != LSR_OK || (!dH && !dW)) return rc;
+    const Fp8Rows wt = fp8_rows(Wt, ldwt, wt_exps, V);
+    const Fp8Job h = dH ? job(N, D, V, g, wt, dH, D) : Fp8Job{}, v = dW ? job(V, D, N, gt, ht, dW, D) : Fp8Job{};
+    float* const h_parts = reinterpret_cast<float*>(ws + w.h_parts);
+    float* const w_parts = reinterpret_cast<float*>(ws + w.w_parts);
+    return h_dtype == LSR_F32 ? launch_grads<true, float>(h, v, plan, h_parts, w_parts, stream)
+                              : launch_grads<false, uint16_t>(h, v, plan, h_parts, w_parts, stream);
 }
 
 }  // extern "C"

@@ -8,6 +8,8 @@ Argument checks and marshalling only: all arithmetic runs in the HIP library, on
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import binding as lsr
@@ -33,6 +35,11 @@ def quantize_blocks(X: torch.Tensor, square: bool = False, transposed: bool = Fa
             q, qt = ((None, 0, None), (Q, Q.shape[1], exps))[::1 if transposed else -1]
             lsr.lsr_fp8_quantize(rows, cols, kind, X, _ld(X), square, *q, *qt)
     return Q, exps
+
+
+@functools.lru_cache(maxsize=256)
+def _backward_bytes(N: int, V: int, D: int, need_h: bool, need_w: bool, need_b: bool) -> int:
+    return lsr.lsr_fp8_backward_workspace_bytes(N, V, D, need_h, need_w, need_b)
 
 
 def _up(n: int, m: int) -> int:
@@ -94,12 +101,12 @@ class _Fp8Logits(torch.autograd.Function):
         need_t = ctx.needs_input_grad[0] and N > 0      # dH takes the matrix transposed: written beside the other from one read
         W8 = torch.empty((V, _up(D, 128)), dtype=torch.uint8, device=H.device)
         exps = torch.empty(lsr.lsr_fp8_exp_bytes(V, D), dtype=torch.uint8, device=H.device)
-        Wt = torch.empty((D, _up(V, 128)), dtype=torch.uint8, device=H.device) if need_t else None
+        Wt = torch.empty(lsr.lsr_fp8_slab_bytes(D, V), dtype=torch.uint8, device=H.device) if need_t else None
         exps_t = torch.empty(lsr.lsr_fp8_exp_bytes(D, V), dtype=torch.uint8, device=H.device) if need_t else None
         out = torch.empty((N, V), dtype=dtype, device=H.device)
         if N:
             with _on(H.device):
-                lsr.lsr_fp8_quantize(V, D, kind, W, _ld(W), True, W8, W8.shape[1], exps, Wt, Wt.shape[1] if need_t else 0, exps_t)
+                lsr.lsr_fp8_quantize(V, D, kind, W, _ld(W), True, W8, W8.shape[1], exps, Wt, 0, exps_t)
                 out = _matmul(H, kind, D, W8, exps, bias, dtype)
         ctx.shape = (N, V, D, _KIND[dtype], kind)
         ctx.has_bias = bias is not None
@@ -124,8 +131,8 @@ class _Fp8Logits(torch.autograd.Function):
         elif need_h or need_w or need_b:
             with _on(dev):
                 y = _rows(dY.detach())
-                ws = _scratch(lsr.lsr_fp8_backward_workspace_bytes(N, V, D, need_h, need_w, need_b), dev)
-                lsr.lsr_fp8_backward(*ctx.shape, y, _ld(y), H, _ld(H), Wt, Wt.shape[1] if need_h else 0, exps_t, dH, dW, db, ws)
+                ws = _scratch(_backward_bytes(N, V, D, need_h, need_w, need_b), dev)
+                lsr.lsr_fp8_backward(*ctx.shape, y, _ld(y), H, _ld(H), Wt, 0, exps_t, dH, dW, db, ws)
             dH, dW, db = first_order_only("fp8_logits", (dH, dW, db), (H, W, dY))
         return dH, dW, db, None
 

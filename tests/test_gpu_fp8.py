@@ -88,6 +88,31 @@ def test_quantize_writes_both_forms_and_nothing_else():
         assert torch.equal(E.view(-1, 200, 4)[..., :3], e[..., :3]) and torch.equal(Et.view(-1, 300, 4)[..., :2], et[..., :2])
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 1), (200, 300), (130, 700)])
+def test_quantize_by_slab(rows, cols):
+    x = values(torch.Generator().manual_seed(rows), (rows, cols), "f32")
+    for square in (0, 1):
+        n = binding.lsr_fp8_slab_bytes(cols, rows)
+        Qt = torch.full((n,), 99, dtype=torch.uint8, device=DEV)
+        Et = torch.zeros(binding.lsr_fp8_exp_bytes(cols, rows), dtype=torch.uint8, device=DEV)
+        binding.lsr_fp8_quantize(rows, cols, lsr.LSR_F32, x, cols, square, None, 0, None, Qt, 0, Et)
+        q, e = fp8.quantize_blocks(x, bool(square), True)
+        slabs = Qt.view(-1, q.shape[1] // 64, 256, 64).permute(0, 2, 1, 3).reshape(-1, q.shape[1])
+        assert torch.equal(slabs[:cols], q) and (slabs[cols:] == 99).all()
+
+
+def test_backward_takes_the_matrix_by_rows_too():
+    gen = torch.Generator().manual_seed(20)
+    N, V, D = 70, 300, 130
+    H, W, dY = values(gen, (N, D), "bf16", 0.5), values(gen, (V, D), "bf16", 0.5), values(gen, (N, V), "bf16")
+    want = train(H, W, None, dY, "bf16")[1]
+    Wt, Et = fp8.quantize_blocks(W, True, True)
+    dH = torch.empty_like(H)
+    ws = torch.empty(binding.lsr_fp8_backward_workspace_bytes(N, V, D, True, False, False), dtype=torch.uint8, device=DEV)
+    binding.lsr_fp8_backward(N, V, D, lsr.LSR_BF16, lsr.LSR_BF16, dY, V, None, 0, Wt, Wt.shape[1], Et, dH, None, None, ws)
+    assert torch.equal(dH, want)
+
+
 def test_quantize_extremes():
     big, tiny = 3.4028234e38, 1e-45
     rows = [[0.0] * 128, [big] * 128, [tiny] * 128, [448.0, -448.0] * 64, [448.0001] + [1.0] * 127, [float("inf"), 3.0] + [0.5] * 126, [float("nan")] * 128,
@@ -101,6 +126,12 @@ def test_quantize_extremes():
         assert np.array_equal(got, want, equal_nan=True)
     q, e = fp8.quantize_blocks(x, True)
     assert np.array_equal(orc.unpack(q.cpu().numpy(), e.cpu().numpy(), 128), orc.blocks(host(x), 128, 128)[0], equal_nan=True)
+    # every bfloat16 there is, in blocks of one power and of all
+    x = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).to(DEV).view(512, 128)
+    for y in (x, x.t().contiguous()):
+        for square in (False, True):
+            q, e = fp8.quantize_blocks(y, square)
+            assert np.array_equal(orc.unpack(q.cpu().numpy(), e.cpu().numpy(), y.shape[1]), orc.blocks(host(y), 128 if square else 1, 128)[0], equal_nan=True)
 
 
 # ---- the product ----
