@@ -14,13 +14,18 @@ namespace lsr {
 // Candidates of different beams are compared by scores that differ little, so the normaliser is summed more exactly than a float32 sum would be: logits that reach
 // the threshold above which the largest are collected (few, but most of the sum) are added in 64 bits, only those below it, each less than exp of the threshold, in
 // float32 and with the threshold as reference.  That reference also keeps the fast pass free of a running maximum: an exponential of what is below it cannot overflow.
-// A vector without a logit at or above the threshold costs a multiply-add, an exponential, an addition and half a maximum per logit.
+// A vector without a logit at or above the threshold costs a multiply-add, an exponential, an addition and half a maximum per logit.  A logit in the list is
+// added when it leaves it, by the thread that ranks it, so the pass itself forms no exponential in 64 bits.
 constexpr int BEAM_THREADS = 256;
 constexpr int BEAM_U = 4;                              // 16-byte vectors per thread and batch
 constexpr int BEAM_WAVES = BEAM_THREADS / 64;
 constexpr int BEAM_MAX_K = 128;
 constexpr int BEAM_MAX_BEAMS = 64;
+// Workgroups per CU (32-bit logits: 24 x 10 rows of 250002, K = 20, 51 us with three, which leave room for all registers, 58 with four; 16-bit logits: 64 x 8 rows
+// of 30522, K = 16, 18 us with four, 20 with three).
+constexpr int beam_resident(int bytes) { return bytes == 4 ? 3 : 4; }
 constexpr int BEAM_CAP = 1024;                         // keys in the list
+constexpr int BEAM_SLACK = 96;                         // keys beyond K before it is cut: a cut costs two microseconds, a loose threshold a few more keys
 constexpr int BEAM_JOIN = 8192;                        // keys of one sequence that the joining launch holds
 constexpr float BEAM_LOWEST = -3.402823466e38f;
 constexpr uint32_t BEAM_LOWEST_BITS = 0x00800000u;     // ordered(BEAM_LOWEST); -inf lies below
@@ -44,9 +49,30 @@ struct BeamParams {
 
 struct BeamShared {
     TopShared top;
-    float most[BEAM_WAVES];
+    float by_rank[BEAM_CAP];     // all logits of the list in order, so that they are added in an order that does not go by chance
     double part[BEAM_WAVES];
 };
+
+// best[0 .. min(K, n)) = the largest of list[0 .. n), in order, and by_rank[0 .. n) the logits of all.  Whole workgroup; the list is complete (a barrier behind its last
+// write); a barrier at the end.
+__device__ __forceinline__ void beam_rank(BeamShared& sh, int n, int K) {
+    for (int i = threadIdx.x; i < n; i += BEAM_THREADS) {
+        const uint64_t k = sh.top.list[i];
+        int rank = 0;
+        int j = 0;
+        for (; j + 8 <= n; j += 8) {             // 16-byte reads, the same address in every lane
+            ulonglong2 q[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[e] = *reinterpret_cast<const ulonglong2*>(&sh.top.list[j + 2 * e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rank += (q[e].x > k ? 1 : 0) + (q[e].y > k ? 1 : 0);
+        }
+        for (; j < n; ++j) rank += sh.top.list[j] > k ? 1 : 0;
+        if (rank < K) sh.top.best[rank] = k;
+        sh.by_rank[rank] = value_of((uint32_t)(k >> 32));
+    }
+    __syncthreads();
+}
 
 // Whether a beam is gone on with from its logits.
 __device__ __forceinline__ bool beam_open(const BeamParams& p, int64_t row) {
@@ -54,7 +80,7 @@ __device__ __forceinline__ bool beam_open(const BeamParams& p, int64_t row) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(BEAM_THREADS, 4) void beam_segment_kernel(BeamParams p) {
+__global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_segment_kernel(BeamParams p) {
     typedef uint32_t V4 __attribute__((ext_vector_type(4)));
     typedef V4 U4 __attribute__((aligned(2)));
     typedef V4 F4 __attribute__((aligned(4)));
@@ -63,7 +89,6 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_segment_kernel(BeamParam
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row = blockIdx.x / p.splits;
     const int split = (int)(blockIdx.x - row * p.splits);
-    if (!beam_open(p, row)) return;
     const int first = split * p.seg;
     const int n = min(p.seg, p.V - first);       // (the host leaves no segment empty)
     const T* const x = reinterpret_cast<const T*>(p.X) + row * p.ldx + first;
@@ -96,6 +121,7 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_segment_kernel(BeamParam
         if constexpr (sizeof(T) == 4) odd = x[nvec * EPV + tid];
         else odd = __uint_as_float((uint32_t)x[nvec * EPV + tid] << 16);
     }
+    if (!beam_open(p, row)) return;              // (asked behind the first loads: their answers come together)
     if (tid == 0) sh.top.count = 0;
 
     // first threshold: of the waves whose threads all have logits (at least one), each one's `want` largest maxima are K logits no smaller than the least of them
@@ -123,118 +149,135 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_segment_kernel(BeamParam
     }
     int before = 0;                              // keys in the list
     bool ordered_list = false;                   // the list is its K largest, in order
-    double hot = 0.0;                            // this thread's sum of exp2((x - hot_m) c) of what reached the threshold
-    float hot_m = -INFINITY;
-    float cold = 0.f;                            // and of what did not, times 2^(-reference)
-    float tv, zc;                                // the threshold's value; times c
+    float tv, zc;                                // the reference, the threshold's value when it was last set for sure; times c
     bool plain;                                  // zc is small enough for one multiply-add (with very low logits or temperatures its rounding would be more than the sum)
-    auto add_hot = [&](float f) {
-        if (f > hot_m) {
-            hot = hot_m == -INFINITY ? hot : hot * exp2((double)(hot_m - f) * cd);      // (0, or NaN)
-            hot_m = f;
-        }
-        hot += f == hot_m ? (f == INFINITY ? __builtin_nan("") : 1.0) : exp2(((double)f - (double)hot_m) * cd);
-    };
+    float cold = 0.f;                            // this thread's sum below the reference, times 2^(-zc)
+    int ties = 0;                                // its logits equal to the reference that found no place in the list
+    double sum = 0.0;                            // its sum of exp2((x - base) c) of all that is done with
+    float base;                                  // an earlier reference
+    double far = 0.0;                            // its sum of exp2((x - far_m) c) of logits above the reference that are not in the list (seldom)
+    float far_m = -INFINITY;
     auto reference = [&]() {
         tv = value_of(max((uint32_t)(thr >> 32), BEAM_LOWEST_BITS));
         zc = tv * c;
         plain = fabsf(zc) < 0x1p20f;
     };
-    // the float32 sum goes to the 64-bit one: before its reference changes, and at the end
-    auto flush = [&]() {
-        if (cold != 0.f) {                       // (also NaN)
-            if (tv > hot_m) {
-                hot = hot_m == -INFINITY ? hot : hot * exp2(((double)hot_m - (double)tv) * cd);
-                hot_m = tv;
-            }
-            // (the fast sum's reference is zc as it was rounded)
-            hot += (double)cold * exp2(((double)tv - (double)hot_m) * cd + (plain ? (double)zc - (double)tv * (double)c : 0.0));
-            cold = 0.f;
-        }
-    };
     reference();
-    // one logit of every lane into the list, where it beats the threshold
+    base = tv;
+    auto part = [&](float f, float of) -> double { return exp2(((double)f - (double)of) * cd); };
+    // what lies below the reference goes to the 64-bit sum (whose own reference is not above it)
+    auto flush = [&]() {
+        if (tv > base) {
+            sum *= part(base, tv);
+            base = tv;
+        }
+        // (the fast sum's reference is zc as it was rounded)
+        sum += (double)cold * exp2(((double)tv - (double)base) * cd + (plain ? (double)zc - (double)tv * (double)c : 0.0)) + (double)ties * part(tv, base);
+        cold = 0.f;
+        ties = 0;
+    };
+    auto add_far = [&](float f) {
+        if (f > far_m) {
+            far = far_m == -INFINITY ? far : far * part(far_m, f);
+            far_m = f;
+        }
+        far += part(f, far_m);
+    };
+    // one logit of every lane, at or above the reference, into the list or among what is not in it
     auto keep = [&](bool on, float f, int index) {
-        if (__any(on)) {
-            const uint64_t k = key_of(ordered(f), (uint32_t)index);
-            on = on && k > thr;
-            const unsigned long long b = __ballot(on);
-            int base = 0;
-            if (lane == 0 && b) base = atomicAdd(&sh.top.count, __popcll(b));
-            base = __builtin_amdgcn_readfirstlane(base) + __popcll(b & ((1ull << lane) - 1ull));
-            if (on && base < BEAM_CAP) sh.top.list[base] = k;
+        const uint64_t k = key_of(ordered(f), (uint32_t)index);
+        const bool in = on && k > thr;
+        const unsigned long long b = __ballot(in);
+        if (b) {
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&sh.top.count, __popcll(b));
+            at = __builtin_amdgcn_readfirstlane(at) + __popcll(b & ((1ull << lane) - 1ull));
+            if (in && at < BEAM_CAP) sh.top.list[at] = k;
+        }
+        const bool tie = on && !in && f == tv;
+        ties += tie ? 1 : 0;
+        if (__any(on && !in && !tie)) {          // (a batch that is gone through again)
+            if (on && !in && !tie) add_far(f);
         }
     };
     auto weight = [&](float f) -> float { return __builtin_amdgcn_exp2f(plain ? fmaf(f, c, -zc) : (f - tv) * c); };
     const int batch = BEAM_U * BEAM_THREADS;
     for (int b0 = 0; b0 == 0 || b0 < nvec; b0 += batch) {
         if (b0 + batch < nvec) fetch(next, b0 + batch);
-        bool again = false;                      // the batch is gone through again: its sum is done
+        const float cold0 = cold;
+        const int ties0 = ties;
+        float far_m0 = far_m;
+        double far0 = far;
+        bool again = false;
         for (;;) {
             if (b0 == 0) {
                 const bool on = odd >= tv;
-                if (!again) {
-                    if (on) add_hot(odd);
-                    else cold += odd == -INFINITY ? 0.f : weight(odd);
-                }
+                cold += on || odd == -INFINITY ? 0.f : weight(odd);
                 keep(on, odd, first + nvec * EPV + tid);
             }
+            uint32_t bits = 0;                   // which of the thread's logits reach the reference: bit u EPV + e
 #pragma unroll
             for (int u = 0; u < BEAM_U; ++u) {
-                const int at = first + (b0 + u * BEAM_THREADS + tid) * EPV;
                 float m = value(w[u], 0);
 #pragma unroll
                 for (int e = 1; e < EPV; ++e) m = fmaxf(m, value(w[u], e));
+                float s = 0.f;
                 if (!__any(m >= tv)) {
-                    if (!again) {
-                        float s = 0.f;
-                        if (plain) {
+                    if (plain) {
 #pragma unroll
-                            for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f(fmaf(value(w[u], e), c, -zc));
-                        } else {
+                        for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f(fmaf(value(w[u], e), c, -zc));
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f((value(w[u], e) - tv) * c);
-                        }
-                        cold += s;
+                        for (int e = 0; e < EPV; ++e) s += __builtin_amdgcn_exp2f((value(w[u], e) - tv) * c);
                     }
                 } else {
-#pragma unroll 1
+#pragma unroll
                     for (int e = 0; e < EPV; ++e) {
-                        float f;
-                        if constexpr (sizeof(T) == 4) {
-                            f = __uint_as_float(e & 2 ? (e & 1 ? w[u][3] : w[u][2]) : (e & 1 ? w[u][1] : w[u][0]));
-                        } else {
-                            const uint32_t d = e & 4 ? (e & 2 ? w[u][3] : w[u][2]) : (e & 2 ? w[u][1] : w[u][0]);
-                            f = __uint_as_float(e & 1 ? d & 0xffff0000u : d << 16);
-                        }
+                        const float f = value(w[u], e);
                         const bool on = f >= tv;
-                        if (!again) {
-                            if (on) add_hot(f);
-                            else cold += weight(f);
-                        }
-                        keep(on, f, at + e);
+                        bits |= on ? 1u << (u * EPV + e) : 0u;
+                        s += on ? 0.f : weight(f);
                     }
                 }
+                cold += s;
+            }
+            // one of each lane at a time (few lanes have any, fewer have two), read again: from the caches, instead of picked out of the registers
+            while (__any(bits != 0)) {
+                const bool on = bits != 0;
+                const int q = __builtin_ctz(bits | 0x80000000u);
+                bits &= bits - 1;
+                const int i = (b0 + (q / EPV) * BEAM_THREADS + tid) * EPV + (q & (EPV - 1));
+                float f = 0.f;
+                if (on) {
+                    if constexpr (sizeof(T) == 4) f = x[i];
+                    else f = __uint_as_float((uint32_t)x[i] << 16);
+                }
+                keep(on, f, first + i);
             }
             __syncthreads();
             const int have = sh.top.count;
-            if (!again && have <= K + K / 4 + 8) {
+            if (!again && have <= K + BEAM_SLACK) {
                 ordered_list = ordered_list && have == before;
                 before = have;
                 __syncthreads();                 // everyone has read the count
                 break;
             }
             const bool fits = have <= BEAM_CAP;
-            top_rank(sh.top, min(have, BEAM_CAP), K);
+            beam_rank(sh, min(have, BEAM_CAP), K);
             const uint64_t kth = sh.top.best[K - 1];
             if (fits) {
                 flush();
+                thr = kth;
+                reference();
+                if (tv > base) {
+                    sum *= part(base, tv);
+                    base = tv;
+                }
+                for (int q = K + tid; q < have; q += BEAM_THREADS) sum += part(sh.by_rank[q], base);      // what leaves the list: not above the new reference
                 for (int q = tid; q < K; q += BEAM_THREADS) sh.top.list[q] = sh.top.best[q];
                 if (tid == 0) sh.top.count = K;
                 before = K;
                 ordered_list = true;
-                thr = kth;
-                reference();
                 __syncthreads();
                 break;
             }
@@ -243,6 +286,10 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_segment_kernel(BeamParam
             // their reference, and the batch ends with a cut to its true K largest.
             again = true;
             thr = kth - 1;
+            cold = cold0;
+            ties = ties0;
+            far = far0;
+            far_m = far_m0;
             uint64_t mine[BEAM_CAP / BEAM_THREADS];
 #pragma unroll
             for (int q = 0; q < BEAM_CAP / BEAM_THREADS; ++q) {
@@ -251,9 +298,14 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_segment_kernel(BeamParam
             }
             if (tid == 0) sh.top.count = 0;
             __syncthreads();
-#pragma unroll
-            for (int q = 0; q < BEAM_CAP / BEAM_THREADS; ++q)
-                if (mine[q] > thr) sh.top.list[atomicAdd(&sh.top.count, 1)] = mine[q];
+#pragma unroll 1
+            for (int q = 0; q < BEAM_CAP / BEAM_THREADS; ++q) {
+                const uint64_t k = mine[q];
+                if (k > thr) sh.top.list[atomicAdd(&sh.top.count, 1)] = k;
+                else if (k) add_far(value_of((uint32_t)(k >> 32)));
+            }
+            far_m0 = far_m;                      // (these are done with, the batch is not)
+            far0 = far;
             __syncthreads();
             before = sh.top.count;
             __syncthreads();
@@ -261,30 +313,26 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_segment_kernel(BeamParam
 #pragma unroll
         for (int u = 0; u < BEAM_U; ++u) w[u] = next[u];
     }
-    flush();
-    // joined over the workgroup: the largest reference first, then every thread rescales once
-    float m = hot_m;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if (lane == 0) sh.most[wave] = m;
-    __syncthreads();
-    m = sh.most[0];
-#pragma unroll
-    for (int k = 1; k < BEAM_WAVES; ++k) m = fmaxf(m, sh.most[k]);
-    double s = hot_m == -INFINITY ? hot : hot * exp2(((double)hot_m - (double)m) * cd);
-#pragma unroll
-    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-    if (lane == 0) sh.part[wave] = s;
     const int have = before;
     for (int i = have + tid; i < K; i += BEAM_THREADS) sh.top.best[i] = 0;      // a segment with fewer than K
     __syncthreads();
-    if (!ordered_list) top_rank(sh.top, have, K);      // (else `best` holds them already)
+    if (!ordered_list) beam_rank(sh, have, K);   // (else `best` and the first of `by_rank` hold them already)
+    flush();
+    // joined over the workgroup, with the largest logit as reference
+    const uint64_t largest = sh.top.best[0];
+    const float m = largest ? value_of((uint32_t)(largest >> 32)) : base;
+    double s = sum * part(base, m) + (far_m == -INFINITY ? far : far * part(far_m, m));
+    for (int q = tid; q < have; q += BEAM_THREADS) s += part(sh.by_rank[q], m);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    if (lane == 0) sh.part[wave] = s;
+    __syncthreads();
     const int64_t at = row * p.splits + split;
     for (int i = tid; i < K; i += BEAM_THREADS) p.keys[at * K + i] = sh.top.best[i];
     if (tid == 0) {
         BeamSum e;
         e.s = (sh.part[0] + sh.part[1]) + (sh.part[2] + sh.part[3]);
-        e.m = m;
+        e.m = e.s == 0.0 ? -INFINITY : m;
         e.pad = 0.f;
         p.sums[at] = e;
     }
@@ -297,85 +345,143 @@ __device__ __forceinline__ uint64_t ordered(double x) {
     return (int64_t)b < 0 ? ~b : b | 0x8000000000000000ull;
 }
 
+__device__ __forceinline__ double score_bits(uint64_t o) {
+    if (o == ~0ull) return __builtin_nan("");
+    return __longlong_as_double((long long)((int64_t)o < 0 ? o & 0x7fffffffffffffffull : ~o));
+}
+
 enum { BEAM_NONE = 0, BEAM_GOES_ON = 1, BEAM_FINISHED = 2, BEAM_NAN = 3 };
 
 // One workgroup per sequence.  Keys are dealt out place by place (all lists' first, then all their second), so that the threads' maxima are the best of the lists; K of
-// them give a threshold, what reaches it goes to a list in LDS, and a candidate's place is the number of better ones.
+// them give a threshold, what reaches it goes to a list in LDS, and a candidate's place is the number of better ones.  Latency bounds it, so the keys are on their way while
+// the normalisers are formed, and each thread keeps the scores of its first BEAM_OWN.
+constexpr int BEAM_OWN = 4;
 __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
-    // a beam's candidates have score s_base + (x / T - s_top): the difference first, which is exact where it is small
+    // a beam's candidates have score s_base + (x - s_top) / T: the difference first, which is exact
     __shared__ double s_base[BEAM_MAX_BEAMS], s_top[BEAM_MAX_BEAMS];
     __shared__ int s_kind[BEAM_MAX_BEAMS];
-    __shared__ uint32_t s_most[BEAM_WAVES];
+    __shared__ __attribute__((aligned(16))) uint32_t s_most[BEAM_THREADS];
+    __shared__ uint32_t s_least;
     __shared__ int s_count;
     __shared__ __attribute__((aligned(16))) uint64_t s_score[BEAM_JOIN];
     __shared__ uint16_t s_at[BEAM_JOIN];
+    __shared__ int s_token[BEAM_JOIN];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t b = blockIdx.x;
-    const double cd = 1.4426950408889634 / p.temperature;
-    // normalisers: a beam per wave at a time, a segment per lane
-    for (int m = wave; m < p.beams; m += BEAM_WAVES) {
-        const int64_t row = b * p.beams + m;
+    const double inv_t = 1.0 / p.temperature, cd = 1.4426950408889634 * inv_t;
+    const int lists = p.beams * p.splits, total = lists * p.K;
+    const uint64_t* const keys = p.keys + b * total;
+    // candidate i is place i / lists of list i % lists, list l of beam l / splits (the quotients are far enough from the next whole number for float32)
+    const float per_lists = 1.f / (float)lists, per_splits = 1.f / (float)p.splits;
+    auto place = [&](int i, int& l, int& m) -> int {
+        const int j = (int)(((float)i + 0.5f) * per_lists);
+        l = i - j * lists;
+        m = (int)(((float)l + 0.5f) * per_splits);
+        return j;
+    };
+    uint64_t own[BEAM_OWN];
+#pragma unroll
+    for (int q = 0; q < BEAM_OWN; ++q) {
+        const int i = q * BEAM_THREADS + tid;
+        own[q] = 0;
+        if (i < total) {
+            int l, m;
+            const int j = place(i, l, m);
+            own[q] = keys[(int64_t)l * p.K + j];       // (of a beam that is not gone on with: whatever is there, not looked at)
+        }
+    }
+    // normalisers: a beam by a group of lanes, a segment by each
+    int group = 1;
+    while (group < p.splits) group *= 2;
+    for (int m0 = 0; m0 < p.beams; m0 += BEAM_THREADS / group) {
+        const int m = m0 + tid / group, part = tid & (group - 1);
+        const bool on = m < p.beams;
+        const int64_t row = b * p.beams + (on ? m : 0);
         const float score = p.scores[row];
-        int kind = score == -INFINITY ? BEAM_NONE : p.finished && p.finished[row] ? BEAM_FINISHED : BEAM_GOES_ON;
+        const bool ended = p.finished && p.finished[row];
+        BeamSum e = p.sums[row * p.splits + min(part, p.splits - 1)];      // (of a beam that is not gone on with: whatever is there)
+        int kind = score == -INFINITY ? BEAM_NONE : ended ? BEAM_FINISHED : BEAM_GOES_ON;
+        if (kind != BEAM_GOES_ON || part >= p.splits) { e.s = 0.0; e.m = -INFINITY; }
+        float most = e.m;
+        for (int o = group >> 1; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+        double s = e.m == -INFINITY ? e.s : e.s * exp2(((double)e.m - (double)most) * cd);
+        for (int o = group >> 1; o; o >>= 1) s += __shfl_xor(s, o);
         double base = score, top = 0.0;
         if (kind == BEAM_GOES_ON) {
-            BeamSum e = {0.0, -INFINITY, 0.f};
-            if (lane < p.splits) e = p.sums[row * p.splits + lane];
-            float most = e.m;
-#pragma unroll
-            for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-            double s = e.m == -INFINITY ? e.s : e.s * exp2(((double)e.m - (double)most) * cd);
-#pragma unroll
-            for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
             if (most == -INFINITY && s == s) kind = BEAM_NONE;          // every logit is -inf
             base = (double)score - log(s);
-            top = (double)most / p.temperature;
+            top = most;
             if (kind == BEAM_GOES_ON && base != base) kind = BEAM_NAN;
         }
-        if (lane == 0) { s_base[m] = base; s_top[m] = top; s_kind[m] = kind; }
+        if (on && part == 0) { s_base[m] = base; s_top[m] = top; s_kind[m] = kind; }
     }
     if (tid == 0) s_count = 0;
     __syncthreads();
-    const int lists = p.beams * p.splits, total = lists * p.K;
-    const uint64_t* const keys = p.keys + b * total;
-    auto score_of = [&](int m, uint32_t o) -> double { return s_base[m] + ((double)value_of(o) / p.temperature - s_top[m]); };
-    // score of candidate i (place i / lists of list i % lists), as ordered bits; 0: there is none
-    auto candidate = [&](int i) -> uint64_t {
-        const int j = i / lists, l = i - j * lists, m = l / p.splits;
+    auto score_of = [&](int m, uint32_t o) -> double { return s_base[m] + ((double)value_of(o) - s_top[m]) * inv_t; };
+    // score of candidate i of key k, as ordered bits; 0: there is none
+    auto candidate = [&](int i, uint64_t k) -> uint64_t {
+        int l, m;
+        const int j = place(i, l, m);
         const int kind = s_kind[m];
-        if (kind == BEAM_NONE) return 0;
+        if (kind == BEAM_GOES_ON) return k ? ordered(score_of(m, (uint32_t)(k >> 32))) : 0;
         if (kind == BEAM_FINISHED) return j == 0 && l == m * p.splits ? ordered(s_base[m]) : 0;
-        if (kind == BEAM_NAN) return ~0ull;
-        const uint32_t o = (uint32_t)(keys[(int64_t)l * p.K + j] >> 32);
-        return o ? ordered(score_of(m, o)) : 0;
+        return kind == BEAM_NAN ? ~0ull : 0;
+    };
+    auto key_at = [&](int i) -> uint64_t {
+        int l, m;
+        const int j = place(i, l, m);
+        return keys[(int64_t)l * p.K + j];
     };
     uint32_t most = 0;
-    for (int i = tid; i < total; i += BEAM_THREADS) most = max(most, (uint32_t)(candidate(i) >> 32));
-    {
-        const int full = max(1, min(total, BEAM_THREADS) >> 6);
-        const int want = (p.K + full - 1) / full;
-        uint32_t t = 0;
-#pragma unroll 4
-        for (uint32_t bit = 1u << 31; bit >= 1u << 8; bit >>= 1) t = __popcll(__ballot(most >= (t | bit))) >= want ? t | bit : t;
-        if (lane == 0) s_most[wave] = wave < full ? t : ~0u;
-        __syncthreads();
-        most = min(min(s_most[0], s_most[1]), min(s_most[2], s_most[3]));
+    uint64_t mine[BEAM_OWN];
+#pragma unroll
+    for (int q = 0; q < BEAM_OWN; ++q) {
+        const int i = q * BEAM_THREADS + tid;
+        mine[q] = i < total ? candidate(i, own[q]) : 0;
+        most = max(most, (uint32_t)(mine[q] >> 32));
     }
-    for (int i = tid; i < total; i += BEAM_THREADS) {
-        const uint64_t o = candidate(i);
+    for (int i = BEAM_OWN * BEAM_THREADS + tid; i < total; i += BEAM_THREADS) most = max(most, (uint32_t)(candidate(i, key_at(i)) >> 32));
+    // the K-th largest of the threads' maxima (of the first 32 bits; at least K threads have candidates): the least that fewer than K are larger than
+    s_most[tid] = most;
+    if (tid == 0) s_least = ~0u;
+    __syncthreads();
+    {
+        int larger = 0;
+#pragma unroll 8
+        for (int r = 0; r < BEAM_THREADS; r += 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(&s_most[r]);
+            larger += (x.x > most ? 1 : 0) + (x.y > most ? 1 : 0) + (x.z > most ? 1 : 0) + (x.w > most ? 1 : 0);
+        }
+        uint32_t least = larger < p.K ? most : ~0u;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) least = min(least, (uint32_t)__shfl_xor((int)least, o));
+        if (lane == 0) atomicMin(&s_least, least);
+    }
+    __syncthreads();
+    most = s_least;
+    auto enter = [&](int i, uint64_t o, uint64_t k) {
         if (o && (uint32_t)(o >> 32) >= most) {
+            int l, m;
+            place(i, l, m);
             const int at = atomicAdd(&s_count, 1);
             s_score[at] = o;
             s_at[at] = (uint16_t)i;
+            s_token[at] = s_kind[m] != BEAM_FINISHED && k ? (int)~(uint32_t)k : p.end_id;
         }
+    };
+#pragma unroll
+    for (int q = 0; q < BEAM_OWN; ++q) enter(q * BEAM_THREADS + tid, mine[q], own[q]);
+    for (int i = BEAM_OWN * BEAM_THREADS + tid; i < total; i += BEAM_THREADS) {
+        const uint64_t k = key_at(i);
+        enter(i, candidate(i, k), k);
     }
     __syncthreads();
     const int n = s_count;
-    auto beam_of = [&](int i) { return (i % lists) / p.splits; };
-    auto key_at = [&](int i) { return keys[(int64_t)(i % lists) * p.K + i / lists]; };
     // whether candidate i comes before j, of equal score
     auto first_of = [&](int i, int j) -> bool {
-        const int mi = beam_of(i), mj = beam_of(j);
+        int li, lj, mi, mj;
+        place(i, li, mi);
+        place(j, lj, mj);
         if (mi != mj) return mi < mj;
         const uint64_t ki = key_at(i), kj = key_at(j);
         return ki != kj ? ki > kj : i < j;
@@ -383,21 +489,27 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
     for (int q = tid; q < n; q += BEAM_THREADS) {
         const uint64_t o = s_score[q];
         const int i = s_at[q];
-        int rank = 0;
-        for (int r = 0; r < n; ++r) {
-            const uint64_t other = s_score[r];
-            rank += other > o ? 1 : 0;
-            if (other == o && r != q) rank += first_of(s_at[r], i) ? 1 : 0;
+        int rank = 0, equal = 0, r = 0;
+        for (; r + 4 <= n; r += 4) {
+            const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(&s_score[r]), y = *reinterpret_cast<const ulonglong2*>(&s_score[r + 2]);
+            rank += (x.x > o ? 1 : 0) + (x.y > o ? 1 : 0) + (y.x > o ? 1 : 0) + (y.y > o ? 1 : 0);
+            equal += (x.x == o ? 1 : 0) + (x.y == o ? 1 : 0) + (y.x == o ? 1 : 0) + (y.y == o ? 1 : 0);
+        }
+        for (; r < n; ++r) {
+            rank += s_score[r] > o ? 1 : 0;
+            equal += s_score[r] == o ? 1 : 0;
+        }
+        if (equal > 1 && rank < p.K) {           // (itself is one)
+            for (r = 0; r < n; ++r)
+                if (s_score[r] == o && r != q) rank += first_of(s_at[r], i) ? 1 : 0;
         }
         if (rank < p.K) {
-            const int m = beam_of(i), kind = s_kind[m];
-            const uint64_t k = kind == BEAM_FINISHED ? 0 : key_at(i);
+            int l, m;
+            place(i, l, m);
             const int64_t to = b * p.K + rank;
-            p.out_scores[to] = (float)(kind == BEAM_NAN      ? __builtin_nan("")
-                                       : kind == BEAM_FINISHED ? s_base[m]
-                                                               : score_of(m, (uint32_t)(k >> 32)));
+            p.out_scores[to] = (float)score_bits(o);
             p.out_beams[to] = m;
-            p.out_tokens[to] = k ? (int)~(uint32_t)k : p.end_id;
+            p.out_tokens[to] = s_token[q];
         }
     }
     for (int r = n + tid; r < p.K; r += BEAM_THREADS) {

@@ -25,14 +25,15 @@ bool select_shape(int64_t B, int64_t beams, int64_t V, int64_t K) {
            K <= BEAM_MAX_K && K <= beams * V;
 }
 
-// Segments per row: enough workgroups to fill the chip where there are few rows, no segment shorter than BEAM_MIN_SEG, no more keys of a sequence than the joining
+// Segments per row: as many as are resident at once where there are few rows (64 x 8 rows of 30522 in bfloat16: 1024 workgroups 17 us, 512 21; 24 x 10 of 250002 in float32:
+// 720 workgroups 51 us, 960 64), no segment shorter than BEAM_MIN_SEG (4 rows of 30522: 2048 7.1 us, 4096 8.7), no more keys of a sequence than the joining
 // launch holds, at most one for each lane of a wave.
-constexpr int64_t BEAM_WANTED = 1024;
-constexpr int64_t BEAM_MIN_SEG = 4096;
+constexpr int64_t BEAM_CUS = 256;     // CUs that it is made for: the size of the workspace does not depend on the device
+constexpr int64_t BEAM_MIN_SEG = 2048;
 struct BeamPlan { int splits, seg; };
-BeamPlan beam_plan(int64_t B, int64_t beams, int64_t V, int64_t K) {
+BeamPlan beam_plan(int64_t B, int64_t beams, int64_t V, int64_t K, int x_bytes) {
     const int64_t rows = B * beams;
-    int64_t s = (BEAM_WANTED + rows - 1) / rows;
+    int64_t s = BEAM_CUS * beam_resident(x_bytes) / rows;
     const int64_t by_len = V / BEAM_MIN_SEG, by_keys = BEAM_JOIN / (beams * K);
     s = s < by_len ? s : by_len;
     s = s < by_keys ? s : by_keys;
@@ -58,7 +59,9 @@ extern "C" {
 
 size_t lsr_beam_select_workspace_bytes(int64_t B, int64_t beams, int64_t V, int64_t K) {
     if (!select_shape(B, beams, V, K)) return 0;
-    return beam_ws(B * beams, beam_plan(B, beams, V, K), K).total;
+    // (of either type of logits: more segments where more are resident)
+    const size_t a = beam_ws(B * beams, beam_plan(B, beams, V, K, 2), K).total, b = beam_ws(B * beams, beam_plan(B, beams, V, K, 4), K).total;
+    return a > b ? a : b;
 }
 
 int lsr_beam_select(int64_t B, int64_t beams, int64_t V, int64_t K, int32_t x_dtype, double temperature, const void* X, int64_t ldx, const float* scores,
@@ -70,9 +73,9 @@ int lsr_beam_select(int64_t B, int64_t beams, int64_t V, int64_t K, int32_t x_dt
     if (off_type(X, x_dtype == LSR_F32 ? 4 : 2) || off_type(scores, 4) || off_type(out_scores, 4) || off_type(out_beams, 4) || off_type(out_tokens, 4))
         return LSR_ERR_ALIGN;
     const int64_t rows = B * beams;
-    const BeamPlan plan = beam_plan(B, beams, V, K);
+    const BeamPlan plan = beam_plan(B, beams, V, K, x_dtype == LSR_F32 ? 4 : 2);
     const BeamWs w = beam_ws(rows, plan, K);
-    if (!workspace || workspace_bytes < w.total) return LSR_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < lsr_beam_select_workspace_bytes(B, beams, V, K)) return LSR_ERR_WORKSPACE;
     if (misaligned(workspace)) return LSR_ERR_ALIGN;
     int n_cus = 0;
     const int rc = check_device(&n_cus);
