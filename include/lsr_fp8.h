@@ -84,7 +84,7 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
  *   Wt [D, ldwt], wt_exps: W transposed as lsr_fp8_quantize leaves Qt and exps_t (square), with ldwt = 0 by slab, which is faster
  *   dH [N, D], dW [V, D] of h_dtype, contiguous; db [V] f32; each may be NULL to skip it.  H is needed for dW alone, Wt for dH alone.
  * Sums are formed as in lsr_fp8_matmul (exact products and float32 sums where h_dtype is LSR_F32), over cuts of the contracted axis where there are
- * few tiles, joined in float32 in a fixed order and rounded once.  Results are the same bits from call to call.
+ * few tiles, joined in float32 in a fixed order and rounded once.  Results are the same bits from call to call.  The workspace may be of 0 bytes, and then NULL.
  * Limits: 1 <= N, V <= 2^22, N V < 2^36, 1 <= D <= 65536, ldwt <= 2^23.
  */
 size_t lsr_fp8_backward_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t need_dh, int32_t need_dw, int32_t need_db);

@@ -111,21 +111,31 @@ def beam_reorder(states, parents: torch.Tensor, out=None):
     _on_gpu("beam_reorder", parents, *states, *(out or ()))
     B, K = parents.shape
     beams = states[0].shape[1] if states[0].dim() > 1 else 0
-    new, table, hold = [], [], []
+    new, table, spans, hold = [], [], [], []
     for i, x in enumerate(states):
-        if x.dim() < 2 or x.shape[0] != B or x.shape[1] != beams:
+        shape = x.shape
+        if len(shape) < 2 or shape[0] != B or shape[1] != beams:
             raise ValueError("beam_reorder: every state must be [B, beams, ...]")
         if out is None:
-            y = torch.empty((B, K, *x.shape[2:]), dtype=x.dtype, device=x.device)
+            y = torch.empty((B, K, *shape[2:]), dtype=x.dtype, device=x.device)
         else:
             y = out[i]
-            if y.shape != (B, K, *x.shape[2:]) or y.dtype != x.dtype:
+            if y.shape != (B, K, *shape[2:]) or y.dtype != x.dtype:
                 raise ValueError("beam_reorder: out must be [B, K, ...] of the states' dtypes")
         new.append(y)
-        if not y.numel():
+        size = y.numel()
+        if not size:
             continue
-        if not x.numel():
+        if not beams:
             y.zero_()
+            continue
+        if x.is_contiguous() and y.is_contiguous():
+            row = size // (B * K) * x.element_size()
+            src, dst = x.data_ptr(), y.data_ptr()
+            table.append((src, dst, beams * row, row, row, K * row, row, row, 1, row))
+            if out is not None:
+                spans.append((dst, dst + B * K * row, True))
+                spans.append((src, src + B * beams * row, False))
             continue
         x = x.detach()
         src, dst = _layout(x), _layout(y)
@@ -144,16 +154,18 @@ def beam_reorder(states, parents: torch.Tensor, out=None):
             hold.append(x)
             src = _layout(x)
             src = (*src[:2], dst[4], *dst[3:])
-        table.append((x, y, *src[:3], *dst))
-    if out is not None and table:
-        # what is written shares no memory with anything else
-        spans = sorted([(*_span(t[1]), 1) for t in table] + [(*_span(t[0]), 0) for t in table])
-        end, written = 0, False
-        for first, last, writes in spans:
-            if first < end and (writes or written):
-                raise ValueError("beam_reorder: the addresses of out overlap the states' or its own")
-            if last > end:
-                end, written = last, bool(writes)
+        table.append((x.data_ptr(), y.data_ptr(), *src[:3], *dst))
+        if out is not None:
+            spans.append((*_span(y), True))
+            spans.append((*_span(states[i]), False))
+    # what is written shares no memory with anything else
+    spans.sort()
+    end, written = 0, False
+    for first, last, writes in spans:
+        if first < end and (writes or written):
+            raise ValueError("beam_reorder: the addresses of out overlap the states' or its own")
+        if last > end:
+            end, written = last, writes
     if table:
         with _on(parents.device):
             lsr.lsr_beam_reorder(B, beams, K, _aligned(parents), table)

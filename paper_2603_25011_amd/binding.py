@@ -7,6 +7,7 @@ or cannot be loaded, importing succeeds but every call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import Optional
@@ -42,12 +43,6 @@ class _Desc(ctypes.Structure):
 class _DistillDesc(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int64), ("D", ctypes.c_int64), ("V", ctypes.c_int64), ("K", ctypes.c_int64),
                 ("hw_dtype", ctypes.c_int32), ("temperature", ctypes.c_float)]
-
-
-class _BeamState(ctypes.Structure):
-    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("src_batch", ctypes.c_int64), ("src_beam", ctypes.c_int64),
-                ("src_piece", ctypes.c_int64), ("dst_batch", ctypes.c_int64), ("dst_beam", ctypes.c_int64), ("dst_piece", ctypes.c_int64),
-                ("pieces", ctypes.c_int64), ("piece_bytes", ctypes.c_int64)]
 
 
 def library_path() -> str:
@@ -134,7 +129,7 @@ def load_library():
     lib.lsr_beam_select.restype = ctypes.c_int
     lib.lsr_beam_select.argtypes = [i64, i64, i64, i64, i32, ctypes.c_double, vp, i64, vp, vp, i64, vp, vp, vp, vp, sz, vp]
     lib.lsr_beam_reorder.restype = ctypes.c_int
-    lib.lsr_beam_reorder.argtypes = [i64, i64, i64, vp, i64, ctypes.POINTER(_BeamState), vp]
+    lib.lsr_beam_reorder.argtypes = [i64, i64, i64, vp, i64, vp, vp]          # (a table of lsr_beam_state: ten 64-bit words each)
     lib.lsr_dropout.restype = ctypes.c_int
     lib.lsr_dropout.argtypes = [i64, i32, vp, vp, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, vp, vp]
     lib.lsr_status_string.restype = ctypes.c_char_p
@@ -163,7 +158,7 @@ def _ptr(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -366,28 +361,28 @@ def lsr_fp8_slab_bytes(rows, cols) -> int:
 
 
 def lsr_fp8_quantize(rows, cols, x_dtype, X, ldx, square, Q, ldq, exps, Qt, ldqt, exps_t, stream=None) -> None:
-    _check(load_library().lsr_fp8_quantize(int(rows), int(cols), int(x_dtype), _ptr(X), int(ldx), int(square), _ptr(Q), int(ldq), _ptr(exps),
-                                           _ptr(Qt), int(ldqt), _ptr(exps_t), _stream(stream)))
+    _check(load_library().lsr_fp8_quantize(rows, cols, x_dtype, _ptr(X), ldx, int(square), _ptr(Q), ldq, _ptr(exps), _ptr(Qt), ldqt, _ptr(exps_t),
+                                           _stream(stream)))
 
 
 def lsr_fp8_matmul_workspace_bytes(N, V, K, a_dtype) -> int:
-    return int(load_library().lsr_fp8_matmul_workspace_bytes(int(N), int(V), int(K), int(a_dtype)))
+    return load_library().lsr_fp8_matmul_workspace_bytes(N, V, K, a_dtype)
 
 
 def lsr_fp8_matmul(N, V, K, a_dtype, out_dtype, A, lda, a_exps, W, ldw, w_exps, bias, out, ldo, workspace, stream=None) -> None:
     wp, wb = _ws(workspace)
-    _check(load_library().lsr_fp8_matmul(int(N), int(V), int(K), int(a_dtype), int(out_dtype), _ptr(A), int(lda), _ptr(a_exps),
-                                         _ptr(W), int(ldw), _ptr(w_exps), _ptr(bias), _ptr(out), int(ldo), wp, wb, _stream(stream)))
+    _check(load_library().lsr_fp8_matmul(N, V, K, a_dtype, out_dtype, _ptr(A), lda, _ptr(a_exps), _ptr(W), ldw, _ptr(w_exps), _ptr(bias), _ptr(out), ldo,
+                                         wp, wb, _stream(stream)))
 
 
 def lsr_fp8_backward_workspace_bytes(N, V, D, need_dh=True, need_dw=True, need_db=True) -> int:
-    return int(load_library().lsr_fp8_backward_workspace_bytes(int(N), int(V), int(D), int(need_dh), int(need_dw), int(need_db)))
+    return load_library().lsr_fp8_backward_workspace_bytes(N, V, D, need_dh, need_dw, need_db)
 
 
 def lsr_fp8_backward(N, V, D, y_dtype, h_dtype, dY, ldy, H, ldh, Wt, ldwt, wt_exps, dH, dW, db, workspace, stream=None) -> None:
     wp, wb = _ws(workspace)
-    _check(load_library().lsr_fp8_backward(int(N), int(V), int(D), int(y_dtype), int(h_dtype), _ptr(dY), int(ldy), _ptr(H), int(ldh), _ptr(Wt),
-                                           int(ldwt), _ptr(wt_exps), _ptr(dH), _ptr(dW), _ptr(db), wp, wb, _stream(stream)))
+    _check(load_library().lsr_fp8_backward(N, V, D, y_dtype, h_dtype, _ptr(dY), ldy, _ptr(H), ldh, _ptr(Wt), ldwt, _ptr(wt_exps), _ptr(dH), _ptr(dW),
+                                           _ptr(db), wp, wb, _stream(stream)))
 
 
 # ---- beam search over the dense logits (include/lsr_beam.h) ----
@@ -405,14 +400,15 @@ def lsr_beam_select(B, beams, V, K, x_dtype, temperature, X, ldx, scores, finish
 
 
 def lsr_beam_reorder(B, beams, K, parents, states, stream=None) -> None:
-    """`states`: sequence of tuples (src, dst, src_batch, src_beam, src_piece, dst_batch, dst_beam, dst_piece, pieces, piece_bytes), strides in bytes."""
-    n = len(states)
-    table = (_BeamState * max(n, 1))(*[_BeamState(_ptr(s[0]), _ptr(s[1]), *map(int, s[2:])) for s in states])
-    _check(load_library().lsr_beam_reorder(int(B), int(beams), int(K), _ptr(parents), n, table, _stream(stream)))
+    """`states`: sequence of tuples (src, dst, src_batch, src_beam, src_piece, dst_batch, dst_beam, dst_piece, pieces, piece_bytes), addresses or tensors
+    and strides in bytes."""
+    table = array.array("q")
+    for s in states:
+        table.extend((_ptr(s[0]) or 0, _ptr(s[1]) or 0, *s[2:]))
+    _check(load_library().lsr_beam_reorder(int(B), int(beams), int(K), _ptr(parents), len(states), table.buffer_info()[0], _stream(stream)))
 
 
 # ---- dropout (include/lsr_dropout.h) ----
 
 def lsr_dropout(n, dtype, X, Y, p, seed, offset, state, stream=None) -> None:
-    _check(load_library().lsr_dropout(int(n), int(dtype), _ptr(X), _ptr(Y), float(p), int(seed) % (1 << 64), int(offset) % (1 << 64), _ptr(state),
-                                      _stream(stream)))
+    _check(load_library().lsr_dropout(n, dtype, _ptr(X), _ptr(Y), p, int(seed) % (1 << 64), int(offset) % (1 << 64), _ptr(state), _stream(stream)))

@@ -394,23 +394,34 @@ __global__ __launch_bounds__(Fp8Tile<4>::THREADS, 2) void fp8_grads_kernel(Fp8Jo
         fp8_store<4, OT, false>(s_ring, acc, nullptr, reinterpret_cast<OT*>(j.out), j.ldo, n0, v0, j.N, j.V);
 }
 
-// Sum of the parts of a product whose contracted axis was cut, in order, rounded once.
+// Sum of the parts of a product whose contracted axis was cut, in order, rounded once; for one or two products in a launch.
+struct Fp8Join {
+    const float* part;
+    void* out;
+    int64_t n, pitch;          // values of a part; from part to part
+    int splits;
+    unsigned blocks;           // of 1024 values
+};
 template <typename OT>
-__global__ __launch_bounds__(256) void fp8_join_kernel(const float* __restrict__ part, int64_t pitch, int splits, int64_t n, OT* __restrict__ out) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= n) return;
-    if (i + 4 <= n) {
+__global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Join a, Fp8Join b) {
+    const bool second = blockIdx.x >= a.blocks;
+    const Fp8Join& j = second ? b : a;
+    const int64_t i = ((int64_t)(blockIdx.x - (second ? a.blocks : 0)) * 256 + threadIdx.x) * 4;
+    const float* const part = j.part;
+    OT* const out = reinterpret_cast<OT*>(j.out);
+    if (i >= j.n) return;
+    if (i + 4 <= j.n) {
         float4 s = *reinterpret_cast<const float4*>(part + i);
-        for (int k = 1; k < splits; ++k) {
-            const float4 x = *reinterpret_cast<const float4*>(part + k * pitch + i);
+        for (int k = 1; k < j.splits; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(part + k * j.pitch + i);
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
         }
         if constexpr (sizeof(OT) == 4) *reinterpret_cast<float4*>(out + i) = s;
         else *reinterpret_cast<uint2*>(out + i) = make_uint2(bf16_bits(s.x) | (uint32_t)bf16_bits(s.y) << 16, bf16_bits(s.z) | (uint32_t)bf16_bits(s.w) << 16);
     } else {
-        for (int64_t e = i; e < n; ++e) {
+        for (int64_t e = i; e < j.n; ++e) {
             float s = part[e];
-            for (int k = 1; k < splits; ++k) s += part[k * pitch + e];
+            for (int k = 1; k < j.splits; ++k) s += part[k * j.pitch + e];
             out[e] = as_type<OT>(s);
         }
     }

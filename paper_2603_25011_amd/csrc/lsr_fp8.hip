@@ -152,12 +152,12 @@ int launch_grads(Fp8Job h, Fp8Job w, const GradsPlan& plan, float* h_parts, floa
     if (plan.h_first) fp8_grads_kernel<EXACT, OT><<<grid, Fp8Tile<4>::THREADS, 0, st>>>(h, w, nh, nw);
     else fp8_grads_kernel<EXACT, OT><<<grid, Fp8Tile<4>::THREADS, 0, st>>>(w, h, nw, nh);
     auto join = [&](const Fp8Job& j, const float* parts, void* out) {
-        if (!j.N || j.splits < 2) return;
+        if (!j.N || j.splits < 2) return Fp8Join{};
         const int64_t n = (int64_t)j.N * j.V;
-        fp8_join_kernel<OT><<<(unsigned)((n + 1023) / 1024), 256, 0, st>>>(parts, j.split_pitch, j.splits, n, static_cast<OT*>(out));
+        return Fp8Join{parts, out, n, j.split_pitch, j.splits, (unsigned)((n + 1023) / 1024)};
     };
-    join(h, h_parts, dH);
-    join(w, w_parts, dW);
+    const Fp8Join a = join(h, h_parts, dH), b = join(w, w_parts, dW);
+    if (a.blocks + b.blocks) fp8_join_kernel<OT><<<a.blocks + b.blocks, 256, 0, st>>>(a, b);
     return launch_status();
 }
 
@@ -195,7 +195,7 @@ BackwardWs backward_ws(int64_t N, int64_t V, int64_t D, bool dh, bool dw, bool d
         w.ht = take((size_t)slab_bytes(D, N));
         w.ht_exp = take((size_t)exp_bytes(D, N));
     }
-    if (db) w.sums = take((size_t)((N + 127) / 128) * V * 4);
+    if (db && N > 128) w.sums = take((size_t)((N + 127) / 128) * V * 4);      // (one row tile's sums are the result)
     w.h_parts = take(dh ? part_bytes(plan.h, N * D) : 0);
     w.w_parts = take(dw ? part_bytes(plan.w, V * D) : 0);
     w.total = at;
@@ -293,18 +293,20 @@ int lsr_fp8_backward(int64_t N, int64_t V, int64_t D, int32_t y_dtype, int32_t h
         return LSR_ERR_ALIGN;
     const GradsPlan plan = grads_plan(N, V, D, dH, dW);
     const BackwardWs w = backward_ws(N, V, D, dH, dW, db, plan);
-    if (!workspace || workspace_bytes < w.total) return LSR_ERR_WORKSPACE;
-    if (misaligned(workspace)) return LSR_ERR_ALIGN;
+    if (w.total) {
+        if (!workspace || workspace_bytes < w.total) return LSR_ERR_WORKSPACE;
+        if (misaligned(workspace)) return LSR_ERR_ALIGN;
+    }
     int n_cus = 0;
     int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
     char* const ws = static_cast<char*>(workspace);
     const Fp8Rows g = dH ? fp8_rows(ws + w.g, 0, ws + w.g_exp, V) : Fp8Rows{};
     const Fp8Rows gt = dW ? fp8_rows(ws + w.gt, 0, ws + w.gt_exp, N) : Fp8Rows{}, ht = dW ? fp8_rows(ws + w.ht, 0, ws + w.ht_exp, N) : Fp8Rows{};
-    float* const sums = db ? reinterpret_cast<float*>(ws + w.sums) : nullptr;
+    float* const sums = db && N > 128 ? reinterpret_cast<float*>(ws + w.sums) : db;
     rc = quantize(y_dtype, N, V, dY, ldy, false, g, gt, sums, stream);
     if (rc == LSR_OK && dW) rc = quantize(h_dtype, N, D, H, ldh, false, Fp8Rows{}, ht, nullptr, stream);
-    if (rc == LSR_OK && db) {
+    if (rc == LSR_OK && db && N > 128) {
         fp8_sums_kernel<<<(unsigned)((V + 63) / 64), 256, 0, stream>>>(sums, (int)((N + 127) / 128), V, db);
         rc = launch_status();
     }

@@ -44,7 +44,7 @@ _HERE = contextlib.nullcontext()
 
 def _on(device):
     """With the tensors' device current, whose stream the work goes to."""
-    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
 
 
 @functools.lru_cache(maxsize=256)

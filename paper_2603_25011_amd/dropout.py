@@ -7,7 +7,23 @@ from __future__ import annotations
 import torch
 
 from . import binding as lsr
-from .distill import _kind, _on, _on_gpu
+from .distill import _KIND, _kind, _on_gpu
+
+
+def _draw(x: torch.Tensor, p: float, seed: int, offset: int, state) -> torch.Tensor:
+    # (the backward runs in a thread where every call costs more than the kernel: few of them)
+    if not x.is_contiguous():
+        x = x.contiguous()
+    y = torch.empty_like(x)
+    n = x.numel()
+    if n:
+        dev = x.get_device()
+        if dev == torch._C._cuda_getDevice():
+            lsr.lsr_dropout(n, _KIND[x.dtype], x, y, p, seed, offset, state, torch._C._cuda_getCurrentRawStream(dev))
+        else:
+            with torch.cuda.device(dev):
+                lsr.lsr_dropout(n, _KIND[x.dtype], x, y, p, seed, offset, state)
+    return y
 
 
 class _Dropout(torch.autograd.Function):
@@ -16,17 +32,15 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, p, seed, offset, state):
         ctx.draw = (p, seed, offset)
-        ctx.save_for_backward(state)
-        y = torch.empty_like(x, memory_format=torch.contiguous_format)
-        if x.numel():
-            x = x.contiguous()
-            with _on(x.device):
-                lsr.lsr_dropout(x.numel(), _kind(x, "dropout", "x"), x, y, p, seed, offset, state)
-        return y
+        if state is not None:
+            ctx.save_for_backward(state)
+        return _draw(x, p, seed, offset, state)
 
     @staticmethod
     def backward(ctx, dy):
-        return _Dropout.apply(dy, *ctx.draw, *ctx.saved_tensors), None, None, None, None
+        state = ctx.saved_tensors
+        f = _Dropout.apply if torch.is_grad_enabled() else _draw
+        return f(dy, *ctx.draw, state[0] if state else None), None, None, None, None
 
 
 def dropout(x: torch.Tensor, p: float, seed: int = 0, offset: int = 0, state: torch.Tensor | None = None) -> torch.Tensor:
@@ -42,4 +56,4 @@ def dropout(x: torch.Tensor, p: float, seed: int = 0, offset: int = 0, state: to
         raise ValueError(f"dropout: p is a probability, not {p}")
     if state is not None and (state.dtype != torch.int64 or state.shape != (2,) or not state.is_contiguous()):
         raise ValueError("dropout: state must be a contiguous int64 tensor of two")
-    return _Dropout.apply(x, float(p), int(seed), int(offset), state)
+    return _Dropout.apply(x, float(p), int(seed) % (1 << 64), int(offset) % (1 << 64), state)

@@ -116,6 +116,7 @@ class _Fp8Logits(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dY):
+        # (this runs in a thread where every call costs more than elsewhere: few of them)
         H, W, Wt, exps_t = ctx.saved_tensors
         N, V, D = ctx.shape[:3]
         need_h, need_w, need_b = ctx.needs_input_grad[:3]
@@ -129,11 +130,12 @@ class _Fp8Logits(torch.autograd.Function):
                 if g is not None:
                     g.zero_()
         elif need_h or need_w or need_b:
+            y = _rows(dY)
             with _on(dev):
-                y = _rows(dY.detach())
-                ws = _scratch(_backward_bytes(N, V, D, need_h, need_w, need_b), dev)
+                ws = torch.empty(_backward_bytes(N, V, D, need_h, need_w, need_b), dtype=torch.uint8, device=dev)
                 lsr.lsr_fp8_backward(*ctx.shape, y, _ld(y), H, _ld(H), Wt, 0, exps_t, dH, dW, db, ws)
-            dH, dW, db = first_order_only("fp8_logits", (dH, dW, db), (H, W, dY))
+            if torch.is_grad_enabled():
+                dH, dW, db = first_order_only("fp8_logits", (dH, dW, db), (H, W, dY))
         return dH, dW, db, None
 
 

@@ -74,7 +74,7 @@ def test_fp8_backward_refusals():
     need = binding.lsr_fp8_backward_workspace_bytes(100, 300, 100)
     assert b(ws=None) == WORKSPACE and b(ws=(P, need - 1)) == WORKSPACE and b(ws=(P + 8, need)) == ALIGN
     some = [binding.lsr_fp8_backward_workspace_bytes(100, 300, 100, *(i == j for j in range(3))) for i in range(3)]
-    assert all(0 < s < need for s in some)
+    assert 0 < some[0] < need and 0 < some[1] < need and some[2] == 0 < binding.lsr_fp8_backward_workspace_bytes(129, 300, 100, False, False, True)
 
 
 def test_beam_select_refusals():
