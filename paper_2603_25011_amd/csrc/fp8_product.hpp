@@ -162,121 +162,131 @@ __device__ __forceinline__ void fp8_product(uint8_t* ring, uint32_t* exps, const
     };
     request_all(0);
     request_all(1);
-    if constexpr (!EXACT) {
-        // A slab's fragments are read while the slab before is multiplied: A's and W's last into registers of their own (by parity of the slab), W's others into
-        // those whose products have just been issued.  The slab NS ahead goes to the stage whose slab is in registers.
-        intx8 w0[3], w3[2], fa[2][2];
-        if (nb > 1) {
+    // Of the tile's 32-row blocks of W only those that exist are multiplied: the walk is instantiated per count of the wave's live blocks (1, 2 or 4), so that each
+    // instance is straight-line code.  (A hidden size of 312 pays for 320 of its 512 columns.)
+    auto walk = [&](auto na_c) {
+        constexpr int NA = decltype(na_c)::value, M = 2 * NA;
+        if constexpr (!EXACT) {
+            // A slab's fragments are read while the slab before is multiplied: A's and W's last into registers of their own (by parity of the slab), W's others into
+            // those whose products have just been issued.  The slab NS ahead goes to the stage whose slab is in registers.
+            intx8 w0[NA], w3[2], fa[2][2];           // (w0[NA - 1] is not used)
+            if (nb > 1) {
 #pragma unroll
-            for (int k = 2; k < NS; ++k) request_all(k);
-            fence(std::integral_constant<int, NS - 1>{});
+                for (int k = 2; k < NS; ++k) request_all(k);
+                fence(std::integral_constant<int, NS - 1>{});
+            } else {
+                fence(I1{});
+            }
+            read_exps(0);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) fa[0][c] = read_a(ring, c);
+#pragma unroll
+            for (int i = 0; i + 1 < NA; ++i) w0[i] = read_w(ring, i);
+            w3[0] = read_w(ring, NA - 1);
+            // one slab: NEXT: there is another, whose fragments are read; MORE: slab kt + NS is requested
+            auto step = [&](int blk, auto cur_c, auto next_c, auto more_c) {
+                constexpr int CUR = decltype(cur_c)::value, NXT = CUR ^ 1, NEXT = decltype(next_c)::value, MORE = decltype(more_c)::value;
+                const uint8_t* const s = ring + stage_after(st, 1) * G::STAGE;
+                const int ahead = 2 * blk + CUR + NS;
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    const int i = m >> 1, c = m & 1;
+                    acc[i][c] = mma_scaled(i < NA - 1 ? w0[i] : w3[CUR], fa[CUR][c], acc[i][c], bw[i], ba[c]);
+                    if constexpr (NEXT) {
+                        if (m < 2) fa[NXT][m] = read_a(s, m);
+                        if (m == (NA == 1 ? 0 : 2)) w3[NXT] = read_w(s, NA - 1);
+                        if (m >= 3 && m - 3 < NA - 1) w0[m - 3] = read_w(s, m - 3);
+                    }
+                    if constexpr (MORE) {
+#pragma unroll
+                        for (int n = m; n < LPT; n += M) request(st, ahead, n);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                // (the next block's word of powers, its own again or another: a branch here, and the compiler moves the products behind it)
+                if constexpr (CUR == 1 && NEXT) read_exps((blk + 1) >> 2);
+                st = stage_after(st, 1);
+            };
+            int blk = 0;
+            for (; blk + 2 < nb; ++blk) {
+                fence(Some{});
+                block_exps(blk);
+                next_word(blk);
+                step(blk, I0{}, I1{}, I1{});
+                fence(Some{});
+                step(blk, I1{}, I1{}, I1{});
+            }
+            if (blk + 1 < nb) {
+                fence(Some{});
+                block_exps(blk);
+                step(blk, I0{}, I1{}, std::integral_constant<int, NS == 3>{});
+                fence(I1{});
+                step(blk, I1{}, I1{}, I0{});
+                ++blk;
+            }
+            fence(I0{});
+            block_exps(blk);
+            step(blk, I0{}, I1{}, I0{});
+            step(blk, I1{}, I0{}, I0{});
         } else {
+            // One slab after the other: widening takes the registers that fragments of the next would need.  The slab NS - 1 ahead goes to the stage of the slab before.
+            if (NS == 4 && nb > 1) request_all(2);
+            auto step = [&](int blk, auto cur_c, auto more_c) {
+                constexpr int CUR = decltype(cur_c)::value;
+                const uint8_t* const s = ring + st * G::STAGE;
+                const int to = stage_after(st, NS - 1), ahead = 2 * blk + CUR + NS - 1;
+                if constexpr (CUR == 0) {
+                    if ((blk & 3) == 0) read_exps(blk >> 2);
+                }
+                intx8 fa[2], fw[NA];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) fa[c] = read_a(s, c);
+#pragma unroll
+                for (int i = 0; i < NA; ++i) fw[i] = read_w(s, i);
+                if constexpr (CUR == 0) block_exps(blk);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    bf16x8 a[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) a[c] = widen((uint32_t)fa[c][2 * j], (uint32_t)fa[c][2 * j + 1], exp_value(ba[c]));
+#pragma unroll
+                    for (int i = 0; i < NA; ++i) {
+                        const bf16x8 w = widen((uint32_t)fw[i][2 * j], (uint32_t)fw[i][2 * j + 1], exp_value(bw[i]));
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) acc[i][c] = mma_chunk(w, a[c], acc[i][c]);
+                    }
+                    if constexpr (decltype(more_c)::value) {
+                        request(to, ahead, j);
+                        if (j < LPT - 4) request(to, ahead, 4 + j);
+                    }
+                }
+                st = stage_after(st, 1);
+            };
+            int blk = 0;
+            for (; blk + 2 < nb; ++blk) {
+                fence(Some{});
+                next_word(blk);
+                step(blk, I0{}, I1{});
+                fence(Some{});
+                step(blk, I1{}, I1{});
+            }
+            if (blk + 1 < nb) {
+                fence(Some{});
+                step(blk, I0{}, I1{});
+                fence(Some{});
+                step(blk, I1{}, std::integral_constant<int, NS == 3>{});
+                ++blk;
+            }
             fence(I1{});
+            step(blk, I0{}, I0{});
+            fence(I0{});
+            step(blk, I1{}, I0{});
         }
-        read_exps(0);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) fa[0][c] = read_a(ring, c);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) w0[i] = read_w(ring, i);
-        w3[0] = read_w(ring, 3);
-        // one slab: NEXT: there is another, whose fragments are read; MORE: slab kt + NS is requested
-        auto step = [&](int blk, auto cur_c, auto next_c, auto more_c) {
-            constexpr int CUR = decltype(cur_c)::value, NXT = CUR ^ 1, NEXT = decltype(next_c)::value, MORE = decltype(more_c)::value;
-            const uint8_t* const s = ring + stage_after(st, 1) * G::STAGE;
-            const int ahead = 2 * blk + CUR + NS;
-#pragma unroll
-            for (int m = 0; m < 8; ++m) {
-                const int i = m >> 1, c = m & 1;
-                acc[i][c] = mma_scaled(i < 3 ? w0[i < 3 ? i : 0] : w3[CUR], fa[CUR][c], acc[i][c], bw[i], ba[c]);
-                if constexpr (NEXT) {
-                    if (m < 2) fa[NXT][m] = read_a(s, m);
-                    else if (m == 2) w3[NXT] = read_w(s, 3);
-                    else if (m < 6) w0[m - 3] = read_w(s, m - 3);
-                }
-                if constexpr (MORE) {
-                    if (m < LPT) request(st, ahead, m);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            // (the next block's word of powers, its own again or another: a branch here, and the compiler moves the products behind it)
-            if constexpr (CUR == 1 && NEXT) read_exps((blk + 1) >> 2);
-            st = stage_after(st, 1);
-        };
-        int blk = 0;
-        for (; blk + 2 < nb; ++blk) {
-            fence(Some{});
-            block_exps(blk);
-            next_word(blk);
-            step(blk, I0{}, I1{}, I1{});
-            fence(Some{});
-            step(blk, I1{}, I1{}, I1{});
-        }
-        if (blk + 1 < nb) {
-            fence(Some{});
-            block_exps(blk);
-            step(blk, I0{}, I1{}, std::integral_constant<int, NS == 3>{});
-            fence(I1{});
-            step(blk, I1{}, I1{}, I0{});
-            ++blk;
-        }
-        fence(I0{});
-        block_exps(blk);
-        step(blk, I0{}, I1{}, I0{});
-        step(blk, I1{}, I0{}, I0{});
-    } else {
-        // One slab after the other: widening takes the registers that fragments of the next would need.  The slab NS - 1 ahead goes to the stage of the slab before.
-        if (NS == 4 && nb > 1) request_all(2);
-        auto step = [&](int blk, auto cur_c, auto more_c) {
-            constexpr int CUR = decltype(cur_c)::value;
-            const uint8_t* const s = ring + st * G::STAGE;
-            const int to = stage_after(st, NS - 1), ahead = 2 * blk + CUR + NS - 1;
-            if constexpr (CUR == 0) {
-                if ((blk & 3) == 0) read_exps(blk >> 2);
-            }
-            intx8 fa[2], fw[4];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) fa[c] = read_a(s, c);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) fw[i] = read_w(s, i);
-            if constexpr (CUR == 0) block_exps(blk);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                bf16x8 a[2];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) a[c] = widen((uint32_t)fa[c][2 * j], (uint32_t)fa[c][2 * j + 1], exp_value(ba[c]));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bf16x8 w = widen((uint32_t)fw[i][2 * j], (uint32_t)fw[i][2 * j + 1], exp_value(bw[i]));
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) acc[i][c] = mma_chunk(w, a[c], acc[i][c]);
-                }
-                if constexpr (decltype(more_c)::value) {
-                    request(to, ahead, j);
-                    if (j < LPT - 4) request(to, ahead, 4 + j);
-                }
-            }
-            st = stage_after(st, 1);
-        };
-        int blk = 0;
-        for (; blk + 2 < nb; ++blk) {
-            fence(Some{});
-            next_word(blk);
-            step(blk, I0{}, I1{});
-            fence(Some{});
-            step(blk, I1{}, I1{});
-        }
-        if (blk + 1 < nb) {
-            fence(Some{});
-            step(blk, I0{}, I1{});
-            fence(Some{});
-            step(blk, I1{}, std::integral_constant<int, NS == 3>{});
-            ++blk;
-        }
-        fence(I1{});
-        step(blk, I0{}, I0{});
-        fence(I0{});
-        step(blk, I1{}, I0{});
-    }
+    };
+    const int live = __builtin_amdgcn_readfirstlane((W.last / 32 + 2 - t.wm) >> 1);      // of the wave's four row blocks wm, wm + 2, ...
+    if (live > 2) walk(std::integral_constant<int, 4>{});
+    else if (live == 2) walk(std::integral_constant<int, 2>{});
+    else walk(std::integral_constant<int, 1>{});
 }
 
 // A product, cut along its contracted axis into `splits` parts that have a result each.
