@@ -370,19 +370,19 @@ __device__ __forceinline__ void fp8_store(uint8_t* ring, const floatx16 (&acc)[4
 }
 
 // Logits.
-template <bool EXACT, int WN, typename OT, bool PAST>
-__global__ __launch_bounds__(Fp8Tile<WN>::THREADS, 2) void fp8_tile_kernel(Fp8Job j, const float* bias) {
-    typedef Fp8Tile<WN> G;
+template <bool EXACT, typename OT, bool PAST>
+__global__ __launch_bounds__(Fp8Tile<2>::THREADS, 2) void fp8_tile_kernel(Fp8Job j, const float* bias) {
+    typedef Fp8Tile<2> G;
     __shared__ __attribute__((aligned(1024))) uint8_t s_ring[G::RING];
     __shared__ __attribute__((aligned(16))) uint32_t s_exps[2 * G::EXP_WORDS];
     __shared__ __attribute__((aligned(16))) float s_bs[TP_T];
     int u, n0, v0, split;
     if (!xcd_unit(j.na * j.nb, u)) return;
     floatx16 acc[4][2];
-    fp8_unit<EXACT, WN>(j, u, s_ring, s_exps, acc, n0, v0, split);
+    fp8_unit<EXACT, 2>(j, u, s_ring, s_exps, acc, n0, v0, split);
     const int tid = threadIdx.x;
     if (tid < TP_T) s_bs[tid] = bias ? bias[min(v0 + tid, j.V - 1)] : 0.f;      // (published by the store's first barrier)
-    fp8_store<WN, OT, PAST>(s_ring, acc, s_bs, reinterpret_cast<OT*>(j.out), j.ldo, n0, v0, j.N, j.V);
+    fp8_store<2, OT, PAST>(s_ring, acc, s_bs, reinterpret_cast<OT*>(j.out), j.ldo, n0, v0, j.N, j.V);
 }
 
 // The two products of a backward in one launch, so that one's last units run beside the other's first: every XCD takes an eighth of either job, `first`'s units before

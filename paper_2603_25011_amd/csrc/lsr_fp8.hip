@@ -17,9 +17,6 @@ constexpr int64_t MAX_AXIS = int64_t(1) << 22;
 constexpr int64_t MAX_VALUES = int64_t(1) << 36;
 constexpr int64_t MAX_HIDDEN = 65536;
 constexpr int64_t MAX_LD = int64_t(1) << 23;
-// Logits in tiles of 256 x 256 from that many slabs of 64 values on.
-constexpr int WIDE_SLABS = 64;
-constexpr size_t CACHE_BYTES = size_t(1) << 28;       // the memory-side cache
 
 inline bool float_type(int32_t t) { return t == LSR_F32 || t == LSR_BF16; }
 inline size_t type_bytes(int32_t t) { return t == LSR_F32 ? 4 : 2; }
@@ -70,18 +67,23 @@ Fp8Job job(int64_t N, int64_t V, int64_t K, const Fp8Rows& A, const Fp8Rows& W, 
     return j;
 }
 
-template <bool EXACT, int WN, typename OT>
-int launch_logits(Fp8Job& j, const float* bias, hipStream_t st) {
-    fp8_tiles<WN>(j);
-    const unsigned grid = xcd_grid(fp8_units(j));
-    if ((size_t)j.N * j.V * sizeof(OT) >= CACHE_BYTES) fp8_tile_kernel<EXACT, WN, OT, true><<<grid, Fp8Tile<WN>::THREADS, 0, st>>>(j, bias);
-    else fp8_tile_kernel<EXACT, WN, OT, false><<<grid, Fp8Tile<WN>::THREADS, 0, st>>>(j, bias);
-    return launch_status();
+// Logits leave past the caches where they would push out operands that are read again: results larger than the memory-side cache whose products take a while, and all that are much
+// larger.  us through the caches : past them, V = 30522, bfloat16 results (float32 results of half the rows are alike):
+//   K = 256     2048 rows (125 MB) 41 : 53    4096 rows (250 MB) 72 : 105    7168 rows (438 MB) 140 : 177    8192 rows (500 MB) 199 : 198
+//   K = 768     2048 rows 64 : 69    4096 rows 123 : 125    7168 rows 221 : 223    8192 rows 316 : 252
+//   K = 1024    2048 rows 72 : 76    4096 rows 157 : 147    7168 rows 256 : 237    8192 rows 374 : 260
+bool past_caches(const Fp8Job& j, size_t bytes) {
+    const size_t all = (size_t)j.N * j.V * bytes;
+    return all >= (size_t(7) << 26) || (all >= (size_t(1) << 28) && j.slabs * FP_SLAB >= 640);
 }
-int logits(Fp8Job& j, const float* bias, int32_t out_type, hipStream_t st) {
-    const bool wide = j.slabs >= WIDE_SLABS;
-    if (out_type == LSR_F32) return wide ? launch_logits<true, 4, float>(j, bias, st) : launch_logits<true, 2, float>(j, bias, st);
-    return wide ? launch_logits<false, 4, uint16_t>(j, bias, st) : launch_logits<false, 2, uint16_t>(j, bias, st);
+// Tiles of 256 x 128 for any K: 8192 x 30522 logits in bfloat16 at K = 768, 1024, 2048, 4096: 252, 260, 542, 968 us, in tiles of 256 x 256 291, 358, 546, 981.
+template <bool EXACT, typename OT>
+int launch_logits(Fp8Job& j, const float* bias, hipStream_t st) {
+    fp8_tiles<2>(j);
+    const unsigned grid = xcd_grid(fp8_units(j));
+    if (past_caches(j, sizeof(OT))) fp8_tile_kernel<EXACT, OT, true><<<grid, Fp8Tile<2>::THREADS, 0, st>>>(j, bias);
+    else fp8_tile_kernel<EXACT, OT, false><<<grid, Fp8Tile<2>::THREADS, 0, st>>>(j, bias);
+    return launch_status();
 }
 
 // The launch of a backward's two products: dH (contracted over the vocabulary) and dW (over the tokens), tiles of 256 x 256, one workgroup per CU at a time.  Either may be
@@ -273,7 +275,7 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
         if (rc != LSR_OK) return rc;
     }
     Fp8Job j = job(N, V, K, states, weights, out, ldo);
-    return logits(j, bias, out_dtype, stream);
+    return out_dtype == LSR_F32 ? launch_logits<true, float>(j, bias, stream) : launch_logits<false, uint16_t>(j, bias, stream);
 }
 
 size_t lsr_fp8_backward_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t need_dh, int32_t need_dw, int32_t need_db) {
