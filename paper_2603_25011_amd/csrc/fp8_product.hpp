@@ -62,7 +62,7 @@ struct Fp8Operand {
 };
 __device__ __forceinline__ Fp8Operand fp8_operand(const Fp8Rows& q, int64_t rows, int64_t row0, int slab0) {
     Fp8Operand o;
-    o.base = reinterpret_cast<const char*>(q.at(row0, (int64_t)slab0 * FP_SLAB));
+    o.base = reinterpret_cast<const char*>(q.at((int)row0, slab0 * FP_SLAB));
     o.pitch = q.ld ? (uint32_t)q.ld : FP_SLAB;
     o.step = q.ld ? FP_SLAB : (uint32_t)FP_SLAB_BYTES;
     o.last = (int)min((int64_t)TP_T, rows - row0) - 1;
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(Fp8Tile<4>::THREADS, 2) void fp8_grads_kernel(Fp8Jo
         fp8_store<4, OT, false>(s_ring, acc, nullptr, reinterpret_cast<OT*>(j.out), j.ldo, n0, v0, j.N, j.V);
 }
 
-// Sum of the parts of a product whose contracted axis was cut, in order, rounded once; for one or two products in a launch.
+// What is left of a backward, in one launch: the sum of the parts of either product whose contracted axis was cut, in order, rounded once; and the sums of the columns.
 struct Fp8Join {
     const float* part;
     void* out;
@@ -413,10 +413,16 @@ struct Fp8Join {
     unsigned blocks;           // of 1024 values
 };
 template <typename OT>
-__global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Join a, Fp8Join b) {
-    const bool second = blockIdx.x >= a.blocks;
+__global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Sums sums, Fp8Join a, Fp8Join b) {
+    __shared__ float s_part[4][64];
+    if (blockIdx.x < sums.blocks) {
+        fp8_sum_columns(sums, blockIdx.x, s_part);
+        return;
+    }
+    const unsigned block = blockIdx.x - sums.blocks;
+    const bool second = block >= a.blocks;
     const Fp8Join& j = second ? b : a;
-    const int64_t i = ((int64_t)(blockIdx.x - (second ? a.blocks : 0)) * 256 + threadIdx.x) * 4;
+    const int64_t i = ((int64_t)(block - (second ? a.blocks : 0)) * 256 + threadIdx.x) * 4;
     const float* const part = j.part;
     OT* const out = reinterpret_cast<OT*>(j.out);
     if (i >= j.n) return;

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "quantize.hpp"
 
 namespace lsr {
@@ -48,7 +50,7 @@ template <> struct Eight<float> {
     static __device__ __forceinline__ uint32_t four_down(const Eight& a, const Eight& b, const Eight& c, const Eight& d, int j, float e) {
         return four_of(a.w[j], b.w[j], c.w[j], d.w[j], e);
     }
-    __device__ __forceinline__ void load(const float* row, int64_t c, int64_t cols) {
+    __device__ __forceinline__ void load(const float* row, int c, int cols) {
         typedef uint32_t V4 __attribute__((ext_vector_type(4)));
         typedef V4 F4 __attribute__((aligned(4)));
         if (c + 8 <= cols) {
@@ -87,7 +89,7 @@ template <> struct Eight<uint16_t> {
         const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;      // the same half of two words
         return four_of(__builtin_amdgcn_perm(b.w[j >> 1], a.w[j >> 1], pick), __builtin_amdgcn_perm(d.w[j >> 1], c.w[j >> 1], pick), e);
     }
-    __device__ __forceinline__ void load(const uint16_t* row, int64_t c, int64_t cols) {
+    __device__ __forceinline__ void load(const uint16_t* row, int c, int cols) {
         typedef uint32_t V4 __attribute__((ext_vector_type(4)));
         typedef V4 U4 __attribute__((aligned(2)));
         if (c + 8 <= cols) {
@@ -128,7 +130,7 @@ struct Fp8Rows {
     int64_t ld;
     int64_t slabs;           // per row (used where ld = 0)
     uint8_t* exps;           // four powers of a row beside each other
-    __device__ __forceinline__ uint8_t* at(int64_t row, int64_t c) const {
+    __device__ __forceinline__ uint8_t* at(int row, int c) const {
         return ld ? q + row * ld + c : q + ((row >> 8) * slabs + (c >> 6)) * FP_SLAB_BYTES + (row & 255) * FP_SLAB + (c & 63);
     }
 };
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(FQ_THREADS) void fp8_rows_kernel(const T* __restric
         Eight<T> x;
         x.load(row, c, cols);
         const uint32_t e = block_exp(row_most(x));
-        if (c < padded) *reinterpret_cast<uint2*>(Q.at(r, c)) = make_uint2(x.four(0, exp_value(e)), x.four(4, exp_value(e)));
+        if (c < padded) *reinterpret_cast<uint2*>(Q.at((int)r, c)) = make_uint2(x.four(0, exp_value(e)), x.four(4, exp_value(e)));
         uint32_t four = e << ((lane >> 4) * 8);
         four |= (uint32_t)__shfl_xor((int)four, 16);
         four |= (uint32_t)__shfl_xor((int)four, 32);
@@ -159,30 +161,34 @@ __global__ __launch_bounds__(FQ_THREADS) void fp8_rows_kernel(const T* __restric
 // Both forms from one read: a workgroup takes 128 rows x 128 columns, a thread 8 x 8 of them, which it keeps in registers as they are stored.  The transposed form goes
 // through LDS (8 rows of a column are 8 bytes, XORed so that the 16 lanes of a write lie on different banks) and leaves in whole lines.
 //   SQUARE  one power for all 128 x 128; else one per row (Q) and one per column (Qt)
-//   SUMS    the sums of the columns over these 128 rows go to `sums` [row tiles][cols], in float32 and a fixed order
+// Where `sums` is not null the sums of the columns over these 128 rows go there, [row tiles][cols], in float32 and a fixed order.
 struct Fp8TileParams {
     const void* X;
     int64_t ldx;
-    int64_t rows, cols;
+    int rows, cols;
     Fp8Rows Q;               // [rows], q may be null
     Fp8Rows Qt;              // [cols], q may be null
     float* sums;
     int row_tiles, col_tiles;
 };
-template <typename T, bool SQUARE, bool SUMS>
-__global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_tile_quantize_kernel(Fp8TileParams p) {
+struct Fp8TileShared {
+    __attribute__((aligned(16))) uint8_t t[128 * 128];
+    __attribute__((aligned(16))) uint32_t most[4][128];
+};
+template <typename T, bool SQUARE>
+__device__ __forceinline__ void fp8_quantize_tile(const Fp8TileParams& p, unsigned block, Fp8TileShared& sh) {
     typedef Eight<T> E;
-    __shared__ __attribute__((aligned(16))) uint8_t s_t[128 * 128];
-    __shared__ __attribute__((aligned(16))) uint32_t s_max[4][128];
+    uint8_t* const s_t = sh.t;
+    uint32_t (&s_max)[4][128] = sh.most;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = tid & 15, g = tid >> 4;
-    const int64_t ct = blockIdx.x % p.col_tiles, rt = blockIdx.x / p.col_tiles;
-    const int64_t r0 = rt * 128 + g * 8, c0 = ct * 128 + l16 * 8;
+    const int rt = (int)(block / (unsigned)p.col_tiles), ct = (int)block - rt * p.col_tiles;
+    const int r0 = rt * 128 + g * 8, c0 = ct * 128 + l16 * 8;
     const T* const X = reinterpret_cast<const T*>(p.X);
     E x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (r0 + i < p.rows) {
-            x[i].load(X + (r0 + i) * p.ldx, c0, p.cols);
+            x[i].load(X + (int64_t)(r0 + i) * p.ldx, c0, p.cols);
         } else {
 #pragma unroll
             for (int j = 0; j < E::WORDS; ++j) x[i].w[j] = 0;
@@ -219,12 +225,12 @@ __global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_tile_q
         if (p.Q.q && l16 == 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (r0 + i < p.rows) p.Q.exps[((ct >> 2) * p.rows + r0 + i) * 4 + (ct & 3)] = (uint8_t)e;
+                if (r0 + i < p.rows) p.Q.exps[((int64_t)(ct >> 2) * p.rows + r0 + i) * 4 + (ct & 3)] = (uint8_t)e;
         }
         if (p.Qt.q && g == 0) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (c0 + j < p.cols) p.Qt.exps[((rt >> 2) * p.cols + c0 + j) * 4 + (rt & 3)] = (uint8_t)e;
+                if (c0 + j < p.cols) p.Qt.exps[((int64_t)(rt >> 2) * p.cols + c0 + j) * 4 + (rt & 3)] = (uint8_t)e;
         }
     } else if (p.Qt.q) {
 #pragma unroll
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_tile_q
                 for (int o = 8; o; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
                 const uint32_t e = block_exp(m);
                 f = exp_value(e);
-                if (l16 == 0 && r0 + i < p.rows) p.Q.exps[((ct >> 2) * p.rows + r0 + i) * 4 + (ct & 3)] = (uint8_t)e;
+                if (l16 == 0 && r0 + i < p.rows) p.Q.exps[((int64_t)(ct >> 2) * p.rows + r0 + i) * 4 + (ct & 3)] = (uint8_t)e;
             }
             if (r0 + i < p.rows) *reinterpret_cast<uint2*>(p.Q.at(r0 + i, c0)) = make_uint2(x[i].four(0, f), x[i].four(4, f));
         }
@@ -259,7 +265,7 @@ __global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_tile_q
                 const int k = l16 * E::COLS + j * E::COLS / 8;
                 const uint32_t e = block_exp(E::column(E::most(E::most(s_max[0][k], s_max[1][k]), E::most(s_max[2][k], s_max[3][k])), j));
                 f = exp_value(e);
-                if (g == 0 && c0 + j < p.cols) p.Qt.exps[((rt >> 2) * p.cols + c0 + j) * 4 + (rt & 3)] = (uint8_t)e;
+                if (g == 0 && c0 + j < p.cols) p.Qt.exps[((int64_t)(rt >> 2) * p.cols + c0 + j) * 4 + (rt & 3)] = (uint8_t)e;
             }
             *reinterpret_cast<uint2*>(s_t + (l16 * 8 + j) * 128 + ((g ^ l16) << 3)) =
                 make_uint2(E::four_down(x[0], x[1], x[2], x[3], j, f), E::four_down(x[4], x[5], x[6], x[7], j, f));
@@ -274,7 +280,7 @@ __global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_tile_q
                     *reinterpret_cast<const uint2*>(s_t + c * 128 + ((piece ^ (c >> 3)) << 3));
         }
     }
-    if constexpr (SUMS) {
+    if (p.sums) {
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -287,22 +293,48 @@ __global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_tile_q
         }
         __syncthreads();
         if (tid < 128 && ct * 128 + tid < p.cols)
-            p.sums[rt * p.cols + ct * 128 + tid] = (__uint_as_float(s_max[0][tid]) + __uint_as_float(s_max[1][tid])) +
+            p.sums[(int64_t)rt * p.cols + ct * 128 + tid] = (__uint_as_float(s_max[0][tid]) + __uint_as_float(s_max[1][tid])) +
                                                    (__uint_as_float(s_max[2][tid]) + __uint_as_float(s_max[3][tid]));
     }
 }
 
+template <typename T, bool SQUARE>
+__global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_tile_quantize_kernel(Fp8TileParams p) {
+    __shared__ Fp8TileShared sh;
+    fp8_quantize_tile<T, SQUARE>(p, blockIdx.x, sh);
+}
+// What a backward takes of the gradients of the logits (TY) and of the hidden states (TH), in one launch: a launch of its own costs the host, and the chip where there are few tokens, more
+// than the hidden states' tiles.
+template <typename TY, typename TH>
+__global__ __launch_bounds__(FQ_THREADS, sizeof(TY) + sizeof(TH) > 4 ? 3 : 4) void fp8_backward_quantize_kernel(Fp8TileParams y, Fp8TileParams h, unsigned n_y) {
+    __shared__ Fp8TileShared sh;
+    const bool second = blockIdx.x >= n_y;
+    const unsigned block = second ? blockIdx.x - n_y : blockIdx.x;
+    if constexpr (std::is_same<TY, TH>::value) {
+        fp8_quantize_tile<TY, false>(second ? h : y, block, sh);
+    } else {
+        if (second) fp8_quantize_tile<TH, false>(h, block, sh);
+        else fp8_quantize_tile<TY, false>(y, block, sh);
+    }
+}
+
 // Sums of the columns over all row tiles: a workgroup takes 64 columns, four threads a column.
-__global__ __launch_bounds__(256) void fp8_sums_kernel(const float* __restrict__ sums, int row_tiles, int64_t cols, float* __restrict__ out) {
-    __shared__ float s_part[4][64];
+struct Fp8Sums {
+    const float* sums;
+    float* out;
+    int64_t cols;
+    int row_tiles;
+    unsigned blocks;
+};
+__device__ __forceinline__ void fp8_sum_columns(const Fp8Sums& p, unsigned block, float (&s_part)[4][64]) {
     const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + l;
+    const int64_t c = (int64_t)block * 64 + l;
     float s = 0.f;
-    if (c < cols)
-        for (int t = w; t < row_tiles; t += 4) s += sums[t * cols + c];
+    if (c < p.cols)
+        for (int t = w; t < p.row_tiles; t += 4) s += p.sums[t * p.cols + c];
     s_part[w][l] = s;
     __syncthreads();
-    if (w == 0 && c < cols) out[c] = (s_part[0][l] + s_part[1][l]) + (s_part[2][l] + s_part[3][l]);
+    if (w == 0 && c < p.cols) p.out[c] = (s_part[0][l] + s_part[1][l]) + (s_part[2][l] + s_part[3][l]);
 }
 
 }  // namespace lsr

@@ -12,7 +12,7 @@ namespace {
 
 using namespace lsr;
 
-// Launches stay below 2^32 threads: 64 per row, 256 per 128 x 128 values, 256 per tile of 128 x 256 results.
+// Launches stay below 2^32 threads: 64 per row, 256 per 128 x 128 values (of two arrays of a backward: at most 2^23 tiles together), 256 per tile of 128 x 256 results.
 constexpr int64_t MAX_AXIS = int64_t(1) << 22;
 constexpr int64_t MAX_VALUES = int64_t(1) << 36;
 constexpr int64_t MAX_HIDDEN = 65536;
@@ -33,26 +33,33 @@ Fp8Rows fp8_rows(const void* q, int64_t ld, const void* exps, int64_t cols) {
 }
 inline int64_t slab_bytes(int64_t rows, int64_t cols) { return up(rows, 256) * up(cols, 128); }
 
+Fp8TileParams tiles_of(int64_t rows, int64_t cols, const void* X, int64_t ldx, const Fp8Rows& q, const Fp8Rows& qt) {
+    Fp8TileParams p = {};
+    p.X = X; p.ldx = ldx; p.rows = (int)rows; p.cols = (int)cols;
+    p.Q = q; p.Qt = qt;
+    p.row_tiles = (int)((rows + 127) / 128); p.col_tiles = (int)((cols + 127) / 128);
+    return p;
+}
+unsigned blocks_of(const Fp8TileParams& p) { return (unsigned)((int64_t)p.row_tiles * p.col_tiles); }
+
 template <typename T>
-int quantize_as(int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Fp8Rows& q, const Fp8Rows& qt, float* sums, hipStream_t st) {
-    if (!square && q.q && !qt.q && !sums) {
+int quantize_as(int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Fp8Rows& q, const Fp8Rows& qt, hipStream_t st) {
+    if (!square && !qt.q) {
         fp8_rows_kernel<T><<<(unsigned)((rows + 3) / 4), FQ_THREADS, 0, st>>>(static_cast<const T*>(X), ldx, rows, (int)cols, q);
         return launch_status();
     }
-    Fp8TileParams p = {};
-    p.X = X; p.ldx = ldx; p.rows = rows; p.cols = cols;
-    p.Q = q; p.Qt = qt;
-    p.sums = sums;
-    p.row_tiles = (int)((rows + 127) / 128); p.col_tiles = (int)((cols + 127) / 128);
-    const unsigned grid = (unsigned)((int64_t)p.row_tiles * p.col_tiles);
-    if (square) fp8_tile_quantize_kernel<T, true, false><<<grid, FQ_THREADS, 0, st>>>(p);
-    else if (sums) fp8_tile_quantize_kernel<T, false, true><<<grid, FQ_THREADS, 0, st>>>(p);
-    else fp8_tile_quantize_kernel<T, false, false><<<grid, FQ_THREADS, 0, st>>>(p);
+    const Fp8TileParams p = tiles_of(rows, cols, X, ldx, q, qt);
+    if (square) fp8_tile_quantize_kernel<T, true><<<blocks_of(p), FQ_THREADS, 0, st>>>(p);
+    else fp8_tile_quantize_kernel<T, false><<<blocks_of(p), FQ_THREADS, 0, st>>>(p);
     return launch_status();
 }
-int quantize(int32_t type, int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Fp8Rows& q, const Fp8Rows& qt, float* sums, hipStream_t st) {
-    return type == LSR_F32 ? quantize_as<float>(rows, cols, X, ldx, square, q, qt, sums, st)
-                           : quantize_as<uint16_t>(rows, cols, X, ldx, square, q, qt, sums, st);
+int quantize(int32_t type, int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Fp8Rows& q, const Fp8Rows& qt, hipStream_t st) {
+    return type == LSR_F32 ? quantize_as<float>(rows, cols, X, ldx, square, q, qt, st) : quantize_as<uint16_t>(rows, cols, X, ldx, square, q, qt, st);
+}
+template <typename TY, typename TH>
+void backward_quantize(const Fp8TileParams& y, const Fp8TileParams& h, hipStream_t st) {
+    const unsigned n = blocks_of(y);
+    fp8_backward_quantize_kernel<TY, TH><<<n + blocks_of(h), FQ_THREADS, 0, st>>>(y, h, n);
 }
 
 // ---- products ----
@@ -136,9 +143,9 @@ GradsPlan grads_plan(int64_t N, int64_t V, int64_t D, bool dh, bool dw) {
 }
 size_t part_bytes(const Cut& c, int64_t n) { return c.splits > 1 ? align_up((size_t)c.splits * up(n, 4) * 4) : 0; }
 
-// Both products of a backward, dh and dw without cuts or parts as yet; a job without units (N = 0) is none.
+// Both products of a backward, h and w without cuts or parts as yet, and the sums of the columns; a job without units (N = 0) is none.
 template <bool EXACT, typename OT>
-int launch_grads(Fp8Job h, Fp8Job w, const GradsPlan& plan, float* h_parts, float* w_parts, hipStream_t st) {
+int launch_grads(Fp8Job h, Fp8Job w, const GradsPlan& plan, float* h_parts, float* w_parts, const Fp8Sums& sums, hipStream_t st) {
     auto prepare = [](Fp8Job& j, const Cut& c, float* parts) -> int {
         if (!j.N) return 0;
         j.splits = c.splits;
@@ -151,15 +158,18 @@ int launch_grads(Fp8Job h, Fp8Job w, const GradsPlan& plan, float* h_parts, floa
     void* const dW = w.out;
     const int nh = prepare(h, plan.h, h_parts), nw = prepare(w, plan.w, w_parts);
     const unsigned grid = xcd_grid(nh) + xcd_grid(nw);
-    if (plan.h_first) fp8_grads_kernel<EXACT, OT><<<grid, Fp8Tile<4>::THREADS, 0, st>>>(h, w, nh, nw);
-    else fp8_grads_kernel<EXACT, OT><<<grid, Fp8Tile<4>::THREADS, 0, st>>>(w, h, nw, nh);
+    if (grid) {
+        if (plan.h_first) fp8_grads_kernel<EXACT, OT><<<grid, Fp8Tile<4>::THREADS, 0, st>>>(h, w, nh, nw);
+        else fp8_grads_kernel<EXACT, OT><<<grid, Fp8Tile<4>::THREADS, 0, st>>>(w, h, nw, nh);
+    }
     auto join = [&](const Fp8Job& j, const float* parts, void* out) {
         if (!j.N || j.splits < 2) return Fp8Join{};
         const int64_t n = (int64_t)j.N * j.V;
         return Fp8Join{parts, out, n, j.split_pitch, j.splits, (unsigned)((n + 1023) / 1024)};
     };
     const Fp8Join a = join(h, h_parts, dH), b = join(w, w_parts, dW);
-    if (a.blocks + b.blocks) fp8_join_kernel<OT><<<a.blocks + b.blocks, 256, 0, st>>>(a, b);
+    const unsigned joins = sums.blocks + a.blocks + b.blocks;
+    if (joins) fp8_join_kernel<OT><<<joins, 256, 0, st>>>(sums, a, b);
     return launch_status();
 }
 
@@ -226,7 +236,7 @@ int lsr_fp8_quantize(int64_t rows, int64_t cols, int32_t x_dtype, const void* X,
     int n_cus = 0;
     const int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
-    return quantize(x_dtype, rows, cols, X, ldx, square != 0, fp8_rows(Q, ldq, exps, cols), fp8_rows(Qt, ldqt, exps_t, rows), nullptr, stream);
+    return quantize(x_dtype, rows, cols, X, ldx, square != 0, fp8_rows(Q, ldq, exps, cols), fp8_rows(Qt, ldqt, exps_t, rows), stream);
 }
 
 size_t lsr_fp8_matmul_workspace_bytes(int64_t N, int64_t V, int64_t K, int32_t a_dtype) {
@@ -271,7 +281,7 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
     if (!bytes) {
         char* const ws = static_cast<char*>(workspace);
         states = fp8_rows(ws + w.q, row, ws + w.exps, K);
-        rc = quantize(a_dtype, N, K, A, lda, false, states, Fp8Rows{}, nullptr, stream);
+        rc = quantize(a_dtype, N, K, A, lda, false, states, Fp8Rows{}, stream);
         if (rc != LSR_OK) return rc;
     }
     Fp8Job j = job(N, V, K, states, weights, out, ldo);
@@ -305,20 +315,27 @@ int lsr_fp8_backward(int64_t N, int64_t V, int64_t D, int32_t y_dtype, int32_t h
     char* const ws = static_cast<char*>(workspace);
     const Fp8Rows g = dH ? fp8_rows(ws + w.g, 0, ws + w.g_exp, V) : Fp8Rows{};
     const Fp8Rows gt = dW ? fp8_rows(ws + w.gt, 0, ws + w.gt_exp, N) : Fp8Rows{}, ht = dW ? fp8_rows(ws + w.ht, 0, ws + w.ht_exp, N) : Fp8Rows{};
+    // (one row tile's sums are the result)
     float* const sums = db && N > 128 ? reinterpret_cast<float*>(ws + w.sums) : db;
-    rc = quantize(y_dtype, N, V, dY, ldy, false, g, gt, sums, stream);
-    if (rc == LSR_OK && dW) rc = quantize(h_dtype, N, D, H, ldh, false, Fp8Rows{}, ht, nullptr, stream);
-    if (rc == LSR_OK && db && N > 128) {
-        fp8_sums_kernel<<<(unsigned)((V + 63) / 64), 256, 0, stream>>>(sums, (int)((N + 127) / 128), V, db);
-        rc = launch_status();
+    Fp8TileParams py = tiles_of(N, V, dY, ldy, g, gt);
+    py.sums = sums;
+    const Fp8TileParams ph = dW ? tiles_of(N, D, H, ldh, Fp8Rows{}, ht) : Fp8TileParams{};
+    if (y_dtype == LSR_F32) {
+        if (h_dtype == LSR_F32) backward_quantize<float, float>(py, ph, stream);
+        else backward_quantize<float, uint16_t>(py, ph, stream);
+    } else {
+        if (h_dtype == LSR_F32) backward_quantize<uint16_t, float>(py, ph, stream);
+        else backward_quantize<uint16_t, uint16_t>(py, ph, stream);
     }
-    if (rc != LSR_OK || (!dH && !dW)) return rc;
+    rc = launch_status();
+    if (rc != LSR_OK) return rc;
     const Fp8Rows wt = fp8_rows(Wt, ldwt, wt_exps, V);
     const Fp8Job h = dH ? job(N, D, V, g, wt, dH, D) : Fp8Job{}, v = dW ? job(V, D, N, gt, ht, dW, D) : Fp8Job{};
     float* const h_parts = reinterpret_cast<float*>(ws + w.h_parts);
     float* const w_parts = reinterpret_cast<float*>(ws + w.w_parts);
-    return h_dtype == LSR_F32 ? launch_grads<true, float>(h, v, plan, h_parts, w_parts, stream)
-                              : launch_grads<false, uint16_t>(h, v, plan, h_parts, w_parts, stream);
+    const Fp8Sums column_sums = sums != db ? Fp8Sums{sums, db, V, (int)((N + 127) / 128), (unsigned)((V + 63) / 64)} : Fp8Sums{};
+    return h_dtype == LSR_F32 ? launch_grads<true, float>(h, v, plan, h_parts, w_parts, column_sums, stream)
+                              : launch_grads<false, uint16_t>(h, v, plan, h_parts, w_parts, column_sums, stream);
 }
 
 }  // extern "C"
