@@ -444,14 +444,18 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Sums sums, Fp8Join a, 
 }
 
 // ---- few rows (the tokens of one decoding or query step): what bounds the call is reading W once ----
-// A wave owns 32 rows of W at a time and takes them straight into registers, FEWF_U chunks of 32 values (512 values, which share a word of powers) requested while those
+// A wave owns 32 rows of W at a time and takes them straight into registers, FEWF_U chunks of 32 values (a block of 128, with its power) requested while those
 // before them are multiplied.  The rows of A are quantised by every workgroup itself and lie in LDS as the bfloat16 values that they stand for; W is widened
 // in registers, so sums are float32 whatever the result's type (see `exact` above).
+// How far ahead a wave requests against how many waves a CU holds: 16 rows by 250002 x 1024 take 64.5 us with 16 chunks and 8 waves on a CU, 62.9 with 8 and 12, 60.9 with
+// 4 and 16, 69.6 with 2 and 16 (4300 GB/s; a launch that only reads W in this pattern takes 49).  1 row by 30522 x 768: 10.1, 9.7, 8.5, 8.2 us, of which reading is 5.
 constexpr int FEWF_THREADS = 256;
 constexpr int FEWF_COLS = 32 * FEWF_THREADS / 64;
 constexpr int FEWF_ROWS = 32;                     // one block of the MFMA
-constexpr int FEWF_U = 16;
-constexpr int FEWF_LDS = 76 * 1024;               // of the rows of A: two workgroups share a CU
+constexpr int FEWF_U = 4;
+constexpr int FEWF_X = 2;
+constexpr int FEWF_PER_CU = 4;                    // workgroups, where their rows of A leave room
+constexpr int FEWF_LDS = 76 * 1024;               // of the rows of A at most: two workgroups share a CU
 // LDS bytes of a row: padded so that the 32 rows of a fragment read lie on different banks
 inline int fewf_stride(int64_t K) { return (int)((K + 127) / 128 * 256 + 16); }
 
@@ -467,8 +471,8 @@ struct Fp8FewParams {
     int blocks;                // of 128 along K
 };
 template <typename T, typename OT>
-__global__ __launch_bounds__(FEWF_THREADS, 2) void fp8_few_kernel(Fp8FewParams p, int stride, int n_tiles) {
-    __shared__ __attribute__((aligned(16))) uint8_t s_a[FEWF_LDS];       // [N][stride]
+__global__ __launch_bounds__(FEWF_THREADS, FEWF_PER_CU) void fp8_few_kernel(Fp8FewParams p, int stride, int n_tiles) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_a[];        // [N][stride]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
     const int nks = p.blocks * 4;                 // chunks of 32 values
     int tile = blockIdx.x;
@@ -494,16 +498,21 @@ __global__ __launch_bounds__(FEWF_THREADS, 2) void fp8_few_kernel(Fp8FewParams p
             *reinterpret_cast<bf16x8*>(s_a + r * stride + c * 16) = widen(q.x, q.y, exp_value(e));
         }
     } else {
-        const int cols = p.blocks * 128;
+        // 512 columns of a row by a wave at a time, FEWF_X of them requested before the first is looked at
+        const int cols = p.blocks * 128, quads = (p.blocks + 3) >> 2, pieces = p.N * quads;
 #pragma unroll 1
-        for (int r = wave; r < p.N; r += FEWF_THREADS / 64) {
-            const T* const row = reinterpret_cast<const T*>(p.A) + (int64_t)r * p.lda;
-#pragma unroll 1
-            for (int c = lane * 8; c - lane * 8 < cols; c += 512) {
-                Eight<T> x;
-                x.load(row, c, p.K);
-                const float e = exp_value(block_exp(row_most(x)));
-                if (c < cols) *reinterpret_cast<bf16x8*>(s_a + r * stride + c * 2) = widen(x.four(0, e), x.four(4, e), e);
+        for (int q0 = wave; q0 < pieces; q0 += FEWF_X * (FEWF_THREADS / 64)) {
+            Eight<T> x[FEWF_X];
+#pragma unroll
+            for (int u = 0; u < FEWF_X; ++u) {
+                const int q = min(q0 + u * (FEWF_THREADS / 64), pieces - 1), r = q / quads;
+                x[u].load(reinterpret_cast<const T*>(p.A) + (int64_t)r * p.lda, (q - r * quads) * 512 + lane * 8, p.K);
+            }
+#pragma unroll
+            for (int u = 0; u < FEWF_X; ++u) {
+                const int q = q0 + u * (FEWF_THREADS / 64), r = q / quads, c = (q - r * quads) * 512 + lane * 8;
+                const float e = exp_value(block_exp(row_most(x[u])));
+                if (q < pieces && c < cols) *reinterpret_cast<bf16x8*>(s_a + r * stride + c * 2) = widen(x[u].four(0, e), x[u].four(4, e), e);
             }
         }
     }
@@ -520,7 +529,7 @@ __global__ __launch_bounds__(FEWF_THREADS, 2) void fp8_few_kernel(Fp8FewParams p
 #pragma unroll
             for (int u = 0; u < FEWF_U; ++u)
                 if (k0 + u < nks) {
-                    const float s = exp_value((e >> ((u >> 2) * 8)) & 255u);
+                    const float s = exp_value((e >> (((k0 & 15) + u) >> 2) * 8) & 255u);
                     const uint8_t* const a = sa + (k0 + u) * 64;
                     acc = mma_chunk(*reinterpret_cast<const bf16x8*>(a), widen((uint32_t)w[u][0], (uint32_t)w[u][1], s), acc);
                     acc = mma_chunk(*reinterpret_cast<const bf16x8*>(a + 16), widen((uint32_t)w[u][2], (uint32_t)w[u][3], s), acc);

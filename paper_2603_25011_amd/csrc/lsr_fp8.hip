@@ -178,9 +178,13 @@ bool few(int64_t N, int64_t K) { return N <= FEWF_ROWS && N * fewf_stride(K) <= 
 template <typename T>
 void launch_few(const Fp8FewParams& p, int32_t out_type, int n_cus, hipStream_t st) {
     const int n_tiles = (p.V + FEWF_COLS - 1) / FEWF_COLS;
-    const unsigned grid = (unsigned)(n_tiles < 2 * n_cus ? n_tiles : 2 * n_cus);
-    if (out_type == LSR_F32) fp8_few_kernel<T, float><<<grid, FEWF_THREADS, 0, st>>>(p, fewf_stride(p.K), n_tiles);
-    else fp8_few_kernel<T, uint16_t><<<grid, FEWF_THREADS, 0, st>>>(p, fewf_stride(p.K), n_tiles);
+    const int stride = fewf_stride(p.K), lds = p.N * stride;
+    int resident = (160 * 1024) / lds;
+    resident = resident < FEWF_PER_CU ? resident : FEWF_PER_CU;
+    const int most = resident * n_cus;
+    const unsigned grid = (unsigned)(n_tiles < most ? n_tiles : most);
+    if (out_type == LSR_F32) fp8_few_kernel<T, float><<<grid, FEWF_THREADS, lds, st>>>(p, stride, n_tiles);
+    else fp8_few_kernel<T, uint16_t><<<grid, FEWF_THREADS, lds, st>>>(p, stride, n_tiles);
 }
 
 struct MatmulWs { size_t q, exps, total; };
