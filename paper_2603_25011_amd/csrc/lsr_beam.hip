@@ -53,6 +53,28 @@ BeamWs beam_ws(int64_t rows, const BeamPlan& p, int64_t K) {
     return w;
 }
 
+// a launch stays below 2^32 threads: arrays that would pass it begin the next one
+constexpr int64_t REORDER_BLOCKS = (int64_t(1) << 24) - 1;
+// One array in the widest accesses that its addresses, strides and pieces allow; returns its blocks.
+int64_t reorder_state(lsr_beam_state a, int64_t rows, ReorderState& s) {
+    if (a.pieces == 1) a.src_piece = a.dst_piece = a.piece_bytes;
+    if (a.src_piece == a.piece_bytes && a.dst_piece == a.piece_bytes) { a.piece_bytes *= a.pieces; a.pieces = 1; }
+    const uint64_t all = reinterpret_cast<uintptr_t>(a.src) | reinterpret_cast<uintptr_t>(a.dst) | (uint64_t)a.src_batch | (uint64_t)a.src_beam |
+                         (uint64_t)a.dst_batch | (uint64_t)a.dst_beam | (uint64_t)a.piece_bytes |
+                         (a.pieces > 1 ? (uint64_t)a.src_piece | (uint64_t)a.dst_piece : 0);
+    int shift = 4;
+    while (shift > 0 && (all & ((1u << shift) - 1))) --shift;
+    s = {};
+    s.src = static_cast<const char*>(a.src); s.dst = static_cast<char*>(a.dst);
+    s.src_batch = a.src_batch; s.src_beam = a.src_beam; s.src_piece = a.src_piece;
+    s.dst_batch = a.dst_batch; s.dst_beam = a.dst_beam; s.dst_piece = a.dst_piece;
+    s.piece_accesses = (uint32_t)(a.piece_bytes >> shift);
+    s.row_accesses = (uint32_t)((a.pieces * a.piece_bytes) >> shift);
+    s.shift = shift;
+    const int64_t per = REORDER_THREADS * REORDER_PER;
+    return (rows * s.row_accesses + per - 1) / per;
+}
+
 }  // namespace
 
 extern "C" {
@@ -108,12 +130,12 @@ int lsr_beam_reorder(int64_t B, int64_t beams, int64_t K, const int32_t* parents
             rows * (s.pieces * s.piece_bytes) >= int64_t(1) << 40 || s.src_batch < 0 || s.src_beam < 0 || s.src_piece < 0 || s.dst_batch < 0 ||
             s.dst_beam < 0 || s.dst_piece < 0)
             return LSR_ERR_SHAPE;
+        ReorderState own;
+        if (reorder_state(s, rows, own) > REORDER_BLOCKS) return LSR_ERR_SHAPE;       // (single bytes of an array of many gigabytes)
     }
     int n_cus = 0;
     const int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
-    // a launch stays below 2^32 threads: arrays that would pass it begin the next one
-    const int64_t most_blocks = (int64_t(1) << 24) - 1;
     ReorderParams p = {};
     p.parents = parents; p.beams = (int)beams; p.K = (int)K; p.rows = rows;
     int64_t blocks = 0;
@@ -123,24 +145,9 @@ int lsr_beam_reorder(int64_t B, int64_t beams, int64_t K, const int32_t* parents
         blocks = 0;
     };
     for (int64_t i = 0; i < n; ++i) {
-        lsr_beam_state a = states[i];
-        if (a.pieces == 1) a.src_piece = a.dst_piece = a.piece_bytes;
-        if (a.src_piece == a.piece_bytes && a.dst_piece == a.piece_bytes) { a.piece_bytes *= a.pieces; a.pieces = 1; }
-        const uint64_t all = reinterpret_cast<uintptr_t>(a.src) | reinterpret_cast<uintptr_t>(a.dst) | (uint64_t)a.src_batch | (uint64_t)a.src_beam |
-                             (uint64_t)a.dst_batch | (uint64_t)a.dst_beam | (uint64_t)a.piece_bytes |
-                             (a.pieces > 1 ? (uint64_t)a.src_piece | (uint64_t)a.dst_piece : 0);
-        int shift = 4;
-        while (shift > 0 && (all & ((1u << shift) - 1))) --shift;
-        ReorderState s = {};
-        s.src = static_cast<const char*>(a.src); s.dst = static_cast<char*>(a.dst);
-        s.src_batch = a.src_batch; s.src_beam = a.src_beam; s.src_piece = a.src_piece;
-        s.dst_batch = a.dst_batch; s.dst_beam = a.dst_beam; s.dst_piece = a.dst_piece;
-        s.piece_accesses = (uint32_t)(a.piece_bytes >> shift);
-        s.row_accesses = (uint32_t)((a.pieces * a.piece_bytes) >> shift);
-        s.shift = shift;
-        const int64_t per = REORDER_THREADS * REORDER_PER, want = (rows * s.row_accesses + per - 1) / per;
-        if (p.n == REORDER_STATES || (p.n && blocks + want > most_blocks)) launch();
-        if (want > most_blocks) return LSR_ERR_SHAPE;       // (single bytes of an array of terabytes)
+        ReorderState s;
+        const int64_t want = reorder_state(states[i], rows, s);
+        if (p.n == REORDER_STATES || (p.n && blocks + want > REORDER_BLOCKS)) launch();
         s.first_block = (uint32_t)blocks;
         p.state[p.n++] = s;
         blocks += want;

@@ -110,6 +110,9 @@ def test_beam_reorder_refusals():
     assert r(parents=None) == NULL and r(states=but(src=None)) == NULL and r(states=but(dst=None)) == NULL and r(parents=P + 2) == ALIGN
     for bad in ({"pieces": 0}, {"piece_bytes": 0}, {"pieces": 1 << 20, "piece_bytes": 1 << 20}, {"src_batch": -1}, {"dst_piece": -1}, {"src_beam": -16}):
         assert r(states=[good] + but(**bad)) == SHAPE, bad
+    # more single bytes than a launch has threads for, behind an array that is in order: nothing is enqueued before the refusal
+    odd = dict(src=P + 1, src_batch=1 << 31, src_beam=1 << 30, dst_batch=1 << 31, dst_beam=1 << 30, piece_bytes=(1 << 30) + 1)
+    assert r(B=16, states=[good] * 40 + but(**odd)) == SHAPE
 
 
 def test_dropout_refusals():
