@@ -95,7 +95,7 @@ def _once(x: torch.Tensor) -> bool:
 def beam_reorder(states, parents: torch.Tensor, out=None):
     """What the beams keep, in the order of their children: new[b, k] = old[b, parents[b, k]] for every tensor [B, beams, ...] of `states` (one, or a list
     of any dtypes, all on one GPU), in one launch for up to 32 of them.  parents [B, K] int32 as beam_select gives them; a parent outside the beams gives zeros.
-    `out`: tensors [B, K, ...] to write, whose addresses lie apart from each other's and the states'; without it new ones.  Returns a tensor or a list, as
+    `out`: tensors [B, K, ...] to write, whose addresses lie apart from each other's, the states' and the parents'; without it new ones.  Returns a tensor or a list, as
     `states` is one.  Strides are free; a tensor whose [b, m] is not pieces of equal length and distance (a cache of which only part of the length is in use
     is) is copied first, and refused as `out`."""
     one = isinstance(states, torch.Tensor)
@@ -112,6 +112,8 @@ def beam_reorder(states, parents: torch.Tensor, out=None):
     B, K = parents.shape
     beams = states[0].shape[1] if states[0].dim() > 1 else 0
     new, table, spans, hold = [], [], [], []
+    if out is not None:
+        spans.append((*_span(parents), False))
     for i, x in enumerate(states):
         shape = x.shape
         if len(shape) < 2 or shape[0] != B or shape[1] != beams:
@@ -122,6 +124,11 @@ def beam_reorder(states, parents: torch.Tensor, out=None):
             y = out[i]
             if y.shape != (B, K, *shape[2:]) or y.dtype != x.dtype:
                 raise ValueError("beam_reorder: out must be [B, K, ...] of the states' dtypes")
+        if x.is_conj() or x.is_neg():
+            x = x.resolve_conj().resolve_neg()
+            hold.append(x)
+        if y.is_conj() or y.is_neg():
+            raise ValueError("beam_reorder: out must hold its values as they are, not conjugated or negated")
         new.append(y)
         size = y.numel()
         if not size:
@@ -163,7 +170,7 @@ def beam_reorder(states, parents: torch.Tensor, out=None):
     end, written = 0, False
     for first, last, writes in spans:
         if first < end and (writes or written):
-            raise ValueError("beam_reorder: the addresses of out overlap the states' or its own")
+            raise ValueError("beam_reorder: the addresses of out overlap the states', the parents' or its own")
         if last > end:
             end, written = last, writes
     if table:

@@ -241,5 +241,18 @@ def test_reorder_refusals():
     assert beam.beam_reorder(x[:0], p[:0]).shape == (0, 3, 10)
 
 
+def test_reorder_out_that_holds_the_parents_and_views_of_other_signs():
+    out = torch.zeros(2, 3, 2, dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError, match="overlap"):
+        beam.beam_reorder(torch.ones_like(out), out.view(-1)[:6].view(2, 3), out)
+    x, p = torch.randn(2, 3, 5, dtype=torch.complex64, device=DEV), torch.tensor([[2, 0, 0], [1, 1, 2]], dtype=torch.int32, device=DEV)
+    for y in (x.conj(), x.conj().imag):
+        assert y.is_conj() or y.is_neg()
+        want = torch.stack([y[b].resolve_conj().resolve_neg()[p[b].long()] for b in range(2)])
+        assert torch.equal(beam.beam_reorder(y, p), want)
+    with pytest.raises(ValueError, match="conjugated"):
+        beam.beam_reorder(x, p, torch.zeros_like(x).conj())
+
+
 def test_entry_points_are_the_package_own():
     assert lsr.lsr_beam_select is binding.lsr_beam_select and lsr.lsr_beam_reorder is binding.lsr_beam_reorder
