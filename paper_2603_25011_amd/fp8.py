@@ -103,11 +103,12 @@ class _Fp8Logits(torch.autograd.Function):
         exps = torch.empty(lsr.lsr_fp8_exp_bytes(V, D), dtype=torch.uint8, device=H.device)
         Wt = torch.empty(lsr.lsr_fp8_slab_bytes(D, V), dtype=torch.uint8, device=H.device) if need_t else None
         exps_t = torch.empty(lsr.lsr_fp8_exp_bytes(D, V), dtype=torch.uint8, device=H.device) if need_t else None
-        out = torch.empty((N, V), dtype=dtype, device=H.device)
         if N:
             with _on(H.device):
                 lsr.lsr_fp8_quantize(V, D, kind, W, _ld(W), True, W8, W8.shape[1], exps, Wt, 0, exps_t)
                 out = _matmul(H, kind, D, W8, exps, bias, dtype)
+        else:
+            out = torch.empty((N, V), dtype=dtype, device=H.device)
         ctx.shape = (N, V, D, _KIND[dtype], kind)
         ctx.has_bias = bias is not None
         ctx.save_for_backward(H, W, Wt, exps_t)
@@ -143,7 +144,9 @@ def fp8_logits(H: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = Non
     """[..., V] logits H W^T + bias of hidden states H [..., D] and a matrix W [V, D] (both float32 or both bfloat16), multiplied in 8-bit
     floating point: H in blocks of 1 x 128 along its rows, W in blocks of 128 x 128.  `dtype` is that of the logits (float32 or bfloat16).
     Differentiable (once) in H, W and bias, the rounding to 8 bits passed over:  dH = q(dY) q(W),  dW = q(dY)^T q(H) with dY and H in blocks of
-    128 tokens,  db = sum of dY.  Gradients come in the parameters' own dtypes."""
+    128 tokens,  db = sum of dY.  Gradients come in the parameters' own dtypes.
+    Where a step is captured into a graph, no result of an eager call on the same parameters may still hold its own autograd graph (autograd would
+    run part of the captured backward on the eager call's stream)."""
     _on_gpu("fp8_logits", H, W, bias)
     if H.dtype != W.dtype or H.dtype not in _KIND:
         raise TypeError("fp8_logits: H and W must both be bfloat16 or both float32")
@@ -151,6 +154,8 @@ def fp8_logits(H: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = Non
         raise TypeError(f"fp8_logits: logits are float32 or bfloat16, not {dtype}")
     if W.dim() != 2 or H.dim() < 1 or H.shape[-1] != W.shape[1] or not W.numel():
         raise ValueError("fp8_logits: H [..., D] and W [V, D] do not fit together")
+    if not torch.is_grad_enabled():
+        H, W = H.detach(), W.detach()               # (no transposed matrix for a backward that will not come)
     lead = H.shape[:-1]
     out = _Fp8Logits.apply(_rows(_as(H, (-1, W.shape[1]))), _rows(W), _bias("fp8_logits", bias, W.shape[0]), dtype)
     return _as(out, (*lead, W.shape[0]))
