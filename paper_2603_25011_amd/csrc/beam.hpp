@@ -352,20 +352,20 @@ __device__ __forceinline__ double score_bits(uint64_t o) {
 
 enum { BEAM_NONE = 0, BEAM_GOES_ON = 1, BEAM_FINISHED = 2, BEAM_NAN = 3 };
 
-// One workgroup per sequence.  Keys are dealt out place by place (all lists' first, then all their second), so that the threads' maxima are the best of the lists; K of
-// them give a threshold, what reaches it goes to a list in LDS, and a candidate's place is the number of better ones.  Latency bounds it, so the keys are on their way while
-// the normalisers are formed, and each thread keeps the scores of its first BEAM_OWN.
+// One workgroup per sequence.  Keys are dealt out place by place (all lists' first, then all their second) and evenly to the waves, so that the threads' maxima are the best
+// of the lists; a threshold comes of them bit by bit from each wave's ballots, what reaches it goes to a list in LDS, and a candidate's place is the number of better ones
+// (counting for each of the 256 maxima the larger ones instead took 1.2 to 2 us longer).  Latency bounds it, so the keys are on their way while the normalisers are formed, and
+// each thread keeps the scores of its first BEAM_OWN: 5.0 us for 4 beams with 14 segments and K = 8, 7.8 for 64 sequences of 8 beams with 2 and K = 16.
 constexpr int BEAM_OWN = 4;
 __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
     // a beam's candidates have score s_base + (x - s_top) / T: the difference first, which is exact
     __shared__ double s_base[BEAM_MAX_BEAMS], s_top[BEAM_MAX_BEAMS];
     __shared__ int s_kind[BEAM_MAX_BEAMS];
-    __shared__ __attribute__((aligned(16))) uint32_t s_most[BEAM_THREADS];
-    __shared__ uint32_t s_least;
+    __shared__ uint32_t s_most[BEAM_WAVES];
     __shared__ int s_count;
     __shared__ __attribute__((aligned(16))) uint64_t s_score[BEAM_JOIN];
     __shared__ uint16_t s_at[BEAM_JOIN];
-    __shared__ int s_token[BEAM_JOIN];
+    __shared__ uint64_t s_key[BEAM_JOIN];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t b = blockIdx.x;
     const double inv_t = 1.0 / p.temperature, cd = 1.4426950408889634 * inv_t;
@@ -379,10 +379,11 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
         m = (int)(((float)l + 0.5f) * per_splits);
         return j;
     };
+    const int deal = lane * BEAM_WAVES + ((wave + lane + (lane >> 2) + (lane >> 4)) & (BEAM_WAVES - 1));      // (every wave gets as many of each place and list)
     uint64_t own[BEAM_OWN];
 #pragma unroll
     for (int q = 0; q < BEAM_OWN; ++q) {
-        const int i = q * BEAM_THREADS + tid;
+        const int i = q * BEAM_THREADS + deal;
         own[q] = 0;
         if (i < total) {
             int l, m;
@@ -436,59 +437,51 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
     uint64_t mine[BEAM_OWN];
 #pragma unroll
     for (int q = 0; q < BEAM_OWN; ++q) {
-        const int i = q * BEAM_THREADS + tid;
+        const int i = q * BEAM_THREADS + deal;
         mine[q] = i < total ? candidate(i, own[q]) : 0;
         most = max(most, (uint32_t)(mine[q] >> 32));
     }
-    for (int i = BEAM_OWN * BEAM_THREADS + tid; i < total; i += BEAM_THREADS) most = max(most, (uint32_t)(candidate(i, key_at(i)) >> 32));
-    // the K-th largest of the threads' maxima (of the first 32 bits; at least K threads have candidates): the least that fewer than K are larger than
-    s_most[tid] = most;
-    if (tid == 0) s_least = ~0u;
-    __syncthreads();
+    for (int i = BEAM_OWN * BEAM_THREADS + deal; i < total; i += BEAM_THREADS) most = max(most, (uint32_t)(candidate(i, key_at(i)) >> 32));
+    // a threshold that K candidates reach: of each wave's maxima (their first 20 bits) as many as its share of K, the least of the waves'
     {
-        int larger = 0;
-#pragma unroll 8
-        for (int r = 0; r < BEAM_THREADS; r += 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(&s_most[r]);
-            larger += (x.x > most ? 1 : 0) + (x.y > most ? 1 : 0) + (x.z > most ? 1 : 0) + (x.w > most ? 1 : 0);
-        }
-        uint32_t least = larger < p.K ? most : ~0u;
+        const int want = (p.K + BEAM_WAVES - 1) / BEAM_WAVES;
+        const uint32_t o = most >> 12;
+        uint32_t t = 0;                          // (0 where fewer lanes have candidates: then all enter)
+#pragma unroll 4
+        for (uint32_t bit = 1u << 19; bit; bit >>= 1) t = __popcll(__ballot(o >= (t | bit))) >= want ? t | bit : t;
+        if (lane == 0) s_most[wave] = t;
+        __syncthreads();
+        t = s_most[0];
 #pragma unroll
-        for (int o = 32; o; o >>= 1) least = min(least, (uint32_t)__shfl_xor((int)least, o));
-        if (lane == 0) atomicMin(&s_least, least);
+        for (int k = 1; k < BEAM_WAVES; ++k) t = min(t, s_most[k]);
+        most = t << 12;
     }
-    __syncthreads();
-    most = s_least;
     auto enter = [&](int i, uint64_t o, uint64_t k) {
         if (o && (uint32_t)(o >> 32) >= most) {
-            int l, m;
-            place(i, l, m);
             const int at = atomicAdd(&s_count, 1);
             s_score[at] = o;
             s_at[at] = (uint16_t)i;
-            s_token[at] = s_kind[m] != BEAM_FINISHED && k ? (int)~(uint32_t)k : p.end_id;
+            s_key[at] = k;
         }
     };
 #pragma unroll
-    for (int q = 0; q < BEAM_OWN; ++q) enter(q * BEAM_THREADS + tid, mine[q], own[q]);
-    for (int i = BEAM_OWN * BEAM_THREADS + tid; i < total; i += BEAM_THREADS) {
+    for (int q = 0; q < BEAM_OWN; ++q) enter(q * BEAM_THREADS + deal, mine[q], own[q]);
+    for (int i = BEAM_OWN * BEAM_THREADS + deal; i < total; i += BEAM_THREADS) {
         const uint64_t k = key_at(i);
         enter(i, candidate(i, k), k);
     }
     __syncthreads();
     const int n = s_count;
-    // whether candidate i comes before j, of equal score
-    auto first_of = [&](int i, int j) -> bool {
-        int li, lj, mi, mj;
-        place(i, li, mi);
-        place(j, lj, mj);
-        if (mi != mj) return mi < mj;
-        const uint64_t ki = key_at(i), kj = key_at(j);
-        return ki != kj ? ki > kj : i < j;
+    // whether entry r comes before q, of equal score
+    auto first_of = [&](int r, int q) -> bool {
+        int l, mr, mq;
+        place(s_at[r], l, mr);
+        place(s_at[q], l, mq);
+        if (mr != mq) return mr < mq;
+        return s_key[r] != s_key[q] ? s_key[r] > s_key[q] : s_at[r] < s_at[q];
     };
     for (int q = tid; q < n; q += BEAM_THREADS) {
         const uint64_t o = s_score[q];
-        const int i = s_at[q];
         int rank = 0, equal = 0, r = 0;
         for (; r + 4 <= n; r += 4) {
             const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(&s_score[r]), y = *reinterpret_cast<const ulonglong2*>(&s_score[r + 2]);
@@ -501,15 +494,16 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
         }
         if (equal > 1 && rank < p.K) {           // (itself is one)
             for (r = 0; r < n; ++r)
-                if (s_score[r] == o && r != q) rank += first_of(s_at[r], i) ? 1 : 0;
+                if (s_score[r] == o && r != q) rank += first_of(r, q) ? 1 : 0;
         }
         if (rank < p.K) {
             int l, m;
-            place(i, l, m);
+            place(s_at[q], l, m);
+            const uint64_t k = s_key[q];
             const int64_t to = b * p.K + rank;
             p.out_scores[to] = (float)score_bits(o);
             p.out_beams[to] = m;
-            p.out_tokens[to] = s_token[q];
+            p.out_tokens[to] = s_kind[m] != BEAM_FINISHED && k ? (int)~(uint32_t)k : p.end_id;
         }
     }
     for (int r = n + tid; r < p.K; r += BEAM_THREADS) {
