@@ -64,7 +64,7 @@ int lsr_fp8_quantize(int64_t rows, int64_t cols, int32_t x_dtype, const void* X,
  *   workspace lsr_fp8_matmul_workspace_bytes (0 for LSR_E4M3: then it may be NULL; 0 also for an invalid shape)
  * For LSR_F32 results products are exact and sums are float32.  For LSR_BF16 results of more than a few rows the matrix cores add products in small groups, in
  * which what lies more than 13 bits below the largest is cut off: 2e-5 of the norm of the sums on normal values, under a rounding of 1.7e-3.
- * A value of A or W below 2^-126 may count as zero.  Exponents and bias are 4-byte aligned.
+ * A value of A or W below 2^-126 may count as zero; one above 1.9375 2^127 rounds to 2^128, which may count as infinite.  Exponents and bias are 4-byte aligned.
  * Limits: 1 <= N, V <= 2^22, N V < 2^36, 1 <= K <= 65536, ldw and the lda of bytes at most 2^23.
  */
 size_t lsr_fp8_matmul_workspace_bytes(int64_t N, int64_t V, int64_t K, int32_t a_dtype);
@@ -74,6 +74,20 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
                    const uint8_t* W, int64_t ldw, const uint8_t* w_exps, const float* bias,
                    void* out, int64_t ldo,
                    void* workspace, size_t workspace_bytes, lsr_stream_t stream);
+
+/*
+ * The same logits of a matrix that is a parameter, as a training step forms them: W [V, ldw] and H [N, ldh] of h_dtype (LSR_F32 or LSR_BF16), any alignment of their
+ * elements, W held in blocks of 128 x 128 and H in blocks of 1 x 128 within the call.
+ *   Wt [D, ldwt], wt_exps: what lsr_fp8_backward takes of the matrix, as lsr_fp8_quantize writes Qt (square; ldwt = 0 by slab), or NULL for no dH
+ *   out, bias: as above; the results are the bits of lsr_fp8_quantize and lsr_fp8_matmul.
+ * Limits: as above, with D for K.
+ */
+size_t lsr_fp8_forward_workspace_bytes(int64_t N, int64_t V, int64_t D);
+
+int lsr_fp8_forward(int64_t N, int64_t V, int64_t D, int32_t h_dtype, int32_t out_dtype,
+                    const void* H, int64_t ldh, const void* W, int64_t ldw, const float* bias,
+                    void* out, int64_t ldo, uint8_t* Wt, int64_t ldwt, uint8_t* wt_exps,
+                    void* workspace, size_t workspace_bytes, lsr_stream_t stream);
 
 /*
  * Gradients of sum dY . (q(H) q(W)^T + bias), the rounding of the operands passed over (its derivative taken as one):

@@ -7,5 +7,5 @@ from .binding import (  # noqa: F401
     LSR_I8, lsr_distill_backward, lsr_distill_forward, lsr_distill_workspace_bytes, lsr_int8_matmul, lsr_int8_matmul_workspace_bytes,
     lsr_int8_row_bytes, lsr_quantize_rows, lsr_top_logits, lsr_top_logits_workspace_bytes,
     LSR_E4M3, lsr_beam_reorder, lsr_beam_select, lsr_beam_select_workspace_bytes, lsr_dropout, lsr_fp8_backward,
-    lsr_fp8_backward_workspace_bytes, lsr_fp8_exp_bytes, lsr_fp8_matmul, lsr_fp8_matmul_workspace_bytes, lsr_fp8_quantize, lsr_fp8_row_bytes, lsr_fp8_slab_bytes,
+    lsr_fp8_backward_workspace_bytes, lsr_fp8_exp_bytes, lsr_fp8_forward, lsr_fp8_forward_workspace_bytes, lsr_fp8_matmul, lsr_fp8_matmul_workspace_bytes, lsr_fp8_quantize, lsr_fp8_row_bytes, lsr_fp8_slab_bytes,
 )

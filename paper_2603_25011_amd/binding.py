@@ -120,6 +120,10 @@ def load_library():
     lib.lsr_fp8_matmul_workspace_bytes.argtypes = [i64, i64, i64, i32]
     lib.lsr_fp8_matmul.restype = ctypes.c_int
     lib.lsr_fp8_matmul.argtypes = [i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+    lib.lsr_fp8_forward_workspace_bytes.restype = sz
+    lib.lsr_fp8_forward_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.lsr_fp8_forward.restype = ctypes.c_int
+    lib.lsr_fp8_forward.argtypes = [i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp]
     lib.lsr_fp8_backward_workspace_bytes.restype = sz
     lib.lsr_fp8_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32]
     lib.lsr_fp8_backward.restype = ctypes.c_int
@@ -373,6 +377,16 @@ def lsr_fp8_matmul(N, V, K, a_dtype, out_dtype, A, lda, a_exps, W, ldw, w_exps, 
     wp, wb = _ws(workspace)
     _check(load_library().lsr_fp8_matmul(N, V, K, a_dtype, out_dtype, _ptr(A), lda, _ptr(a_exps), _ptr(W), ldw, _ptr(w_exps), _ptr(bias), _ptr(out), ldo,
                                          wp, wb, _stream(stream)))
+
+
+def lsr_fp8_forward_workspace_bytes(N, V, D) -> int:
+    return load_library().lsr_fp8_forward_workspace_bytes(N, V, D)
+
+
+def lsr_fp8_forward(N, V, D, h_dtype, out_dtype, H, ldh, W, ldw, bias, out, ldo, Wt, ldwt, wt_exps, workspace, stream=None) -> None:
+    wp, wb = _ws(workspace)
+    _check(load_library().lsr_fp8_forward(N, V, D, h_dtype, out_dtype, _ptr(H), ldh, _ptr(W), ldw, _ptr(bias), _ptr(out), ldo, _ptr(Wt), ldwt, _ptr(wt_exps), wp, wb,
+                                          _stream(stream)))
 
 
 def lsr_fp8_backward_workspace_bytes(N, V, D, need_dh=True, need_dw=True, need_db=True) -> int:

@@ -139,9 +139,9 @@ struct Fp8Rows {
 // Bound by memory traffic.
 constexpr int FQ_THREADS = 256;
 template <typename T>
-__global__ __launch_bounds__(FQ_THREADS) void fp8_rows_kernel(const T* __restrict__ X, int64_t ldx, int64_t rows, int cols, Fp8Rows Q) {
+__device__ __forceinline__ void fp8_quantize_rows(const T* __restrict__ X, int64_t ldx, int64_t rows, int cols, const Fp8Rows& Q, unsigned block) {
     const int lane = threadIdx.x & 63;
-    const int64_t r = (int64_t)blockIdx.x * (FQ_THREADS / 64) + (threadIdx.x >> 6);
+    const int64_t r = (int64_t)block * (FQ_THREADS / 64) + (threadIdx.x >> 6);
     if (r >= rows) return;
     const T* const row = X + r * ldx;
     const int padded = (cols + 127) / 128 * 128;
@@ -156,6 +156,10 @@ __global__ __launch_bounds__(FQ_THREADS) void fp8_rows_kernel(const T* __restric
         four |= (uint32_t)__shfl_xor((int)four, 32);
         if (lane == 0) reinterpret_cast<uint32_t*>(Q.exps)[(int64_t)q * rows + r] = four;
     }
+}
+template <typename T>
+__global__ __launch_bounds__(FQ_THREADS) void fp8_rows_kernel(const T* __restrict__ X, int64_t ldx, int64_t rows, int cols, Fp8Rows Q) {
+    fp8_quantize_rows(X, ldx, rows, cols, Q, blockIdx.x);
 }
 
 // Both forms from one read: a workgroup takes 128 rows x 128 columns, a thread 8 x 8 of them, which it keeps in registers as they are stored.  The transposed form goes
@@ -302,6 +306,14 @@ template <typename T, bool SQUARE>
 __global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_tile_quantize_kernel(Fp8TileParams p) {
     __shared__ Fp8TileShared sh;
     fp8_quantize_tile<T, SQUARE>(p, blockIdx.x, sh);
+}
+// What a training step's forward takes of the matrix (blocks of 128 x 128, in both forms) and of the hidden states (blocks along their rows), in one launch.
+template <typename T>
+__global__ __launch_bounds__(FQ_THREADS, sizeof(T) == 4 ? 3 : 4) void fp8_forward_quantize_kernel(Fp8TileParams w, unsigned n_w, const T* __restrict__ H, int64_t ldh, int64_t rows, int cols,
+                                                                                                  Fp8Rows Q) {
+    __shared__ Fp8TileShared sh;
+    if (blockIdx.x < n_w) fp8_quantize_tile<T, true>(w, blockIdx.x, sh);
+    else fp8_quantize_rows(H, ldh, rows, cols, Q, blockIdx.x - n_w);
 }
 // What a backward takes of the gradients of the logits (TY) and of the hidden states (TH), in one launch: a launch of its own costs the host, and the chip where there are few tokens, more
 // than the hidden states' tiles.

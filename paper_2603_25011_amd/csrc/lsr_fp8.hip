@@ -56,6 +56,11 @@ int quantize_as(int64_t rows, int64_t cols, const void* X, int64_t ldx, bool squ
 int quantize(int32_t type, int64_t rows, int64_t cols, const void* X, int64_t ldx, bool square, const Fp8Rows& q, const Fp8Rows& qt, hipStream_t st) {
     return type == LSR_F32 ? quantize_as<float>(rows, cols, X, ldx, square, q, qt, st) : quantize_as<uint16_t>(rows, cols, X, ldx, square, q, qt, st);
 }
+template <typename T>
+void forward_quantize(const Fp8TileParams& w, const void* H, int64_t ldh, int64_t rows, int64_t cols, const Fp8Rows& q, hipStream_t st) {
+    const unsigned n = blocks_of(w);
+    fp8_forward_quantize_kernel<T><<<n + (unsigned)((rows + 3) / 4), FQ_THREADS, 0, st>>>(w, n, static_cast<const T*>(H), ldh, rows, (int)cols, q);
+}
 template <typename TY, typename TH>
 void backward_quantize(const Fp8TileParams& y, const Fp8TileParams& h, hipStream_t st) {
     const unsigned n = blocks_of(y);
@@ -187,6 +192,34 @@ void launch_few(const Fp8FewParams& p, int32_t out_type, int n_cus, hipStream_t 
     else fp8_few_kernel<T, uint16_t><<<grid, FEWF_THREADS, lds, st>>>(p, stride, n_tiles);
 }
 
+int few_logits(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out_dtype, const void* A, int64_t lda, const uint8_t* a_exps, const Fp8Rows& W, const float* bias,
+               void* out, int64_t ldo, int n_cus, hipStream_t st) {
+    Fp8FewParams p = {};
+    p.A = static_cast<const uint8_t*>(A); p.lda = lda; p.a_exp = reinterpret_cast<const uint32_t*>(a_exps);
+    p.W = W.q; p.ldw = W.ld; p.w_exp = reinterpret_cast<const uint32_t*>(W.exps);
+    p.bias = bias; p.out = out; p.ldo = ldo;
+    p.N = (int)N; p.V = (int)V; p.K = (int)K; p.blocks = (int)(up(K, 128) / 128);
+    if (a_dtype == LSR_E4M3) launch_few<uint8_t>(p, out_dtype, n_cus, st);
+    else if (a_dtype == LSR_F32) launch_few<float>(p, out_dtype, n_cus, st);
+    else launch_few<uint16_t>(p, out_dtype, n_cus, st);
+    return launch_status();
+}
+int logits(int64_t N, int64_t V, int64_t K, int32_t out_dtype, const Fp8Rows& A, const Fp8Rows& W, const float* bias, void* out, int64_t ldo, hipStream_t st) {
+    Fp8Job j = job(N, V, K, A, W, out, ldo);
+    return out_dtype == LSR_F32 ? launch_logits<true, float>(j, bias, st) : launch_logits<false, uint16_t>(j, bias, st);
+}
+
+struct ForwardWs { size_t w, w_exp, q, exps, total; };
+ForwardWs forward_ws(int64_t N, int64_t V, int64_t D) {
+    ForwardWs w;
+    w.w = 0;
+    w.w_exp = align_up((size_t)V * up(D, 128));
+    w.q = w.w_exp + align_up((size_t)exp_bytes(V, D));
+    w.exps = w.q + (few(N, D) ? 0 : align_up((size_t)N * up(D, 128)));
+    w.total = w.exps + (few(N, D) ? 0 : (size_t)exp_bytes(N, D));
+    return w;
+}
+
 struct MatmulWs { size_t q, exps, total; };
 MatmulWs matmul_ws(int64_t N, int64_t K) {
     MatmulWs w;
@@ -270,17 +303,7 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
     int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
     const Fp8Rows weights = fp8_rows(W, ldw, w_exps, K);
-    if (few(N, K)) {
-        Fp8FewParams p = {};
-        p.A = static_cast<const uint8_t*>(A); p.lda = lda; p.a_exp = reinterpret_cast<const uint32_t*>(a_exps);
-        p.W = W; p.ldw = ldw; p.w_exp = reinterpret_cast<const uint32_t*>(w_exps);
-        p.bias = bias; p.out = out; p.ldo = ldo;
-        p.N = (int)N; p.V = (int)V; p.K = (int)K; p.blocks = (int)(row / 128);
-        if (bytes) launch_few<uint8_t>(p, out_dtype, n_cus, stream);
-        else if (a_dtype == LSR_F32) launch_few<float>(p, out_dtype, n_cus, stream);
-        else launch_few<uint16_t>(p, out_dtype, n_cus, stream);
-        return launch_status();
-    }
+    if (few(N, K)) return few_logits(N, V, K, a_dtype, out_dtype, A, lda, a_exps, weights, bias, out, ldo, n_cus, stream);
     Fp8Rows states = fp8_rows(A, lda, a_exps, K);
     if (!bytes) {
         char* const ws = static_cast<char*>(workspace);
@@ -288,8 +311,42 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
         rc = quantize(a_dtype, N, K, A, lda, false, states, Fp8Rows{}, stream);
         if (rc != LSR_OK) return rc;
     }
-    Fp8Job j = job(N, V, K, states, weights, out, ldo);
-    return out_dtype == LSR_F32 ? launch_logits<true, float>(j, bias, stream) : launch_logits<false, uint16_t>(j, bias, stream);
+    return logits(N, V, K, out_dtype, states, weights, bias, out, ldo, stream);
+}
+
+size_t lsr_fp8_forward_workspace_bytes(int64_t N, int64_t V, int64_t D) {
+    if (!matrix(N, V) || D < 1 || D > MAX_HIDDEN) return 0;
+    return forward_ws(N, V, D).total;
+}
+
+int lsr_fp8_forward(int64_t N, int64_t V, int64_t D, int32_t h_dtype, int32_t out_dtype, const void* H, int64_t ldh, const void* W, int64_t ldw, const float* bias, void* out,
+                    int64_t ldo, uint8_t* Wt, int64_t ldwt, uint8_t* wt_exps, void* workspace, size_t workspace_bytes, lsr_stream_t stream) {
+    if (!float_type(h_dtype) || !float_type(out_dtype)) return LSR_ERR_DTYPE;
+    if (!matrix(N, V) || D < 1 || D > MAX_HIDDEN || ldh < D || ldw < D || ldo < V || (Wt && ldwt != 0 && ldwt < up(V, 128))) return LSR_ERR_SHAPE;
+    if (!H || !W || !out || (Wt && !wt_exps)) return LSR_ERR_NULL;
+    if (off_type(H, type_bytes(h_dtype)) || off_type(W, type_bytes(h_dtype)) || off_type(bias, 4) || off_type(out, type_bytes(out_dtype)) ||
+        (Wt && (misaligned(Wt) || ldwt % 16 != 0 || off_type(wt_exps, 4))))
+        return LSR_ERR_ALIGN;
+    const ForwardWs w = forward_ws(N, V, D);
+    if (!workspace || workspace_bytes < w.total) return LSR_ERR_WORKSPACE;
+    if (misaligned(workspace)) return LSR_ERR_ALIGN;
+    int n_cus = 0;
+    int rc = check_device(&n_cus);
+    if (rc != LSR_OK) return rc;
+    char* const ws = static_cast<char*>(workspace);
+    const Fp8Rows weights = fp8_rows(ws + w.w, up(D, 128), ws + w.w_exp, D), turned = Wt ? fp8_rows(Wt, ldwt, wt_exps, V) : Fp8Rows{};
+    if (few(N, D)) {
+        rc = quantize(h_dtype, V, D, W, ldw, true, weights, turned, stream);
+        if (rc != LSR_OK) return rc;
+        return few_logits(N, V, D, h_dtype, out_dtype, H, ldh, nullptr, weights, bias, out, ldo, n_cus, stream);
+    }
+    const Fp8Rows states = fp8_rows(ws + w.q, up(D, 128), ws + w.exps, D);
+    const Fp8TileParams p = tiles_of(V, D, W, ldw, weights, turned);
+    if (h_dtype == LSR_F32) forward_quantize<float>(p, H, ldh, N, D, states, stream);
+    else forward_quantize<uint16_t>(p, H, ldh, N, D, states, stream);
+    rc = launch_status();
+    if (rc != LSR_OK) return rc;
+    return logits(N, V, D, out_dtype, states, weights, bias, out, ldo, stream);
 }
 
 size_t lsr_fp8_backward_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t need_dh, int32_t need_dw, int32_t need_db) {

@@ -38,6 +38,12 @@ def quantize_blocks(X: torch.Tensor, square: bool = False, transposed: bool = Fa
 
 
 @functools.lru_cache(maxsize=256)
+def _forward_bytes(N: int, V: int, D: int):
+    """(of the workspace, of the matrix transposed by slab, of its exponents)"""
+    return lsr.lsr_fp8_forward_workspace_bytes(N, V, D), lsr.lsr_fp8_slab_bytes(D, V), lsr.lsr_fp8_exp_bytes(D, V)
+
+
+@functools.lru_cache(maxsize=256)
 def _backward_bytes(N: int, V: int, D: int, need_h: bool, need_w: bool, need_b: bool) -> int:
     return lsr.lsr_fp8_backward_workspace_bytes(N, V, D, need_h, need_w, need_b)
 
@@ -98,27 +104,27 @@ class _Fp8Logits(torch.autograd.Function):
         N, D = H.shape
         V = W.shape[0]
         kind = _KIND[H.dtype]
-        need_t = ctx.needs_input_grad[0] and N > 0      # dH takes the matrix transposed: written beside the other from one read
-        W8 = torch.empty((V, _up(D, 128)), dtype=torch.uint8, device=H.device)
-        exps = torch.empty(lsr.lsr_fp8_exp_bytes(V, D), dtype=torch.uint8, device=H.device)
-        Wt = torch.empty(lsr.lsr_fp8_slab_bytes(D, V), dtype=torch.uint8, device=H.device) if need_t else None
-        exps_t = torch.empty(lsr.lsr_fp8_exp_bytes(D, V), dtype=torch.uint8, device=H.device) if need_t else None
+        need_t = ctx.needs_input_grad[0] and N > 0      # dH takes the matrix transposed, exponents behind it: written beside the other from one read
+        out = torch.empty((N, V), dtype=dtype, device=H.device)
+        Wt = None
         if N:
+            ws_bytes, slab_bytes, exp_bytes = _forward_bytes(N, V, D)
             with _on(H.device):
-                lsr.lsr_fp8_quantize(V, D, kind, W, _ld(W), True, W8, W8.shape[1], exps, Wt, 0, exps_t)
-                out = _matmul(H, kind, D, W8, exps, bias, dtype)
-        else:
-            out = torch.empty((N, V), dtype=dtype, device=H.device)
+                ws = torch.empty(ws_bytes, dtype=torch.uint8, device=H.device)
+                if need_t:
+                    Wt = torch.empty(slab_bytes + exp_bytes, dtype=torch.uint8, device=H.device)
+                    at = Wt.data_ptr()
+                lsr.lsr_fp8_forward(N, V, D, kind, _KIND[dtype], H, _ld(H), W, _ld(W), bias, out, V, *((at, 0, at + slab_bytes) if need_t else (None, 0, None)), ws)
         ctx.shape = (N, V, D, _KIND[dtype], kind)
         ctx.has_bias = bias is not None
-        ctx.save_for_backward(H, W, Wt, exps_t)
+        ctx.save_for_backward(H, W, Wt)
         ctx.set_materialize_grads(False)
         return out
 
     @staticmethod
     def backward(ctx, dY):
         # (this runs in a thread where every call costs more than elsewhere: few of them)
-        H, W, Wt, exps_t = ctx.saved_tensors
+        H, W, Wt = ctx.saved_tensors
         N, V, D = ctx.shape[:3]
         need_h, need_w, need_b = ctx.needs_input_grad[:3]
         need_b = need_b and ctx.has_bias
@@ -132,9 +138,14 @@ class _Fp8Logits(torch.autograd.Function):
                     g.zero_()
         elif need_h or need_w or need_b:
             y = _rows(dY)
+            if need_h:
+                at = Wt.data_ptr()
+                Wt = (at, 0, at + _forward_bytes(N, V, D)[1])
+            else:
+                Wt = (None, 0, None)
             with _on(dev):
                 ws = torch.empty(_backward_bytes(N, V, D, need_h, need_w, need_b), dtype=torch.uint8, device=dev)
-                lsr.lsr_fp8_backward(*ctx.shape, y, _ld(y), H, _ld(H), Wt, 0, exps_t, dH, dW, db, ws)
+                lsr.lsr_fp8_backward(*ctx.shape, y, _ld(y), H, _ld(H), *Wt, dH, dW, db, ws)
             if torch.is_grad_enabled():
                 dH, dW, db = first_order_only("fp8_logits", (dH, dW, db), (H, W, dY))
         return dH, dW, db, None

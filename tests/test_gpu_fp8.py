@@ -354,6 +354,29 @@ def test_shapes_types_and_views_in_training():
             bad()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,D", [(1, 1, 1), (20, 700, 768), (33, 129, 100), (300, 1000, 312), (5, 300, 4000)])
+def test_forward_is_quantize_and_matmul(N, V, D, dtype):
+    gen = torch.Generator().manual_seed(N)
+    H, W = values(gen, (N, D + 3), dtype, 0.5)[:, 1:D + 1], values(gen, (V, D + 5), dtype, 0.5)[:, 3:D + 3]
+    bias = torch.randn(V, generator=gen).to(DEV)
+    ws = torch.empty(binding.lsr_fp8_forward_workspace_bytes(N, V, D), dtype=torch.uint8, device=DEV)
+    head = fp8.Fp8Head(W, bias)
+    qt, et = fp8.quantize_blocks(W, True, True)
+    for out in TYPES:
+        for wide in (0, 32):
+            Y = torch.full((N, V + 3), 7.0, dtype=TYPES[out], device=DEV)
+            Wt = torch.full((D, qt.shape[1] + wide), 99, dtype=torch.uint8, device=DEV)
+            Et = torch.zeros(et.numel(), dtype=torch.uint8, device=DEV)
+            binding.lsr_fp8_forward(N, V, D, KIND[dtype], KIND[out], H, D + 3, W, D + 5, bias, Y, V + 3, *((Wt, Wt.shape[1], Et) if wide else (None, 0, None)), ws)
+            assert torch.equal(Y[:, :V], head.logits(H, TYPES[out])) and (Y[:, V:] == 7).all()
+            if wide:
+                used = (V + 127) // 128
+                assert torch.equal(Wt[:, :qt.shape[1]], qt) and (Wt[:, qt.shape[1]:] == 99).all()
+                for b in range(used):
+                    assert torch.equal(Et.view(-1, D, 4)[b // 4, :, b % 4], et[b // 4, :, b % 4])
+
+
 def test_second_derivatives_raise():
     gen = torch.Generator().manual_seed(12)
     H, W = values(gen, (5, 32), "f32", 0.5).requires_grad_(True), values(gen, (40, 32), "f32", 0.5).requires_grad_(True)

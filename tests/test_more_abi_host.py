@@ -61,6 +61,21 @@ def test_fp8_matmul_refusals():
     assert binding.lsr_fp8_matmul_workspace_bytes(100, 300, 100, 3) == 0 and binding.lsr_fp8_matmul_workspace_bytes(0, 300, 100, 0) == 0
 
 
+def test_fp8_forward_refusals():
+    def f(N=100, V=300, D=100, h=lsr.LSR_BF16, o=lsr.LSR_F32, H=P, ldh=100, W=P, ldw=100, bias=P, out=P, ldo=300, Wt=P, ldwt=384, et=P, ws=WS):
+        return status(binding.lsr_fp8_forward, N, V, D, h, o, H, ldh, W, ldw, bias, out, ldo, Wt, ldwt, et, ws)
+    assert f(h=3) == f(h=lsr.LSR_I8) == f(o=3) == DTYPE
+    for bad in ({"N": 0}, {"V": 0}, {"D": 0}, {"D": 65537, "ldh": 65537, "ldw": 65537}, {"ldh": 99}, {"ldw": 99}, {"ldo": 299}, {"ldwt": 368},
+                {"N": 1 << 20, "V": 1 << 20, "ldo": 1 << 20, "ldwt": 0}):
+        assert f(**bad) == SHAPE, bad
+    assert f(H=None) == f(W=None) == f(out=None) == f(et=None) == NULL
+    assert f(H=P + 1) == f(W=P + 1) == f(bias=P + 2) == f(out=P + 2) == f(Wt=P + 8) == f(ldwt=392) == f(et=P + 2) == f(h=lsr.LSR_F32, W=P + 2) == ALIGN
+    g = binding.lsr_fp8_forward_workspace_bytes
+    need = g(100, 300, 100)
+    assert need >= 400 * 132 and f(ws=None) == WORKSPACE and f(ws=(P, need - 1)) == WORKSPACE and f(ws=(P + 8, need)) == ALIGN
+    assert g(0, 300, 100) == g(100, 300, 65537) == 0 and g(1, 300, 100) >= 300 * 132
+
+
 def test_fp8_backward_refusals():
     def b(N=100, V=300, D=100, y=lsr.LSR_BF16, h=lsr.LSR_BF16, dY=P, ldy=300, H=P, ldh=100, Wt=P, ldwt=384, et=P, dH=P, dW=P, db=P, ws=WS):
         return status(binding.lsr_fp8_backward, N, V, D, y, h, dY, ldy, H, ldh, Wt, ldwt, et, dH, dW, db, ws)
