@@ -80,7 +80,7 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
  * elements, W held in blocks of 128 x 128 and H in blocks of 1 x 128 within the call.
  *   Wt [D, ldwt], wt_exps: what lsr_fp8_backward takes of the matrix, as lsr_fp8_quantize writes Qt (square; ldwt = 0 by slab), or NULL for no dH
  *   out, bias: as above; the results are the bits of lsr_fp8_quantize and lsr_fp8_matmul.
- * Limits: as above, with D for K.
+ * Limits: 1 <= N, V <= 2^22, 1 <= D <= 65536, N V, N D and V D < 2^36.
  */
 size_t lsr_fp8_forward_workspace_bytes(int64_t N, int64_t V, int64_t D);
 
@@ -99,7 +99,7 @@ int lsr_fp8_forward(int64_t N, int64_t V, int64_t D, int32_t h_dtype, int32_t ou
  *   dH [N, D], dW [V, D] of h_dtype, contiguous; db [V] f32; each may be NULL to skip it.  H is needed for dW alone, Wt for dH alone.
  * Sums are formed as in lsr_fp8_matmul (exact products and float32 sums where h_dtype is LSR_F32), over cuts of the contracted axis where there are
  * few tiles, joined in float32 in a fixed order and rounded once.  Results are the same bits from call to call.  The workspace may be of 0 bytes, and then NULL.
- * Limits: 1 <= N, V <= 2^22, N V < 2^36, 1 <= D <= 65536, ldwt <= 2^23.
+ * Limits: 1 <= N, V <= 2^22, 1 <= D <= 65536, N V, N D and V D < 2^36, ldwt <= 2^23.
  */
 size_t lsr_fp8_backward_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t need_dh, int32_t need_dw, int32_t need_db);
 

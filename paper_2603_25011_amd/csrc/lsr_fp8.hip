@@ -12,7 +12,7 @@ namespace {
 
 using namespace lsr;
 
-// Launches stay below 2^32 threads: 64 per row, 256 per 128 x 128 values (of two arrays of a backward: at most 2^23 tiles together), 256 per tile of 128 x 256 results.
+// Launches stay below 2^32 threads: 64 per row, 256 per 128 x 128 values (a step's two arrays have at most 2^23 such tiles together), 256 per tile of 128 x 256 results.
 constexpr int64_t MAX_AXIS = int64_t(1) << 22;
 constexpr int64_t MAX_VALUES = int64_t(1) << 36;
 constexpr int64_t MAX_HIDDEN = 65536;
@@ -25,6 +25,8 @@ inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 inline bool matrix(int64_t rows, int64_t cols) {
     return rows >= 1 && rows <= MAX_AXIS && cols >= 1 && cols <= MAX_AXIS && rows * cols < MAX_VALUES;
 }
+// N tokens, V rows of the matrix, D values of either
+inline bool step_shape(int64_t N, int64_t V, int64_t D) { return matrix(N, V) && matrix(N, D) && matrix(V, D) && D <= MAX_HIDDEN; }
 inline int64_t exp_bytes(int64_t rows, int64_t cols) { return 4 * rows * ((cols + 511) / 512); }
 
 // e4m3 rows of `cols` values, ld apart or (ld = 0) by slab.
@@ -315,14 +317,14 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
 }
 
 size_t lsr_fp8_forward_workspace_bytes(int64_t N, int64_t V, int64_t D) {
-    if (!matrix(N, V) || D < 1 || D > MAX_HIDDEN) return 0;
+    if (!step_shape(N, V, D)) return 0;
     return forward_ws(N, V, D).total;
 }
 
 int lsr_fp8_forward(int64_t N, int64_t V, int64_t D, int32_t h_dtype, int32_t out_dtype, const void* H, int64_t ldh, const void* W, int64_t ldw, const float* bias, void* out,
                     int64_t ldo, uint8_t* Wt, int64_t ldwt, uint8_t* wt_exps, void* workspace, size_t workspace_bytes, lsr_stream_t stream) {
     if (!float_type(h_dtype) || !float_type(out_dtype)) return LSR_ERR_DTYPE;
-    if (!matrix(N, V) || D < 1 || D > MAX_HIDDEN || ldh < D || ldw < D || ldo < V || (Wt && ldwt != 0 && ldwt < up(V, 128))) return LSR_ERR_SHAPE;
+    if (!step_shape(N, V, D) || ldh < D || ldw < D || ldo < V || (Wt && ldwt != 0 && ldwt < up(V, 128))) return LSR_ERR_SHAPE;
     if (!H || !W || !out || (Wt && !wt_exps)) return LSR_ERR_NULL;
     if (off_type(H, type_bytes(h_dtype)) || off_type(W, type_bytes(h_dtype)) || off_type(bias, 4) || off_type(out, type_bytes(out_dtype)) ||
         (Wt && (misaligned(Wt) || ldwt % 16 != 0 || off_type(wt_exps, 4))))
@@ -350,7 +352,7 @@ int lsr_fp8_forward(int64_t N, int64_t V, int64_t D, int32_t h_dtype, int32_t ou
 }
 
 size_t lsr_fp8_backward_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t need_dh, int32_t need_dw, int32_t need_db) {
-    if (!matrix(N, V) || D < 1 || D > MAX_HIDDEN) return 0;
+    if (!step_shape(N, V, D)) return 0;
     return backward_ws(N, V, D, need_dh != 0, need_dw != 0, need_db != 0, grads_plan(N, V, D, need_dh != 0, need_dw != 0)).total;
 }
 
@@ -358,7 +360,7 @@ int lsr_fp8_backward(int64_t N, int64_t V, int64_t D, int32_t y_dtype, int32_t h
                      const uint8_t* Wt, int64_t ldwt, const uint8_t* wt_exps, void* dH, void* dW, float* db, void* workspace, size_t workspace_bytes,
                      lsr_stream_t stream) {
     if (!float_type(y_dtype) || !float_type(h_dtype)) return LSR_ERR_DTYPE;
-    if (!matrix(N, V) || D < 1 || D > MAX_HIDDEN || ldy < V) return LSR_ERR_SHAPE;
+    if (!step_shape(N, V, D) || ldy < V) return LSR_ERR_SHAPE;
     if ((dW && ldh < D) || (dH && ((ldwt != 0 && ldwt < up(V, 128)) || ldwt > MAX_LD))) return LSR_ERR_SHAPE;
     if (!dY || (!dH && !dW && !db) || (dW && !H) || (dH && (!Wt || !wt_exps))) return LSR_ERR_NULL;
     if (off_type(dY, type_bytes(y_dtype)) || (dW && off_type(H, type_bytes(h_dtype))) || (dH && (misaligned(Wt) || ldwt % 16 != 0 || off_type(wt_exps, 4))) ||

@@ -138,14 +138,13 @@ class _Fp8Logits(torch.autograd.Function):
                     g.zero_()
         elif need_h or need_w or need_b:
             y = _rows(dY)
+            turned = (None, 0, None)
             if need_h:
                 at = Wt.data_ptr()
-                Wt = (at, 0, at + _forward_bytes(N, V, D)[1])
-            else:
-                Wt = (None, 0, None)
+                turned = (at, 0, at + _forward_bytes(N, V, D)[1])
             with _on(dev):
                 ws = torch.empty(_backward_bytes(N, V, D, need_h, need_w, need_b), dtype=torch.uint8, device=dev)
-                lsr.lsr_fp8_backward(*ctx.shape, y, _ld(y), H, _ld(H), *Wt, dH, dW, db, ws)
+                lsr.lsr_fp8_backward(*ctx.shape, y, _ld(y), H, _ld(H), *turned, dH, dW, db, ws)
             if torch.is_grad_enabled():
                 dH, dW, db = first_order_only("fp8_logits", (dH, dW, db), (H, W, dY))
         return dH, dW, db, None

@@ -66,7 +66,8 @@ def test_fp8_forward_refusals():
         return status(binding.lsr_fp8_forward, N, V, D, h, o, H, ldh, W, ldw, bias, out, ldo, Wt, ldwt, et, ws)
     assert f(h=3) == f(h=lsr.LSR_I8) == f(o=3) == DTYPE
     for bad in ({"N": 0}, {"V": 0}, {"D": 0}, {"D": 65537, "ldh": 65537, "ldw": 65537}, {"ldh": 99}, {"ldw": 99}, {"ldo": 299}, {"ldwt": 368},
-                {"N": 1 << 20, "V": 1 << 20, "ldo": 1 << 20, "ldwt": 0}):
+                {"N": 1 << 20, "V": 1 << 20, "ldo": 1 << 20, "ldwt": 0}, {"N": 1 << 22, "D": 1 << 15, "ldh": 1 << 15, "ldw": 1 << 15},
+                {"N": 40, "V": 1 << 22, "ldo": 1 << 22, "D": 1 << 15, "ldh": 1 << 15, "ldw": 1 << 15, "ldwt": 0}):
         assert f(**bad) == SHAPE, bad
     assert f(H=None) == f(W=None) == f(out=None) == f(et=None) == NULL
     assert f(H=P + 1) == f(W=P + 1) == f(bias=P + 2) == f(out=P + 2) == f(Wt=P + 8) == f(ldwt=392) == f(et=P + 2) == f(h=lsr.LSR_F32, W=P + 2) == ALIGN
@@ -81,7 +82,7 @@ def test_fp8_backward_refusals():
         return status(binding.lsr_fp8_backward, N, V, D, y, h, dY, ldy, H, ldh, Wt, ldwt, et, dH, dW, db, ws)
     assert b(y=3) == DTYPE and b(h=lsr.LSR_I8) == DTYPE
     for bad in ({"N": 0}, {"V": 0}, {"D": 0}, {"D": 65537, "ldh": 65537}, {"ldy": 299}, {"ldh": 99}, {"ldwt": 368}, {"ldwt": (1 << 23) + 16},
-                {"N": 1 << 20, "V": 1 << 20, "ldy": 1 << 20}):
+                {"N": 1 << 20, "V": 1 << 20, "ldy": 1 << 20}, {"N": 1 << 22, "D": 1 << 15, "ldh": 1 << 15}, {"V": 1 << 22, "ldy": 1 << 22, "D": 1 << 15, "ldh": 1 << 15, "ldwt": 0}):
         assert b(**bad) == SHAPE, bad
     assert b(dY=None) == NULL and b(H=None) == NULL and b(Wt=None) == NULL and b(et=None) == NULL and b(dH=None, dW=None, db=None) == NULL
     assert b(dY=P + 1) == ALIGN and b(H=P + 1) == ALIGN and b(Wt=P + 8) == ALIGN and b(ldwt=392) == ALIGN and b(et=P + 2) == ALIGN
