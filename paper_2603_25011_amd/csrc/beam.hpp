@@ -358,7 +358,9 @@ enum { BEAM_NONE = 0, BEAM_GOES_ON = 1, BEAM_FINISHED = 2, BEAM_NAN = 3 };
 // of the lists; a threshold comes of them bit by bit from each wave's ballots, what reaches it goes to a list in LDS, and a candidate's place is the number of better ones
 // (counting for each of the 256 maxima the larger ones instead took 1.2 to 2 us longer).  Latency bounds it, so the keys are on their way while the normalisers are formed, and
 // each thread keeps the scores of its first BEAM_OWN: 5.0 us for 4 beams with 14 segments and K = 8, 7.8 for 64 sequences of 8 beams with 2 and K = 16.
+// More candidates than BEAM_RANKED at or above the threshold have equal scores as a rule (a head whose logits are all alike): ranking them against each other took 50 ms for 16 beams and K = 32.
 constexpr int BEAM_OWN = 4;
+constexpr int BEAM_RANKED = 256;
 __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
     // a beam's candidates have score s_base + (x - s_top) / T: the difference first, which is exact
     __shared__ double s_base[BEAM_MAX_BEAMS], s_top[BEAM_MAX_BEAMS];
@@ -368,6 +370,10 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
     __shared__ __attribute__((aligned(16))) uint64_t s_score[BEAM_JOIN];
     __shared__ uint16_t s_at[BEAM_JOIN];
     __shared__ uint64_t s_key[BEAM_JOIN];
+    __shared__ uint64_t s_pick_score[BEAM_MAX_K], s_pick_key[BEAM_MAX_K];
+    __shared__ uint16_t s_pick_at[BEAM_MAX_K];
+    __shared__ uint32_t s_some[BEAM_WAVES], s_every[BEAM_WAVES];
+    __shared__ int s_sum[2][BEAM_WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t b = blockIdx.x;
     const double inv_t = 1.0 / p.temperature, cd = 1.4426950408889634 * inv_t;
@@ -473,7 +479,84 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_join_kernel(BeamParams p) {
         enter(i, candidate(i, k), k);
     }
     __syncthreads();
-    const int n = s_count;
+    int n = s_count;
+    if (n > BEAM_RANKED) {
+        // so many (of equal scores, as a rule) are cut to the K best first, bit by bit of all that orders them; a thread sees to every BEAM_THREADS-th
+        auto word = [&](int at, int w) -> uint32_t {
+            if (w == 0) return (uint32_t)(s_score[at] >> 32);
+            if (w == 1) return (uint32_t)s_score[at];
+            if (w == 3) return (uint32_t)(s_key[at] >> 32);
+            if (w == 4) return (uint32_t)s_key[at];
+            if (w == 5) return 0xffffu - s_at[at];
+            int l, m;
+            place(s_at[at], l, m);
+            return (uint32_t)(BEAM_MAX_BEAMS - 1 - m);
+        };
+        static_assert(BEAM_JOIN <= 32 * BEAM_THREADS, "a thread's entries have a bit each");
+        const int mine_n = (n - tid + BEAM_THREADS - 1) / BEAM_THREADS;
+        uint32_t open = mine_n >= 32 ? ~0u : (1u << mine_n) - 1u, in = 0;       // whose place is not decided yet; who is among the K
+        int need = p.K, left = n, turn = 0;
+        for (int w = 0; w < 6 && left != need; ++w) {
+            // the bits in which not all are alike
+            uint32_t some = 0, every = ~0u;
+            for (uint32_t rest = open; rest; rest &= rest - 1) {
+                const uint32_t x = word(__builtin_ctz(rest) * BEAM_THREADS + tid, w);
+                some |= x;
+                every &= x;
+            }
+#pragma unroll
+            for (int o = 32; o; o >>= 1) {
+                some |= (uint32_t)__shfl_xor((int)some, o);
+                every &= (uint32_t)__shfl_xor((int)every, o);
+            }
+            if (lane == 0) { s_some[wave] = some; s_every[wave] = every; }
+            __syncthreads();
+            uint32_t bits = (s_some[0] | s_some[1] | s_some[2] | s_some[3]) & ~(s_every[0] & s_every[1] & s_every[2] & s_every[3]);
+            __syncthreads();
+            while (bits && left != need) {
+                const int bit = 31 - __builtin_clz(bits);
+                bits &= ~(1u << bit);
+                uint32_t ones = 0;
+                for (uint32_t rest = open; rest; rest &= rest - 1) {
+                    const int q = __builtin_ctz(rest);
+                    ones |= (word(q * BEAM_THREADS + tid, w) >> bit & 1u) << q;
+                }
+                int c = __popc(ones);
+#pragma unroll
+                for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
+                if (lane == 0) s_sum[turn][wave] = c;
+                __syncthreads();
+                c = (s_sum[turn][0] + s_sum[turn][1]) + (s_sum[turn][2] + s_sum[turn][3]);
+                turn ^= 1;
+                if (c >= need) {
+                    open = ones;
+                    left = c;
+                } else {
+                    in |= ones;
+                    open &= ~ones;
+                    need -= c;
+                    left -= c;
+                }
+            }
+        }
+        in |= open;                              // (all of them: candidates differ in their numbers at the latest)
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+        for (; in; in &= in - 1) {
+            const int from = __builtin_ctz(in) * BEAM_THREADS + tid, at = atomicAdd(&s_count, 1);
+            s_pick_score[at] = s_score[from];
+            s_pick_key[at] = s_key[from];
+            s_pick_at[at] = s_at[from];
+        }
+        __syncthreads();
+        n = p.K;
+        if (tid < n) {
+            s_score[tid] = s_pick_score[tid];
+            s_key[tid] = s_pick_key[tid];
+            s_at[tid] = s_pick_at[tid];
+        }
+        __syncthreads();
+    }
     // whether entry r comes before q, of equal score
     auto first_of = [&](int r, int q) -> bool {
         int l, mr, mq;

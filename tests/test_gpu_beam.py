@@ -106,6 +106,52 @@ def test_hard_rows(V, dtype):
     check(x, s, 16, 0.05, None, 3)
 
 
+def check_alike(X, scores, K):
+    """Continuations of different beams may be equal in exact arithmetic while either side rounds them apart (score 1 with logits 1, 0, 1 and score 0 with 1, 1, 0: the
+    second token of the one and the first of the other both have -log(2 + 1/e)).  A score of either beam is off by at most 64 u (its normaliser, see above) + u |s|, so two
+    whose exact scores differ by less than 128 u + 2 u |s| may stand in either order: a place holds what is wanted there or another continuation that near it, none twice."""
+    got = beam.beam_select(X, scores, K)
+    x, s = host(X), host(scores)
+    want = orc.select(x, s, K)
+    values, beams, tokens = (t.cpu().numpy() for t in got)
+    for b in range(X.shape[0]):
+        seen = set()
+        for k in range(K):
+            w, m, t = want[0][b, k], int(beams[b, k]), int(tokens[b, k])
+            assert (math.isnan(w) and math.isnan(values[b, k])) or w == values[b, k] or abs(w - values[b, k]) <= U * abs(w) + 64 * U
+            if not math.isfinite(w):
+                assert (m, t) == (want[1][b, k], want[2][b, k])
+                continue
+            assert (m, t) not in seen
+            seen.add((m, t))
+            if (m, t) != (want[1][b, k], want[2][b, k]):
+                z = x[b, m]
+                own = s[b, m] + ((z[t] - z.max()) - np.log(np.exp(z - z.max()).sum()))
+                assert abs(own - w) <= 128 * U + 2 * U * abs(w), (b, k, own, w)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,beams,V,K", [(2, 16, 30522, 32), (1, 64, 1500, 128), (3, 5, 20000, 7), (2, 12, 700, 1)])
+def test_many_candidates_of_equal_score(B, beams, V, K, dtype):
+    """More than are ranked against each other: by beam and token, whatever is alike."""
+    gen = torch.Generator().manual_seed(V)
+    x = torch.zeros(B, beams, V, dtype=TYPES[dtype], device=DEV)
+    s = torch.zeros(B, beams, device=DEV)
+    got = check(x, s, K)
+    assert (got[1] == 0).all() and torch.equal(got[2], torch.arange(K, dtype=torch.int32, device=DEV).expand(B, K))
+    s[:, 0] = -1.0                             # the best are another beam's
+    check(x, s, K)
+    x[:] = (torch.rand(B, beams, V, generator=gen) < 0.5).to(x)          # two values
+    s[:] = torch.randint(0, 2, (B, beams), generator=gen).to(s)
+    check_alike(x, s, K)
+    x[0, beams // 2, V // 3] = math.nan        # a beam that comes first, and has places enough
+    check_alike(x, s, K)
+    x[:, :, 3:] = -math.inf                    # fewer than there are places for, and then none
+    check_alike(x, s, K)
+    x[:] = -math.inf
+    check_alike(x, s, K)
+
+
 def test_the_first_of_equal_beams_wins():
     x = torch.zeros(1, 3, 50, device=DEV)
     s = torch.zeros(1, 3, device=DEV)
