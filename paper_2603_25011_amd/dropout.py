@@ -49,7 +49,8 @@ def dropout(x: torch.Tensor, p: float, seed: int = 0, offset: int = 0, state: to
     The number of element i (in row-major order, whatever the strides) is the (i % 8)-th half word of the Philox4x32-10 block at counter (i // 8,
     offset) with key `seed`: calls with other seeds or offsets draw other masks, the same call draws the same one.  `state`, an int64 tensor
     of two on the same GPU, is added to (seed, offset) when the work runs: a program that captures a step into a graph advances it between replays, and between steps only
-    (the backward reads it again; where it was changed before, autograd says so)."""
+    (the backward reads it again; where it was changed before, autograd says so).  While a step is captured no result of an eager call on the same
+    tensor may still hold its own autograd graph (autograd would run part of the captured backward on the eager call's stream)."""
     _on_gpu("dropout", x, state)
     _kind(x, "dropout", "x")
     if not 0.0 <= p <= 1.0:

@@ -377,6 +377,36 @@ def test_forward_is_quantize_and_matmul(N, V, D, dtype):
                     assert torch.equal(Et.view(-1, D, 4)[b // 4, :, b % 4], et[b // 4, :, b % 4])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_what_is_not_finite_in_training_shows_where_it_belongs(dtype):
+    """A gradient, a token or a row of the matrix that is not finite: in its own rows and columns, and all else as without it but for the blocks that it shares."""
+    gen = torch.Generator().manual_seed(21)
+    N, V, D = 300, 517, 200
+    H, W, dY = values(gen, (N, D), dtype, 0.0), values(gen, (V, D), dtype, 0.0), values(gen, (N, V), dtype, 0.0)
+    H[7, 3], W[400, 150], dY[130, 20], dY[131, 21] = float("nan"), float("inf"), float("inf"), float("nan")
+    y, dH, dW, db = train(H, W, torch.zeros(V, device=DEV), dY, dtype)
+    h, w, g = host(H), host(W), host(dY)
+    with np.errstate(invalid="ignore"):
+        hq, wq, gq = orc.blocks(h, 1, 128)[0], orc.blocks(w, 128, 128)[0], orc.blocks(g, 1, 128)[0]
+        ht, gt = orc.blocks(h, 128, 1)[0], orc.blocks(g, 128, 1)[0]
+        for got, a, b in ((y, hq, wq), (dH, gq, wq.T), (dW, gt.T, ht.T)):
+            want = a @ b.T
+            got = host(got)
+            assert np.array_equal(np.isnan(got), np.isnan(want)) and 0 < np.isnan(want).sum() < want.size
+            fine = np.where(np.isnan(want), 0.0, want)
+            close(np.where(np.isnan(got), 0.0, got), fine, tolerance(np.nan_to_num(a, nan=0.0), np.nan_to_num(b, nan=0.0), fine, dtype), "values")
+        want = g.sum(axis=0)
+    assert np.isinf(host(db)[20]) and np.isnan(host(db)[21]) and np.isfinite(np.delete(host(db), [20, 21])).all() and np.isnan(want[21])
+
+
+def test_no_gradient_recorded():
+    gen = torch.Generator().manual_seed(22)
+    H, W = values(gen, (50, 64), "bf16").requires_grad_(True), values(gen, (90, 64), "bf16").requires_grad_(True)
+    with torch.no_grad():
+        y = fp8.fp8_logits(H, W)
+    assert not y.requires_grad and torch.equal(y, fp8.fp8_logits(H, W).detach())
+
+
 def test_second_derivatives_raise():
     gen = torch.Generator().manual_seed(12)
     H, W = values(gen, (5, 32), "f32", 0.5).requires_grad_(True), values(gen, (40, 32), "f32", 0.5).requires_grad_(True)
