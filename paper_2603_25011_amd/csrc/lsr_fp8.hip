@@ -180,7 +180,9 @@ int launch_grads(Fp8Job h, Fp8Job w, const GradsPlan& plan, float* h_parts, floa
     return launch_status();
 }
 
-bool few(int64_t N, int64_t K) { return N <= FEWF_ROWS && N * fewf_stride(K) <= FEWF_LDS; }
+// Few rows: 32 for float32 results, 24 for bfloat16 ones, where the tiles have the faster instruction.  us of few rows : of tiles, 250002 x 1024 (30522 x 768 alike), float32 64 : 68 at 32
+// rows, bfloat16 46.7 : 50 at 16, 51.8 : 50 at 24, 60.6 : 50 at 32.
+bool few(int64_t N, int64_t K, int32_t out_type) { return N <= (out_type == LSR_F32 ? FEWF_ROWS : 24) && N * fewf_stride(K) <= FEWF_LDS; }
 
 template <typename T>
 void launch_few(const Fp8FewParams& p, int32_t out_type, int n_cus, hipStream_t st) {
@@ -217,8 +219,8 @@ ForwardWs forward_ws(int64_t N, int64_t V, int64_t D) {
     w.w = 0;
     w.w_exp = align_up((size_t)V * up(D, 128));
     w.q = w.w_exp + align_up((size_t)exp_bytes(V, D));
-    w.exps = w.q + (few(N, D) ? 0 : align_up((size_t)N * up(D, 128)));
-    w.total = w.exps + (few(N, D) ? 0 : (size_t)exp_bytes(N, D));
+    w.exps = w.q + (few(N, D, LSR_BF16) ? 0 : align_up((size_t)N * up(D, 128)));
+    w.total = w.exps + (few(N, D, LSR_BF16) ? 0 : (size_t)exp_bytes(N, D));
     return w;
 }
 
@@ -305,7 +307,7 @@ int lsr_fp8_matmul(int64_t N, int64_t V, int64_t K, int32_t a_dtype, int32_t out
     int rc = check_device(&n_cus);
     if (rc != LSR_OK) return rc;
     const Fp8Rows weights = fp8_rows(W, ldw, w_exps, K);
-    if (few(N, K)) return few_logits(N, V, K, a_dtype, out_dtype, A, lda, a_exps, weights, bias, out, ldo, n_cus, stream);
+    if (few(N, K, out_dtype)) return few_logits(N, V, K, a_dtype, out_dtype, A, lda, a_exps, weights, bias, out, ldo, n_cus, stream);
     Fp8Rows states = fp8_rows(A, lda, a_exps, K);
     if (!bytes) {
         char* const ws = static_cast<char*>(workspace);
@@ -337,7 +339,7 @@ int lsr_fp8_forward(int64_t N, int64_t V, int64_t D, int32_t h_dtype, int32_t ou
     if (rc != LSR_OK) return rc;
     char* const ws = static_cast<char*>(workspace);
     const Fp8Rows weights = fp8_rows(ws + w.w, up(D, 128), ws + w.w_exp, D), turned = Wt ? fp8_rows(Wt, ldwt, wt_exps, V) : Fp8Rows{};
-    if (few(N, D)) {
+    if (few(N, D, out_dtype)) {
         rc = quantize(h_dtype, V, D, W, ldw, true, weights, turned, stream);
         if (rc != LSR_OK) return rc;
         return few_logits(N, V, D, h_dtype, out_dtype, H, ldh, nullptr, weights, bias, out, ldo, n_cus, stream);
