@@ -208,8 +208,6 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
         if (b0 + batch < nvec) fetch(next, b0 + batch);
         const float cold0 = cold;
         const int ties0 = ties;
-        float far_m0 = far_m;
-        double far0 = far;
         bool again = false;
         for (;;) {
             if (b0 == 0) {
@@ -265,16 +263,16 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
                 break;
             }
             const bool fits = have <= BEAM_CAP;
-            beam_rank(sh, min(have, BEAM_CAP), K);
-            const uint64_t kth = sh.top.best[K - 1];
+            beam_rank(sh, fits ? have : before, K);
             if (fits) {
                 flush();
-                thr = kth;
+                thr = sh.top.best[K - 1];
                 reference();
                 if (tv > base) {
                     sum *= part(base, tv);
                     base = tv;
                 }
+#pragma unroll 1
                 for (int q = K + tid; q < have; q += BEAM_THREADS) sum += part(sh.by_rank[q], base);      // what leaves the list: not above the new reference
                 for (int q = tid; q < K; q += BEAM_THREADS) sh.top.list[q] = sh.top.best[q];
                 if (tid == 0) sh.top.count = K;
@@ -283,33 +281,46 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
                 __syncthreads();
                 break;
             }
-            // too many of this batch for the list: what was there before it stays as far as it beats the new threshold, and the batch is
-            // gone through again (the K-th key itself may be one of the batch).  Which keys found room is chance, and so is this threshold: the sums keep
-            // their reference, and the batch ends with a cut to its true K largest.
-            again = true;
-            thr = kth - 1;
+            // Too many of this batch for the list (seldom: as where logits ascend): it is gone through again with a threshold that K of it, but no more than there is room for, reach,
+            // found bit by bit (all keys differ, so at the last bit it is the K-th).  The sums keep their reference, and the batch ends with a cut to its true K largest.
+            again = true;                        // (nothing of the batch is in `far` yet: what is above the reference was in the list, or equal to it)
             cold = cold0;
             ties = ties0;
-            far = far0;
-            far_m = far_m0;
-            uint64_t mine[BEAM_CAP / BEAM_THREADS];
-#pragma unroll
-            for (int q = 0; q < BEAM_CAP / BEAM_THREADS; ++q) {
-                const int k = q * BEAM_THREADS + tid;
-                mine[q] = k < before ? sh.top.list[k] : 0;
-            }
-            if (tid == 0) sh.top.count = 0;
-            __syncthreads();
+            uint64_t t = 0;
+            int reach = BEAM_CAP;
 #pragma unroll 1
-            for (int q = 0; q < BEAM_CAP / BEAM_THREADS; ++q) {
-                const uint64_t k = mine[q];
-                if (k > thr) sh.top.list[atomicAdd(&sh.top.count, 1)] = k;
-                else if (k) add_far(value_of((uint32_t)(k >> 32)));
+            for (int bit = 63; reach > BEAM_CAP / 2; --bit) {
+                const uint64_t higher = t | 1ull << bit;
+                int c = 0;
+#pragma unroll 1
+                for (int i = b0 * EPV + tid; i < min(b0 + batch, nvec) * EPV; i += BEAM_THREADS) {      // (read again: from the caches)
+                    float f;
+                    if constexpr (sizeof(T) == 4) f = x[i];
+                    else f = __uint_as_float((uint32_t)x[i] << 16);
+                    c += key_of(ordered(f), (uint32_t)(first + i)) >= higher ? 1 : 0;
+                }
+#pragma unroll
+                for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
+                if (lane == 0) sh.top.most[wave] = (uint32_t)c;
+                __syncthreads();
+                c = 0;
+#pragma unroll
+                for (int k = 0; k < BEAM_WAVES; ++k) c += (int)sh.top.most[k];
+                __syncthreads();
+                if (c >= K) {
+                    t = higher;
+                    reach = c;
+                }
             }
-            far_m0 = far_m;                      // (these are done with, the batch is not)
-            far0 = far;
-            __syncthreads();
-            before = sh.top.count;
+            thr = t - 1;                         // (above what it was: more than BEAM_CAP / 2 of the batch beat that)
+            // what was in the list before the batch stays as far as it beats the threshold
+            const int kept = __syncthreads_count(tid < min(before, K) && sh.top.best[tid] > thr);
+#pragma unroll 1
+            for (int q = kept + tid; q < before; q += BEAM_THREADS) add_far(sh.by_rank[q]);
+            for (int q = tid; q < kept; q += BEAM_THREADS) sh.top.list[q] = sh.top.best[q];
+            if (tid == 0) sh.top.count = kept;
+            before = kept;
+            ordered_list = false;
             __syncthreads();
         }
 #pragma unroll
@@ -324,6 +335,7 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
     const uint64_t largest = sh.top.best[0];
     const float m = largest ? value_of((uint32_t)(largest >> 32)) : base;
     double s = sum * part(base, m) + (far_m == -INFINITY ? far : far * part(far_m, m));
+#pragma unroll 1
     for (int q = tid; q < have; q += BEAM_THREADS) s += part(sh.by_rank[q], m);
 #pragma unroll
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);

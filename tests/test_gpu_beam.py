@@ -176,6 +176,27 @@ def test_normaliser_is_closer_than_float32():
         assert np.abs(host(got) - want).max() <= 1.1 * 2.0 ** -23
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_beat_every_threshold(dtype):
+    """Ascending logits, of one wave alone, or alike but for their index: more than the list holds in every batch.  Equal beams have equal sums, call after call."""
+    gen = torch.Generator().manual_seed(31)
+    V = 30011
+    x = torch.zeros(5, 3, V, device=DEV)
+    x[0] = torch.arange(V, device=DEV) * 3e-4
+    x[1] = (torch.arange(V) * 1e-3 + torch.rand(V, generator=gen) * 0.01).to(DEV)
+    x[2] = torch.where((torch.arange(V) // 512 % 4 == 1).to(DEV), x[1, 0] + 1.0, x[1, 0] - 40.0)
+    x[3] = 2.0
+    x[4] = (torch.arange(V, device=DEV) // 5000).float()
+    x[3, :, V // 2:] = 3.0
+    x = x.to(TYPES[dtype])
+    s = torch.zeros(5, 3, device=DEV)
+    got = check(x, s, 16)
+    check(x, s, 128)
+    check(x, s, 1)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(got, beam.beam_select(x, s, 16)))
+
+
 def test_rows_beyond_4_gib():
     V = 1 << 26
     x = torch.full((2, 20, V), -1.0, dtype=torch.bfloat16, device=DEV)
