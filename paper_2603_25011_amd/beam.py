@@ -124,11 +124,11 @@ def beam_reorder(states, parents: torch.Tensor, out=None):
             y = out[i]
             if y.shape != (B, K, *shape[2:]) or y.dtype != x.dtype:
                 raise ValueError("beam_reorder: out must be [B, K, ...] of the states' dtypes")
+            if y.is_conj() or y.is_neg():
+                raise ValueError("beam_reorder: out must hold its values as they are, not conjugated or negated")
         if x.is_conj() or x.is_neg():
             x = x.resolve_conj().resolve_neg()
             hold.append(x)
-        if y.is_conj() or y.is_neg():
-            raise ValueError("beam_reorder: out must hold its values as they are, not conjugated or negated")
         new.append(y)
         size = y.numel()
         if not size:

@@ -418,8 +418,8 @@ def lsr_beam_reorder(B, beams, K, parents, states, stream=None) -> None:
     and strides in bytes."""
     table = array.array("q")
     for s in states:
-        table.extend((_ptr(s[0]) or 0, _ptr(s[1]) or 0, *s[2:]))
-    _check(load_library().lsr_beam_reorder(int(B), int(beams), int(K), _ptr(parents), len(states), table.buffer_info()[0], _stream(stream)))
+        table.extend(s if type(s[0]) is int and type(s[1]) is int else (_ptr(s[0]) or 0, _ptr(s[1]) or 0, *s[2:]))
+    _check(load_library().lsr_beam_reorder(B, beams, K, _ptr(parents), len(states), table.buffer_info()[0], _stream(stream)))
 
 
 # ---- dropout (include/lsr_dropout.h) ----
