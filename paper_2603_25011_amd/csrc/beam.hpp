@@ -282,7 +282,9 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
                 break;
             }
             // Too many of this batch for the list (seldom: as where logits ascend): it is gone through again with a threshold that K of it, but no more than there is room for, reach,
-            // found bit by bit (all keys differ, so at the last bit it is the K-th).  The sums keep their reference, and the batch ends with a cut to its true K largest.
+            // found bit by bit (all keys differ, so at the last bit it is the K-th).  What `keep` does not take is not counted: a NaN's key is above all numbers', and a threshold
+            // of NaNs' keys would leave the list with fewer than K, of which the cut below reads the K-th.  (More than BEAM_CAP / 2 numbers of the batch beat the old threshold.)
+            // The sums keep their reference, and the batch ends with a cut to its true K largest.
             again = true;                        // (nothing of the batch is in `far` yet: what is above the reference was in the list, or equal to it)
             cold = cold0;
             ties = ties0;
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
                     float f;
                     if constexpr (sizeof(T) == 4) f = x[i];
                     else f = __uint_as_float((uint32_t)x[i] << 16);
-                    c += key_of(ordered(f), (uint32_t)(first + i)) >= higher ? 1 : 0;
+                    c += f == f && key_of(ordered(f), (uint32_t)(first + i)) >= higher ? 1 : 0;
                 }
 #pragma unroll
                 for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
