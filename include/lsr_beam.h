@@ -18,7 +18,9 @@ extern "C" {
  * For each of B sequences the K best continuations of its beams:
  *   s(m, v) = scores[b,m] + X[b beams + m, v] / temperature - lse(b, m),   lse = log sum_v exp(X[b beams + m, v] / temperature)
  * in descending order, equal ones by ascending beam and, of one beam, by descending logit and ascending token.  Scores are compared as
- * formed in 64 bits, with lse summed in float32 and 64 bits to about 1e-8.
+ * formed in 64 bits.  lse is off by about 1e-8 where the largest logits hold most of the sum, and by less than 3e-6 whatever they are (a term below the largest ones, a =
+ * log2 of its ratio to them, is formed in float32 to (1.4 |a| + 14) 2^-24 of itself; sums are 64 bits from a batch of a few thousand logits on).  Beams of equal rows have
+ * equal lse; continuations of different rows whose scores are closer than that may change places.
  *   X          [B beams, ldx] x_dtype (LSR_F32 or LSR_BF16), any alignment of its elements, ldx >= V
  *   scores     [B, beams] f32; a beam of -inf has no continuation, and its logits are not read
  *   finished   [B, beams] uint8 or NULL: a beam whose byte is not 0 has one continuation, end_id with its own score; its logits are not read

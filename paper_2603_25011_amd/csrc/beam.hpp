@@ -13,7 +13,8 @@ namespace lsr {
 //
 // Candidates of different beams are compared by scores that differ little, so the normaliser is summed more exactly than a float32 sum would be: logits that reach
 // the threshold above which the largest are collected (few, but most of the sum) are added in 64 bits, only those below it, each less than exp of the threshold, in
-// float32 and with the threshold as reference.  That reference also keeps the fast pass free of a running maximum: an exponential of what is below it cannot overflow.
+// float32 and with the threshold as reference, and these in 64 bits from batch to batch: a thread's float32 sum is never longer than a batch, or many equal terms would be off by
+// as many roundings in one direction (3e-5 with 2^21 logits a row).  Kept in LDS, where 16-bit logits leave no register for it: 64 x 8 x 30522 23.9 us, in registers 25.5.  That reference also keeps the fast pass free of a running maximum: an exponential of what is below it cannot overflow.
 // A vector without a logit at or above the threshold costs a multiply-add, an exponential, an addition and half a maximum per logit.  A logit in the list is
 // added when it leaves it, by the thread that ranks it, so the pass itself forms no exponential in 64 bits.
 // Bound by vector instructions per logit and, with few rows, by the latency of the two launches: 4 rows of 30522 in float32 6.8 + 5.1 us, 512 in bfloat16 17.2 + 7.2 (31 MB, read in 6.4
@@ -53,6 +54,7 @@ struct BeamShared {
     TopShared top;
     float by_rank[BEAM_CAP];     // all logits of the list in order, so that they are added in an order that does not go by chance
     double part[BEAM_WAVES];
+    double below[BEAM_THREADS];  // a thread's own (no registers are left for it)
 };
 
 // best[0 .. min(K, n)) = the largest of list[0 .. n), in order, and by_rank[0 .. n) the logits of all.  Whole workgroup; the list is complete (a barrier behind its last
@@ -153,7 +155,8 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
     bool ordered_list = false;                   // the list is its K largest, in order
     float tv, zc;                                // the reference, the threshold's value when it was last set for sure; times c
     bool plain;                                  // zc is small enough for one multiply-add (with very low logits or temperatures its rounding would be more than the sum)
-    float cold = 0.f;                            // this thread's sum below the reference, times 2^(-zc)
+    float cold = 0.f;                            // this thread's sum below the reference of the batch at hand, times 2^(-zc)
+    sh.below[tid] = 0.0;                         // and of the batches before it
     int ties = 0;                                // its logits equal to the reference that found no place in the list
     double sum = 0.0;                            // its sum of exp2((x - base) c) of all that is done with
     float base;                                  // an earlier reference
@@ -174,7 +177,8 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
             base = tv;
         }
         // (the fast sum's reference is zc as it was rounded)
-        sum += (double)cold * exp2(((double)tv - (double)base) * cd + (plain ? (double)zc - (double)tv * (double)c : 0.0)) + (double)ties * part(tv, base);
+        sum += (sh.below[tid] + (double)cold) * exp2(((double)tv - (double)base) * cd + (plain ? (double)zc - (double)tv * (double)c : 0.0)) + (double)ties * part(tv, base);
+        sh.below[tid] = 0.0;
         cold = 0.f;
         ties = 0;
     };
@@ -206,7 +210,6 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
     const int batch = BEAM_U * BEAM_THREADS;
     for (int b0 = 0; b0 == 0 || b0 < nvec; b0 += batch) {
         if (b0 + batch < nvec) fetch(next, b0 + batch);
-        const float cold0 = cold;
         const int ties0 = ties;
         bool again = false;
         for (;;) {
@@ -259,6 +262,8 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
             if (!again && have <= K + BEAM_SLACK) {
                 ordered_list = ordered_list && have == before;
                 before = have;
+                sh.below[tid] += (double)cold;
+                cold = 0.f;
                 __syncthreads();                 // everyone has read the count
                 break;
             }
@@ -286,7 +291,7 @@ __global__ __launch_bounds__(BEAM_THREADS, beam_resident(sizeof(T))) void beam_s
             // of NaNs' keys would leave the list with fewer than K, of which the cut below reads the K-th.  (More than BEAM_CAP / 2 numbers of the batch beat the old threshold.)
             // The sums keep their reference, and the batch ends with a cut to its true K largest.
             again = true;                        // (nothing of the batch is in `far` yet: what is above the reference was in the list, or equal to it)
-            cold = cold0;
+            cold = 0.f;
             ties = ties0;
             uint64_t t = 0;
             int reach = BEAM_CAP;
