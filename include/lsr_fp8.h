@@ -62,8 +62,10 @@ int lsr_fp8_quantize(int64_t rows, int64_t cols, int32_t x_dtype, const void* X,
  *   bias      [V] f32, or NULL for none
  *   out       [N, ldo] out_dtype (LSR_F32 or LSR_BF16), any alignment of its elements, ldo >= V
  *   workspace lsr_fp8_matmul_workspace_bytes (0 for LSR_E4M3: then it may be NULL; 0 also for an invalid shape)
- * For LSR_F32 results products are exact and sums are float32.  For LSR_BF16 results of more than a few rows the matrix cores add products in small groups, in
- * which what lies more than 13 bits below the largest is cut off: 2e-5 of the norm of the sums on normal values, under a rounding of 1.7e-3.
+ * For LSR_F32 results products are exact and sums are float32, in an order that does not depend on N: a row's results have the same bits whatever rows are beside it.
+ * For LSR_BF16 results of up to 24 rows (fewer where K is above 1536: N rows of 2 K + 16 bytes, K up to a multiple of 128, are at most 76 KB) the same sums are rounded.
+ * From there on the matrix cores add products in small groups, in which what lies more than 13 bits below the largest is cut off: 2e-5 of the norm of the sums on normal
+ * values (5e-5 where magnitudes spread over 2^8), under a rounding of 1.7e-3.  So a row's bfloat16 results in a call of few rows and in one of many may be a rounding apart.
  * A value of A or W below 2^-126 may count as zero; one above 1.9375 2^127 rounds to 2^128, which may count as infinite.  Exponents and bias are 4-byte aligned.
  * Limits: 1 <= N, V <= 2^22, N V < 2^36, 1 <= K <= 65536, ldw and the lda of bytes at most 2^23.
  */

@@ -80,7 +80,9 @@ class Fp8Head:
         self.bias = bias
 
     def logits(self, H: torch.Tensor, dtype: torch.dtype = torch.float32) -> torch.Tensor:
-        """[..., V] logits of hidden states H [..., D] (float32 or bfloat16), which are held in blocks of 128 within the call."""
+        """[..., V] logits of hidden states H [..., D] (float32 or bfloat16), which are held in blocks of 128 within the call.  A row's float32 logits do not depend on
+        the rows beside it; bfloat16 ones of few rows (up to 24) are those rounded, of more rows sums of the matrix cores' 8-bit instruction (2e-5 of their norm, then rounded), so that a row's may
+        be a rounding apart in a call of few rows and in one of many."""
         _on_gpu("Fp8Head.logits", H, self.W8)
         kind = _kind(H, "Fp8Head.logits", "H")
         if dtype not in _KIND:
@@ -152,7 +154,8 @@ class _Fp8Logits(torch.autograd.Function):
 
 def fp8_logits(H: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """[..., V] logits H W^T + bias of hidden states H [..., D] and a matrix W [V, D] (both float32 or both bfloat16), multiplied in 8-bit
-    floating point: H in blocks of 1 x 128 along its rows, W in blocks of 128 x 128.  `dtype` is that of the logits (float32 or bfloat16).
+    floating point: H in blocks of 1 x 128 along its rows, W in blocks of 128 x 128.  `dtype` is that of the logits (float32 or bfloat16; sums as in
+    Fp8Head.logits, those of a gradient by the type that it is stored in).
     Differentiable (once) in H, W and bias, the rounding to 8 bits passed over:  dH = q(dY) q(W),  dW = q(dY)^T q(H) with dY and H in blocks of
     128 tokens,  db = sum of dY.  Gradients come in the parameters' own dtypes.
     Where a step is captured into a graph, no result of an eager call on the same parameters may still hold its own autograd graph (autograd would
