@@ -55,7 +55,8 @@ typedef struct {
  *   parents  [B, K] int32 (4-byte aligned)
  *   states   n of them in HOST memory, read before the call returns
  * Any alignment (the widest access that addresses, strides and pieces allow).  No dst may overlap a src or another dst.
- * Limits: 1 <= B, beams, K; B beams, B K < 2^31; 0 <= n <= 4096; pieces >= 1, piece_bytes >= 1, pieces piece_bytes < 2^31; B K pieces piece_bytes < 2^40.
+ * Limits: 1 <= B, beams, K; B beams, B K < 2^31; 0 <= n <= 4096; pieces >= 1, piece_bytes >= 1, pieces piece_bytes < 2^31; B K pieces piece_bytes < 2^40 and,
+ * in accesses of 16 bytes or of as few as the alignment of an array's addresses, strides and pieces allows, at most 1024 (2^24 - 1) of them (16 GiB of single bytes).
  */
 int lsr_beam_reorder(int64_t B, int64_t beams, int64_t K, const int32_t* parents, int64_t n, const lsr_beam_state* states, lsr_stream_t stream);
 

@@ -97,7 +97,7 @@ def beam_reorder(states, parents: torch.Tensor, out=None):
     of any dtypes, all on one GPU), in one launch for up to 32 of them.  parents [B, K] int32 as beam_select gives them; a parent outside the beams gives zeros.
     `out`: tensors [B, K, ...] to write, whose addresses lie apart from each other's, the states' and the parents'; without it new ones.  Returns a tensor or a list, as
     `states` is one.  Strides are free; a tensor whose [b, m] is not pieces of equal length and distance (a cache of which only part of the length is in use
-    is) is copied first, and refused as `out`."""
+    is) is copied first, and refused as `out`.  A tensor whose addresses, strides or pieces are odd may have up to 16 GiB to write, in multiples of 2 bytes 32, and so on."""
     one = isinstance(states, torch.Tensor)
     states = [states] if one else list(states)
     if out is not None:
