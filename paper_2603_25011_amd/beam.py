@@ -61,8 +61,6 @@ def _layout(x: torch.Tensor):
             dims[-1] = (dims[-1][0] * n, st)
         else:
             dims.append((n, st))
-    if any(st < 0 for st in x.stride()):
-        return None
     if dims and dims[-1][1] == 1:
         inner = dims.pop()[0]
     else:

@@ -30,8 +30,7 @@ constexpr int beam_resident(int bytes) { return bytes == 4 ? 3 : 4; }
 constexpr int BEAM_CAP = 1024;                         // keys in the list
 constexpr int BEAM_SLACK = 96;                         // keys beyond K before it is cut: a cut costs two microseconds, a loose threshold a few more keys
 constexpr int BEAM_JOIN = 8192;                        // keys of one sequence that the joining launch holds
-constexpr float BEAM_LOWEST = -3.402823466e38f;
-constexpr uint32_t BEAM_LOWEST_BITS = 0x00800000u;     // ordered(BEAM_LOWEST); -inf lies below
+constexpr uint32_t BEAM_LOWEST_BITS = 0x00800000u;     // ordered() of the lowest float32; -inf lies below
 
 struct BeamSum { double s; float m; float pad; };      // sum of exp2((x - m) c); m = -inf: s is 0, or NaN
 
