@@ -13,12 +13,15 @@ namespace lsr {
 //
 // Candidates of different beams are compared by scores that differ little, so the normaliser is summed more exactly than a float32 sum would be: logits that reach
 // the threshold above which the largest are collected (few, but most of the sum) are added in 64 bits, only those below it, each less than exp of the threshold, in
-// float32 and with the threshold as reference, and these in 64 bits from batch to batch: a thread's float32 sum is never longer than a batch, or many equal terms would be off by
-// as many roundings in one direction (3e-5 with 2^21 logits a row).  Kept in LDS, where 16-bit logits leave no register for it: 64 x 8 x 30522 23.9 us, in registers 25.5.  That reference also keeps the fast pass free of a running maximum: an exponential of what is below it cannot overflow.
+// float32 and with the threshold as reference, and these in 64 bits from batch to batch: a thread's float32 sum is never longer than a batch, or many equal terms
+// would be off by as many roundings in one direction (3e-5 with 2^21 logits a row).  The 64-bit sum of batches lies in LDS, since 16-bit logits leave no register for it:
+// 64 x 8 x 30522 23.9 us, in registers 25.5.  The threshold as reference also keeps the fast pass free of a running maximum: an exponential of what is below it
+// cannot overflow.
 // A vector without a logit at or above the threshold costs a multiply-add, an exponential, an addition and half a maximum per logit.  A logit in the list is
 // added when it leaves it, by the thread that ranks it, so the pass itself forms no exponential in 64 bits.
-// Bound by vector instructions per logit and, with few rows, by the latency of the two launches: 4 rows of 30522 in float32 6.8 + 5.1 us, 512 in bfloat16 17.2 + 7.2 (31 MB, read in 6.4
-// at the rate of a copy), 240 of 250002 in float32, a fifth of them at their end, 49.8 + 6.9 (194 MB read, 40).
+// A wave issues about 16 vector instructions per logit and 450 for a segment's beginning and end.  512 rows of 30522 in bfloat16 take 17.3 + 7.9 us (31 MB, read in 6.4 at the rate of a
+// copy): vector instructions are issued in 69 % of the cycles, a third of them that fixed work.  240 rows of 250002 in float32, a fifth of them at their end, 56 to 60 + 7.0 (194 MB
+// read, 40): in 47 %, while waves wait (loads, barriers) for 60 % of their time.  4 rows of 30522 in float32 7.0 + 4.9: latency.
 constexpr int BEAM_THREADS = 256;
 constexpr int BEAM_U = 4;                              // 16-byte vectors per thread and batch
 constexpr int BEAM_WAVES = BEAM_THREADS / 64;
@@ -375,7 +378,8 @@ enum { BEAM_NONE = 0, BEAM_GOES_ON = 1, BEAM_FINISHED = 2, BEAM_NAN = 3 };
 // One workgroup per sequence.  Keys are dealt out place by place (all lists' first, then all their second) and evenly to the waves, so that the threads' maxima are the best
 // of the lists; a threshold comes of them bit by bit from each wave's ballots, what reaches it goes to a list in LDS, and a candidate's place is the number of better ones
 // (counting for each of the 256 maxima the larger ones instead took 1.2 to 2 us longer).  Latency bounds it, so the keys are on their way while the normalisers are formed, and
-// each thread keeps the scores of its first BEAM_OWN: 5.0 us for 4 beams with 14 segments and K = 8, 7.8 for 64 sequences of 8 beams with 2 and K = 16.
+// each thread keeps the scores of its first BEAM_OWN: 4.9 us for 4 beams with 14 segments and K = 8, 7.9 for 64 sequences of 8 beams with 2 and K = 16.  Its LDS (151 KB, for the largest
+// K and beams) leaves room for one workgroup per CU, which bounds calls of many sequences: 65536 of one beam take 1.3 ms.
 // More candidates than BEAM_RANKED at or above the threshold have equal scores as a rule (a head whose logits are all alike): ranking them against each other took 50 ms for 16 beams and K = 32.
 constexpr int BEAM_OWN = 4;
 constexpr int BEAM_RANKED = 256;
